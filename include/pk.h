@@ -13,8 +13,8 @@
  *     explicit zero padding.
  *
  * Conventions shared by every call:
- *   - Every tensor pointer is a DEVICE pointer to fp32 data.  The caller owns
- *     all memory; the library allocates no device memory and keeps no pointer
+ *   - Every tensor pointer is a DEVICE pointer, to fp32 data except in the
+ *     8-bit operators.  The caller owns all memory; the library allocates no device memory and keeps no pointer
  *     after a call returns.
  *   - Storage is row-major (C order).  A column-major caller maps onto the
  *     same call by swapping the operands: the column-major product
@@ -307,6 +307,85 @@ int pk_tune_conv2d_fwd(const float *x, int64_t N, int64_t H, int64_t W, int64_t 
                        int iters, void *stream, pk_tune_result *result);
 int pk_tune_reset(void);
 
+/*
+ * 8-bit operators: a layer whose weights and activations are held in 8-bit
+ * integers, one fp32 scale for each row (each token of the activations, each
+ * output channel of the weights).  An element stands for q * scale.
+ *
+ * Conventions beside the common ones: matrices are row-major with a leading
+ * dimension in elements; floating elements have one of the types below and
+ * their type's alignment, 8-bit ones any address and leading dimension (rows
+ * that start at multiples of 16 bytes are read fastest).  Dimensions and
+ * leading dimensions up to 2^30 (else PK_ERR_NOT_SUPPORTED).  Results are
+ * deterministic, and the calls need no workspace.
+ */
+typedef enum { PK_F32 = 0, PK_BF16 = 1, PK_F16 = 2 } pk_dtype;
+
+/*
+ * Rows to 8 bits: for each row z of x, with a = max |z|,
+ *   q = rint(z * (127 / a))  (ties to even, |q| <= 127),  scale = a / 127.
+ * A row with a < 127 * 2^-126 (a row of zeros) gets q = 0 and scale = 0; a row
+ * that holds an infinity or a NaN gets q = 0 and that infinity or NaN as its
+ * scale, so that it reads back, and multiplies, as NaN.
+ *   x       M x N of `dtype`, ldx >= max(1, N).
+ *   q       M x N, ldq >= max(1, N).      scale   M floats.
+ * N == 0 writes scale = 0.
+ */
+int pk_quantize_i8(const void *x, int dtype, int64_t M, int64_t N, int64_t ldx,
+                   int8_t *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, to 8 bits:
+ *   h = x + residual (x without one), summed in fp32 and rounded to `dtype`;
+ *   y = h * weight / sqrt(mean(h^2) + eps), rows of y to 8 bits as above.
+ * The factor 1 / sqrt(...) is common to a row and goes into its scale alone:
+ * q = rint(z * (127 / a)) for z = h * weight and a = max |z|, scale =
+ * a / sqrt(...) / 127; the rules for zeros, infinities and NaN are applied to
+ * z.  The mean is taken in fp32: rows whose sum of squares passes its range
+ * have scale 0.
+ *   residual      M x N or NULL.
+ *   weight        N elements of weight_dtype, which is `dtype` or PK_F32.
+ *   eps           >= 0.
+ *   sum           h, M x N of `dtype`, or NULL (no residual: must be NULL).  It
+ *                 may be the memory of residual or x (same leading dimension).
+ */
+int pk_rmsnorm_i8(const void *x, int dtype, int64_t M, int64_t N, int64_t ldx,
+                  const void *residual, int64_t ldr, const void *weight, int weight_dtype,
+                  float eps, void *sum, int64_t lds, int8_t *q, int64_t ldq, float *scale,
+                  void *stream);
+
+/*
+ * Gated activation to 8 bits: rows of act(gate) * up, computed in fp32.
+ *   PK_ACT_SILU   act(g) = g / (1 + exp(-g))
+ *   PK_ACT_GELU   act(g) = g / 2 * (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)))
+ * gate and up are M x N; the two halves of one M x 2N product are two views of
+ * it with its leading dimension.
+ */
+typedef enum { PK_ACT_SILU = 0, PK_ACT_GELU = 1 } pk_activation;
+int pk_gated_i8(const void *gate, int64_t ldg, const void *up, int64_t ldu, int dtype, int act,
+                int64_t M, int64_t N, int8_t *q, int64_t ldq, float *scale, void *stream);
+
+/* Rows read back: x = q * scale, rounded to `dtype`. */
+int pk_dequantize_i8(const int8_t *q, int64_t ldq, const float *scale, int64_t M, int64_t N,
+                     void *x, int dtype, int64_t ldx, void *stream);
+
+/*
+ * Product of 8-bit integers with a scale for each row of either side:
+ *   C[m][n] = a_scale[m] * b_scale[n] * sum_k A[m][k] * B[n][k] + bias[n]
+ * The sum is exact (32-bit integers); it is converted to fp32, scaled and added
+ * to there, and rounded to `dtype` once.
+ *   A, lda     M x K activations, lda >= max(1, K).     a_scale   M floats.
+ *   B, ldb     N x K weights (a row is an output channel), ldb >= max(1, K).
+ *   b_scale    N floats.      bias   N floats or NULL.
+ *   C, ldc     M x N of `dtype`, ldc >= max(1, N).
+ * K <= 131071 (128 * 128 * K stays below 2^31; else PK_ERR_NOT_SUPPORTED).
+ * M == 0 or N == 0 does nothing; K == 0 gives the bias, or zeros, without
+ * reading A, B or the scales.
+ */
+int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
+               const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
+               void *C, int dtype, int64_t ldc, void *stream);
+
 /* Static text for a status code. */
 const char *pk_status_string(int status);
 
@@ -315,7 +394,8 @@ int pk_last_invalid_param(void);
 
 /* Name of the compiled configuration this thread's last pk_sgemm or
  * pk_conv2d_fwd call ran ("" after an error or an empty problem, "scale" for
- * C <- beta * C).  Static storage. */
+ * C <- beta * C); of the 8-bit operators, the operator's name, with the tile
+ * that pk_gemm_i8 ran.  Static storage. */
 const char *pk_last_config_name(void);
 
 /*

@@ -5,6 +5,6 @@ include/pk.h); this package only marshals arguments into it.
 """
 from .binding import (PkError, PkLibraryMissing, configs, conv2d_fwd, conv2d_out_dims,  # noqa: F401
                       conv2d_same_pads, conv2d_winograd, conv2d_winograd_workspace_bytes,
-                      conv2d_workspace_bytes, force_config, force_splits, gemm, tune_conv2d, tune_gemm,
-                      tune_reset,
+                      conv2d_workspace_bytes, dequantize_i8, force_config, force_splits, gated_i8, gemm, gemm_i8,
+                      quantize_i8, rmsnorm_i8, tune_conv2d, tune_gemm, tune_reset,
                       last_config_name, last_invalid_param, load)

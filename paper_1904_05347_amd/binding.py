@@ -91,6 +91,12 @@ SIGNATURES = {
                                           _i64, _i64, _i64, _i64, _i64, _i64, _p, _i64, _i64,
                                           _p, ctypes.c_size_t, ctypes.c_int, _p, ctypes.POINTER(TuneResult)]),
     "pk_tune_reset": (ctypes.c_int, []),
+    "pk_quantize_i8": (ctypes.c_int, [_p, ctypes.c_int, _i64, _i64, _i64, _p, _i64, _p, _p]),
+    "pk_rmsnorm_i8": (ctypes.c_int, [_p, ctypes.c_int, _i64, _i64, _i64, _p, _i64, _p, ctypes.c_int, ctypes.c_float,
+                                     _p, _i64, _p, _i64, _p, _p]),
+    "pk_gated_i8": (ctypes.c_int, [_p, _i64, _p, _i64, ctypes.c_int, ctypes.c_int, _i64, _i64, _p, _i64, _p, _p]),
+    "pk_dequantize_i8": (ctypes.c_int, [_p, _i64, _p, _i64, _i64, _p, ctypes.c_int, _i64, _p]),
+    "pk_gemm_i8": (ctypes.c_int, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _p, ctypes.c_int, _i64, _p]),
     "pk_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "pk_last_invalid_param": (ctypes.c_int, []),
     "pk_last_config_name": (ctypes.c_char_p, []),
@@ -131,7 +137,8 @@ def load():
 EXT_PATH = os.path.join(HERE, "_pk_torch.so")
 _NATIVE_ENTRIES = ("pk_sgemm_ws", "pk_sgemm_workspace_bytes_for", "pk_conv2d_fwd", "pk_conv2d_workspace_bytes_for",
                    "pk_conv2d_out_dims", "pk_conv2d_same_pads", "pk_conv2d_winograd_tile_fwd",
-                   "pk_conv2d_winograd_tile_workspace_bytes")
+                   "pk_conv2d_winograd_tile_workspace_bytes", "pk_quantize_i8", "pk_rmsnorm_i8", "pk_gated_i8",
+                   "pk_dequantize_i8", "pk_gemm_i8")
 _native = None
 
 
@@ -143,6 +150,7 @@ class _PythonOnly:
         return None
 
     conv2d_fwd = conv2d_winograd = gemm
+    quantize_i8 = rmsnorm_i8 = gated_i8 = dequantize_i8 = gemm_i8 = gemm
 
 
 def _load_native():
@@ -493,6 +501,188 @@ def conv2d_winograd(x, w, padding="SAME", out=None, workspace=None, tile=2):
                                   pt, pl, pb, pr, out.data_ptr(), Ho, Wo, int(tile), workspace.data_ptr(),
                                   workspace.numel() * 4, _stream_handle(out))
     _check(st, "pk_conv2d_winograd_tile_fwd")
+    return out
+
+
+# ------------------------------------------------------- 8-bit operators
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def _dtype_code(dtype, what):
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16" % what)
+    return code
+
+
+def _check_cuda(t, what, dtype=None, like=None):
+    """A tensor on a HIP device (that of ``like``), of this type."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or (dtype is not None and t.dtype != dtype):
+        raise TypeError("%s must be %s tensor on a HIP device"
+                        % (what, "a" if dtype is None else "a %s" % str(dtype).replace("torch.", "")))
+    if like is not None and t.device != like.device:
+        raise ValueError("%s must be on %s" % (what, like.device))
+
+
+def _check_vector(t, n, what, dtype, like):
+    _check_cuda(t, what, dtype, like)
+    if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be a contiguous vector of %d" % (what, n))
+
+
+def _rows_out(M, N, like, out, scale):
+    """The 8-bit output and its scales: the caller's, or new ones whose rows
+    start at multiples of 16 bytes."""
+    import torch
+    if out is None:
+        out = torch.empty_strided((M, N), (max(1, (N + 15) // 16 * 16), 1), dtype=torch.int8, device=like.device)
+    _check_cuda(out, "out", torch.int8, like)
+    if tuple(out.shape) != (M, N):
+        raise ValueError("out must be %d x %d" % (M, N))
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=like.device)
+    _check_vector(scale, M, "scale", torch.float32, like)
+    return out, _ld_2d(out, "out"), scale
+
+
+def quantize_i8(x, out=None, scale=None):
+    """The rows of ``x`` (M x N, float32, bfloat16 or float16) as 8-bit integers
+    with a scale each: ``(q, scale)``, q * scale[:, None] standing for x (see
+    pk_quantize_i8).  New outputs' rows start at multiples of 16 bytes."""
+    r = (_native or _load_native()).quantize_i8(x, out, scale)
+    if r is not None:
+        return r
+    _check_cuda(x, "x")
+    dt = _dtype_code(x.dtype, "x")
+    ldx = _ld_2d(x, "x")
+    M, N = x.shape
+    out, ldq, scale = _rows_out(M, N, x, out, scale)
+    _check(load().pk_quantize_i8(x.data_ptr(), dt, M, N, ldx, out.data_ptr(), ldq, scale.data_ptr(),
+                                 _stream_handle(x)), "pk_quantize_i8")
+    return out, scale
+
+
+def rmsnorm_i8(x, weight, residual=None, eps=1e-6, sum_out=None, out=None, scale=None):
+    """Root-mean-square norm of ``x + residual`` with the output in 8 bits:
+    ``(q, scale, h)``, h the sum in x's type (x itself without a residual) and
+    q * scale[:, None] standing for h * weight / sqrt(mean(h^2) + eps) (see
+    pk_rmsnorm_i8).  ``weight`` has x's type or float32.  ``sum_out`` receives h
+    and may be ``residual`` or ``x`` itself; a new tensor when None."""
+    r = (_native or _load_native()).rmsnorm_i8(x, weight, residual, eps, sum_out, out, scale)
+    if r is not None:
+        return r
+    import torch
+    _check_cuda(x, "x")
+    dt = _dtype_code(x.dtype, "x")
+    ldx = _ld_2d(x, "x")
+    M, N = x.shape
+    _check_cuda(weight, "weight", None, x)
+    if weight.dtype not in (x.dtype, torch.float32):
+        raise TypeError("weight must have x's type or float32")
+    _check_vector(weight, N, "weight", weight.dtype, x)
+    ldr = lds = 0
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out needs a residual")
+    else:
+        if sum_out is None:
+            sum_out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        for t, what in ((residual, "residual"), (sum_out, "sum_out")):
+            _check_cuda(t, what, x.dtype, x)
+            if tuple(t.shape) != (M, N):
+                raise ValueError("%s must be %d x %d" % (what, M, N))
+        ldr, lds = _ld_2d(residual, "residual"), _ld_2d(sum_out, "sum_out")
+    out, ldq, scale = _rows_out(M, N, x, out, scale)
+    _check(load().pk_rmsnorm_i8(x.data_ptr(), dt, M, N, ldx, None if residual is None else residual.data_ptr(), ldr,
+                                weight.data_ptr(), _dtype_code(weight.dtype, "weight"), float(eps),
+                                None if residual is None else sum_out.data_ptr(), lds, out.data_ptr(), ldq,
+                                scale.data_ptr(), _stream_handle(x)), "pk_rmsnorm_i8")
+    return out, scale, x if residual is None else sum_out
+
+
+def gated_i8(gate, up, activation="silu", out=None, scale=None):
+    """act(gate) * up with the output in 8 bits: ``(q, scale)`` (see pk_gated_i8).
+    ``activation`` is 'silu' or 'gelu' (its tanh form).  The halves of one
+    product are two slices of it: ``gated_i8(p[:, :n], p[:, n:])``."""
+    r = (_native or _load_native()).gated_i8(gate, up, activation, out, scale)
+    if r is not None:
+        return r
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation must be 'silu' or 'gelu'")
+    _check_cuda(gate, "gate")
+    dt = _dtype_code(gate.dtype, "gate")
+    ldg = _ld_2d(gate, "gate")
+    _check_cuda(up, "up", gate.dtype, gate)
+    if up.shape != gate.shape:
+        raise ValueError("gate and up must have the same shape")
+    ldu = _ld_2d(up, "up")
+    M, N = gate.shape
+    out, ldq, scale = _rows_out(M, N, gate, out, scale)
+    _check(load().pk_gated_i8(gate.data_ptr(), ldg, up.data_ptr(), ldu, dt, ACTIVATIONS[activation], M, N,
+                              out.data_ptr(), ldq, scale.data_ptr(), _stream_handle(gate)), "pk_gated_i8")
+    return out, scale
+
+
+def dequantize_i8(q, scale, dtype=None, out=None):
+    """q * scale[:, None] in ``dtype`` (float32, bfloat16 or float16; that of
+    ``out``, or float32, when None)."""
+    r = (_native or _load_native()).dequantize_i8(q, scale, dtype, out)
+    if r is not None:
+        return r
+    import torch
+    _check_cuda(q, "q", torch.int8)
+    ldq = _ld_2d(q, "q")
+    M, N = q.shape
+    _check_vector(scale, M, "scale", torch.float32, q)
+    if out is None:
+        dtype = torch.float32 if dtype is None else dtype
+        _dtype_code(dtype, "dtype")
+        out = torch.empty((M, N), dtype=dtype, device=q.device)
+    _check_cuda(out, "out", dtype, q)
+    dt = _dtype_code(out.dtype, "out")
+    if tuple(out.shape) != (M, N):
+        raise ValueError("out must be %d x %d" % (M, N))
+    _check(load().pk_dequantize_i8(q.data_ptr(), ldq, scale.data_ptr(), M, N, out.data_ptr(), dt, _ld_2d(out, "out"),
+                                   _stream_handle(q)), "pk_dequantize_i8")
+    return out
+
+
+def gemm_i8(a, b, a_scale, b_scale, bias=None, dtype=None, out=None):
+    """Product of 8-bit integers with a scale for each row of either side:
+    out[m, n] = a_scale[m] * b_scale[n] * sum_k a[m, k] * b[n, k] + bias[n].
+
+    ``a`` is M x K (tokens), ``b`` N x K (a row is an output channel), both int8
+    row-major views with unit column stride; the sum is exact.  The result is
+    rounded once, to ``dtype`` (that of ``out``, or bfloat16, when None).
+    """
+    r = (_native or _load_native()).gemm_i8(a, b, a_scale, b_scale, bias, dtype, out)
+    if r is not None:
+        return r
+    import torch
+    _check_cuda(a, "a", torch.int8)
+    _check_cuda(b, "b", torch.int8, a)
+    lda, ldb = _ld_2d(a, "a"), _ld_2d(b, "b")
+    (M, K), (N, Kb) = a.shape, b.shape
+    if Kb != K:
+        raise ValueError("inner dimensions differ: %d vs %d" % (K, Kb))
+    _check_vector(a_scale, M, "a_scale", torch.float32, a)
+    _check_vector(b_scale, N, "b_scale", torch.float32, a)
+    if bias is not None:
+        _check_vector(bias, N, "bias", torch.float32, a)
+    if out is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+        _dtype_code(dtype, "dtype")
+        out = torch.empty((M, N), dtype=dtype, device=a.device)
+    _check_cuda(out, "out", dtype, a)
+    dt = _dtype_code(out.dtype, "out")
+    if tuple(out.shape) != (M, N):
+        raise ValueError("out must be %d x %d" % (M, N))
+    _check(load().pk_gemm_i8(M, N, K, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
+                             None if bias is None else bias.data_ptr(), out.data_ptr(), dt, _ld_2d(out, "out"),
+                             _stream_handle(a)), "pk_gemm_i8")
     return out
 
 

@@ -18,6 +18,7 @@
 #include <string_view>
 
 #include "../../include/pk.h"
+#include "pk_api_state.hpp"
 #include "pk_configs.hpp"
 #include "pk_cost.hpp"
 
@@ -990,6 +991,14 @@ int out_dims(int64_t H, int64_t W, int64_t KH, int64_t KW, int64_t sh, int64_t s
 }
 
 }  // namespace
+
+namespace pk {
+
+void api_begin() { begin(); }
+int api_invalid(int position) { return invalid(position); }
+void api_ran(const char *config) { t_last_config = config; }
+
+}  // namespace pk
 
 extern "C" {
 

@@ -1,5 +1,5 @@
 // pk_torch.cpp -- the tensor calls of binding.py (gemm, conv2d_fwd,
-// conv2d_winograd) marshalled natively: torch tensors in, one C-ABI call on the
+// conv2d_winograd and the 8-bit operators) marshalled natively: torch tensors in, one C-ABI call on the
 // current stream, the output tensor out.
 //
 // Why: a 64 x 64 x 64 product takes the GPU 4 us, the C-ABI call 0.8 us and
@@ -21,8 +21,10 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -41,6 +43,11 @@ decltype(&pk_conv2d_out_dims) f_out_dims;
 decltype(&pk_conv2d_same_pads) f_same_pads;
 decltype(&pk_conv2d_winograd_tile_fwd) f_winograd;
 decltype(&pk_conv2d_winograd_tile_workspace_bytes) f_winograd_workspace_bytes;
+decltype(&pk_quantize_i8) f_quantize_i8;
+decltype(&pk_rmsnorm_i8) f_rmsnorm_i8;
+decltype(&pk_gated_i8) f_gated_i8;
+decltype(&pk_dequantize_i8) f_dequantize_i8;
+decltype(&pk_gemm_i8) f_gemm_i8;
 PyObject *f_check;  // binding._check(status, entry point): raises
 
 // The answer to a status other than PK_OK.
@@ -290,16 +297,269 @@ PyObject *py_conv2d_winograd(PyObject *, PyObject *const *args, Py_ssize_t nargs
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses, check): the eight entry points above, in their order, and the
+// ------------------------------------------------------- 8-bit operators
+
+int dtype_code(at::ScalarType t)
+{
+    return t == at::kFloat ? PK_F32 : t == at::kBFloat16 ? PK_BF16 : t == at::kHalf ? PK_F16 : -1;
+}
+
+// A plain strided tensor on a GPU, or NULL.
+const at::Tensor *on_gpu(PyObject *o)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided ? &t : nullptr;
+}
+
+// A plain matrix of float32, bfloat16 or float16, with its code and leading dimension.
+const at::Tensor *matrix(PyObject *o, int *code, int64_t *ld)
+{
+    const at::Tensor *t = on_gpu(o);
+    if (!t || (*code = dtype_code(t->scalar_type())) < 0 || (*ld = ld_2d(*t)) < 0) return nullptr;
+    return t;
+}
+
+const at::Tensor *matrix_i8(PyObject *o, int64_t *ld)
+{
+    const at::Tensor *t = on_gpu(o);
+    return t && t->scalar_type() == at::kChar && (*ld = ld_2d(*t)) >= 0 ? t : nullptr;
+}
+
+// A contiguous vector of n elements of this type on that device.
+const at::Tensor *vec(PyObject *o, int64_t n, at::ScalarType type, const at::Tensor &like)
+{
+    const at::Tensor *t = on_gpu(o);
+    if (!t || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1) ||
+        t->device() != like.device())
+        return nullptr;
+    return t;
+}
+
+bool same_shape(const at::Tensor &t, int64_t M, int64_t N, const at::Tensor &like)
+{
+    return t.dim() == 2 && t.size(0) == M && t.size(1) == N && t.device() == like.device();
+}
+
+// The 8-bit output and its scales: the caller's, or new ones whose rows start
+// at multiples of 16 bytes.
+struct RowsOut {
+    at::Tensor q, scale;
+    int64_t ld;
+};
+
+bool rows_out(PyObject *out, PyObject *scale, int64_t M, int64_t N, const at::Tensor &like, RowsOut *r)
+{
+    if (out == Py_None) {
+        r->ld = std::max<int64_t>(1, (N + 15) / 16 * 16);
+        r->q = at::empty_strided({M, N}, {r->ld, 1}, like.options().dtype(at::kChar));
+    } else {
+        const at::Tensor *t = matrix_i8(out, &r->ld);
+        if (!t || !same_shape(*t, M, N, like)) return false;
+        r->q = *t;
+    }
+    if (scale == Py_None) {
+        r->scale = at::empty({M}, like.options().dtype(at::kFloat));
+    } else {
+        const at::Tensor *t = vec(scale, M, at::kFloat, like);
+        if (!t) return false;
+        r->scale = *t;
+    }
+    return true;
+}
+
+// `given`, or the new tensor in its place.
+PyObject *given_or(PyObject *given, at::Tensor &&t)
+{
+    if (given == Py_None) return THPVariable_Wrap(std::move(t));
+    Py_INCREF(given);
+    return given;
+}
+
+PyObject *pair(PyObject *out, PyObject *scale, RowsOut &&r)
+{
+    PyObject *a = given_or(out, std::move(r.q)), *b = a ? given_or(scale, std::move(r.scale)) : nullptr;
+    PyObject *t = b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return t;
+}
+
+// quantize_i8(x, out, scale)
+PyObject *py_quantize_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int dt;
+    int64_t ldx;
+    RowsOut r;
+    if (nargs != 3 || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *x = matrix(args[0], &dt, &ldx);
+    if (!x || !rows_out(args[1], args[2], x->size(0), x->size(1), *x, &r)) Py_RETURN_NONE;
+    void *stream = stream_of(*x);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_quantize_i8(x->data_ptr(), dt, x->size(0), x->size(1), ldx, (int8_t *)r.q.data_ptr(), r.ld,
+                       (float *)r.scale.data_ptr(), stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_quantize_i8");
+    return pair(args[1], args[2], std::move(r));
+    END_HANDLE_TH_ERRORS
+}
+
+// rmsnorm_i8(x, weight, residual, eps, sum_out, out, scale)
+PyObject *py_rmsnorm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int dt, dr, wt;
+    int64_t ldx, ldr = 0, lds = 0;
+    float eps;
+    RowsOut r;
+    if (nargs != 7 || !as_float(args[3], &eps) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *x = matrix(args[0], &dt, &ldx), *w = on_gpu(args[1]), *res = nullptr;
+    if (!x || !w) Py_RETURN_NONE;
+    const int64_t M = x->size(0), N = x->size(1);
+    wt = dtype_code(w->scalar_type());
+    if ((wt != dt && wt != PK_F32) || !vec(args[1], N, w->scalar_type(), *x)) Py_RETURN_NONE;
+    at::Tensor sum;
+    if (args[2] == Py_None) {
+        if (args[4] != Py_None) Py_RETURN_NONE;
+    } else {
+        res = matrix(args[2], &dr, &ldr);
+        if (!res || dr != dt || !same_shape(*res, M, N, *x)) Py_RETURN_NONE;
+        if (args[4] == Py_None) {
+            sum = at::empty({M, N}, x->options());
+            lds = std::max<int64_t>(N, 1);
+        } else {
+            const at::Tensor *t = matrix(args[4], &dr, &lds);
+            if (!t || dr != dt || !same_shape(*t, M, N, *x)) Py_RETURN_NONE;
+            sum = *t;
+        }
+    }
+    if (!rows_out(args[5], args[6], M, N, *x, &r)) Py_RETURN_NONE;
+    void *stream = stream_of(*x);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_rmsnorm_i8(x->data_ptr(), dt, M, N, ldx, res ? res->data_ptr() : nullptr, ldr, w->data_ptr(), wt, eps,
+                      res ? sum.data_ptr() : nullptr, lds, (int8_t *)r.q.data_ptr(), r.ld,
+                      (float *)r.scale.data_ptr(), stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_rmsnorm_i8");
+    PyObject *a = given_or(args[5], std::move(r.q)), *b = a ? given_or(args[6], std::move(r.scale)) : nullptr;
+    PyObject *c = !b ? nullptr : res ? given_or(args[4], std::move(sum)) : given_or(args[0], at::Tensor());
+    PyObject *t = c ? PyTuple_Pack(3, a, b, c) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    Py_XDECREF(c);
+    return t;
+    END_HANDLE_TH_ERRORS
+}
+
+// gated_i8(gate, up, activation, out, scale)
+PyObject *py_gated_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int dt, du;
+    int64_t ldg, ldu;
+    RowsOut r;
+    if (nargs != 5 || !PyUnicode_CheckExact(args[2]) || modes_active()) Py_RETURN_NONE;
+    const int act = PyUnicode_CompareWithASCIIString(args[2], "silu") == 0   ? PK_ACT_SILU
+                    : PyUnicode_CompareWithASCIIString(args[2], "gelu") == 0 ? PK_ACT_GELU
+                                                                             : -1;
+    const at::Tensor *gate = matrix(args[0], &dt, &ldg), *up = matrix(args[1], &du, &ldu);
+    if (act < 0 || !gate || !up || du != dt || !same_shape(*up, gate->size(0), gate->size(1), *gate)) Py_RETURN_NONE;
+    if (!rows_out(args[3], args[4], gate->size(0), gate->size(1), *gate, &r)) Py_RETURN_NONE;
+    void *stream = stream_of(*gate);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_gated_i8(gate->data_ptr(), ldg, up->data_ptr(), ldu, dt, act, gate->size(0), gate->size(1),
+                    (int8_t *)r.q.data_ptr(), r.ld, (float *)r.scale.data_ptr(), stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_gated_i8");
+    return pair(args[3], args[4], std::move(r));
+    END_HANDLE_TH_ERRORS
+}
+
+// The floating output of M x N: the caller's, or a new one of the type asked
+// for (`standard` when none is).
+bool float_out(PyObject *out, PyObject *dtype, at::ScalarType standard, int64_t M, int64_t N, const at::Tensor &like,
+               at::Tensor *t, int *code, int64_t *ld)
+{
+    if (dtype != Py_None && !THPDtype_Check(dtype)) return false;
+    if (out == Py_None) {
+        const at::ScalarType type = dtype == Py_None ? standard : ((THPDtype *)dtype)->scalar_type;
+        if ((*code = dtype_code(type)) < 0) return false;
+        *t = at::empty({M, N}, like.options().dtype(type));
+        *ld = std::max<int64_t>(N, 1);
+        return true;
+    }
+    const at::Tensor *p = matrix(out, code, ld);
+    if (!p || (dtype != Py_None && p->scalar_type() != ((THPDtype *)dtype)->scalar_type) || !same_shape(*p, M, N, like))
+        return false;
+    *t = *p;
+    return true;
+}
+
+// dequantize_i8(q, scale, dtype, out)
+PyObject *py_dequantize_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int dt;
+    int64_t ldq, ldx;
+    at::Tensor x;
+    if (nargs != 4 || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *q = matrix_i8(args[0], &ldq);
+    if (!q) Py_RETURN_NONE;
+    const int64_t M = q->size(0), N = q->size(1);
+    const at::Tensor *scale = vec(args[1], M, at::kFloat, *q);
+    if (!scale || !float_out(args[3], args[2], at::kFloat, M, N, *q, &x, &dt, &ldx)) Py_RETURN_NONE;
+    void *stream = stream_of(*q);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_dequantize_i8((const int8_t *)q->data_ptr(), ldq, (const float *)scale->data_ptr(), M, N, x.data_ptr(), dt,
+                         ldx, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_dequantize_i8");
+    return given_or(args[3], std::move(x));
+    END_HANDLE_TH_ERRORS
+}
+
+// gemm_i8(a, b, a_scale, b_scale, bias, dtype, out)
+PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int dt;
+    int64_t lda, ldb, ldc;
+    at::Tensor c;
+    if (nargs != 7 || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *a = matrix_i8(args[0], &lda), *b = matrix_i8(args[1], &ldb), *bias = nullptr;
+    if (!a || !b || a->size(1) != b->size(1) || a->device() != b->device()) Py_RETURN_NONE;
+    const int64_t M = a->size(0), N = b->size(0), K = a->size(1);
+    const at::Tensor *sa = vec(args[2], M, at::kFloat, *a), *sb = vec(args[3], N, at::kFloat, *a);
+    if (!sa || !sb || (args[4] != Py_None && !(bias = vec(args[4], N, at::kFloat, *a)))) Py_RETURN_NONE;
+    if (!float_out(args[6], args[5], at::kBFloat16, M, N, *a, &c, &dt, &ldc)) Py_RETURN_NONE;
+    void *stream = stream_of(*a);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_gemm_i8(M, N, K, (const int8_t *)a->data_ptr(), lda, (const float *)sa->data_ptr(),
+                   (const int8_t *)b->data_ptr(), ldb, (const float *)sb->data_ptr(),
+                   bias ? (const float *)bias->data_ptr() : nullptr, c.data_ptr(), dt, ldc, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_gemm_i8");
+    return given_or(args[6], std::move(c));
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses, check): the entry points above, in their order, and the
 // function that raises for a status.
 PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 9) {
-        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of eight entry points and a function");
+    constexpr int kEntries = 13;
+    if (nargs != kEntries + 1) {
+        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of thirteen entry points and a function");
         return nullptr;
     }
-    void *p[8];
-    for (int i = 0; i < 8; ++i) {
+    void *p[kEntries];
+    for (int i = 0; i < kEntries; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
@@ -314,8 +574,13 @@ PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     f_same_pads = (decltype(f_same_pads))p[5];
     f_winograd = (decltype(f_winograd))p[6];
     f_winograd_workspace_bytes = (decltype(f_winograd_workspace_bytes))p[7];
-    Py_INCREF(args[8]);
-    Py_XSETREF(f_check, args[8]);
+    f_quantize_i8 = (decltype(f_quantize_i8))p[8];
+    f_rmsnorm_i8 = (decltype(f_rmsnorm_i8))p[9];
+    f_gated_i8 = (decltype(f_gated_i8))p[10];
+    f_dequantize_i8 = (decltype(f_dequantize_i8))p[11];
+    f_gemm_i8 = (decltype(f_gemm_i8))p[12];
+    Py_INCREF(args[kEntries]);
+    Py_XSETREF(f_check, args[kEntries]);
     Py_RETURN_NONE;
 }
 
@@ -324,6 +589,11 @@ PyMethodDef kMethods[] = {
     {"gemm", (PyCFunction)(void (*)(void))py_gemm, METH_FASTCALL, nullptr},
     {"conv2d_fwd", (PyCFunction)(void (*)(void))py_conv2d_fwd, METH_FASTCALL, nullptr},
     {"conv2d_winograd", (PyCFunction)(void (*)(void))py_conv2d_winograd, METH_FASTCALL, nullptr},
+    {"quantize_i8", (PyCFunction)(void (*)(void))py_quantize_i8, METH_FASTCALL, nullptr},
+    {"rmsnorm_i8", (PyCFunction)(void (*)(void))py_rmsnorm_i8, METH_FASTCALL, nullptr},
+    {"gated_i8", (PyCFunction)(void (*)(void))py_gated_i8, METH_FASTCALL, nullptr},
+    {"dequantize_i8", (PyCFunction)(void (*)(void))py_dequantize_i8, METH_FASTCALL, nullptr},
+    {"gemm_i8", (PyCFunction)(void (*)(void))py_gemm_i8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
