@@ -119,10 +119,16 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 // ------------------------------------------------------------- many rows of A
 //
 // A work-group makes a BM x BN tile of C, its WM x WN waves a part each.  Both
-// operands pass through LDS in K-blocks of 128 bytes, two stages of it: while
-// one is multiplied the next is copied straight from memory into the other
-// (DMA; operands whose rows start at multiples of four bytes), or is in flight
-// to registers and written there afterwards (any other alignment).
+// operands pass through LDS in K-blocks of 128 bytes, STAGES of them: while one
+// is multiplied the next ones are copied straight from memory (DMA; operands
+// whose rows start at multiples of four bytes), or the next one is in flight to
+// registers and written there afterwards (any other alignment; two stages).
+//
+// A block is multiplied in two halves of 64, and the operands of a half are read
+// from LDS while the half before it is multiplied.  So the work-group's only
+// barrier of a block stands where every wave has a half's operands in registers
+// and its products ahead of it: nobody waits for LDS after a barrier.
+//
 // A row's eight 16-byte chunks lie in LDS with their position's low bits
 // exchanged by the row's, so that the sixteen rows a wave reads at once, 128
 // bytes apart, lie in different banks.
@@ -137,9 +143,10 @@ __device__ __forceinline__ int swizzle_a(int row) { return row & 7; }
 template <int TN>
 __device__ __forceinline__ int swizzle_b(int row) { return (row & 3) | (row / (4 * TN) & 1) << 2; }
 
-// A tile's rows of an operand for copies from memory straight into LDS.  They
-// stop at the operand's last element (its four-byte word, which lies in memory
-// whole): the last row's last chunk may reach past it.
+// A tile's rows of an operand for copies from memory straight into LDS.  What
+// lies past the operand's last element (its four-byte word, which lies in memory
+// whole) is not read and arrives as zeros: rows past the last, and what the last
+// row's last chunk has past its end.
 struct Source {
     __amdgpu_buffer_rsrc_t rs;
     __device__ __forceinline__ Source(const int8_t *at, int64_t rows, int64_t ld, int K)
@@ -147,147 +154,229 @@ struct Source {
         const int64_t bytes = ((rows - 1) * ld + K + 3) & ~(int64_t)3;
         rs = __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, bytes < 0x7fffffff ? (int)bytes : 0x7fffffff, 0x00020000);
     }
-    // the wave's 64 lanes' 16 bytes at off + k, one after the other to `to`; zeros for off < 0
+    // the wave's 64 lanes' 16 bytes at off + k (k < K), one after the other to
+    // `to`; zeros for off < 0.  Written out, because the compiler would wait for
+    // every such copy before the next read of LDS, whichever stage that reads;
+    // the kernel's own waits are at its barriers.  A copy's use of m0 comes one
+    // wait state after it is set.
     __device__ __forceinline__ void copy16(int8_t *to, int off, int k) const
     {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)to, 16, off, k, 0, 0);
+        const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :
+                     : "s"(at), "v"(off), "s"(rs), "s"(k)
+                     : "memory", "m0");
     }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool DMA>
-__global__ void __launch_bounds__(WM * WN * 64) gemm_i8_tile_kernel(Args p, int tiles_m, int tiles_n, int group_m)
+template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool DMA>
+__global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, int tiles_m, int tiles_n, int group_m)
 {
     constexpr int BK = 128, NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * BK;
-    constexpr int LA = BM / (8 * NW), LB = BN / (8 * NW);  // copies of 16 bytes a lane, for A and for B
+    constexpr int LA = BM / (8 * NW), LB = BN / (8 * NW), L = LA + LB;  // copies of 16 bytes a lane and block
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM * WM * 16 == BM && TN * WN * 16 == BN, "whole copies");
-    __shared__ __attribute__((aligned(16))) int8_t lds[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    static_assert(DMA ? (STAGES - 2) * L < 64 : STAGES == 2, "copies in flight are counted in six bits");
+    static_assert(BM <= 256 && BN <= 256, "offsets in a tile are 32-bit for leading dimensions up to kMostLd");
+    __shared__ __attribute__((aligned(16))) int8_t lds[STAGES * STAGE];
+    __shared__ __attribute__((aligned(16))) float factors[BM + 2 * BN];  // the scales of the tile's rows and columns, the bias
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15,
+              g = lane >> 4;
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn;
     pk::tile_of_ints(tiles_m, tiles_n, group_m, pk::xcd_tile(blockIdx.x, tiles_m * tiles_n, 8), tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, K = p.K;
+    const int m0 = tm * BM, n0 = tn * BN, K = p.K, blocks = (K + BK - 1) / BK;
+    const int lda = (int)p.lda, ldb = (int)p.ldb;
     const int8_t *A = p.A + (int64_t)m0 * p.lda, *B = p.B + (int64_t)n0 * p.ldb;
     const int rows_a = p.M - m0, rows_b = p.N - n0;
 
-    // copy slot u of this lane: row (u NW + wave) 8 + lane / 8 of the tile, chunk position lane % 8
-    int off_a[LA], off_b[LB], k_a[LA], k_b[LB];
+    // copy u of this lane: row (u NW + wave) 8 + lane / 8 of the tile, chunk position lane % 8;
+    // the swizzles do not depend on u
+    const int row = wave * 8 + lane / 8;
+    const int k_a = ((lane & 7) ^ swizzle_a(row)) * 16, k_b = ((lane & 7) ^ swizzle_b<TN>(row)) * 16;
+    static_assert(8 * NW % (8 * TN) == 0, "swizzle_b");
+    const Source src_a(A, rows_a, lda, K), src_b(B, rows_b, ldb, K);
+    auto copy = [&]<bool WHOLE>(int kb, int stage) {
+        const int k0 = kb * BK;
+        const bool whole = WHOLE || k0 + BK <= K;
+        const int oa = whole || k0 + k_a < K ? row * lda + k_a : (int)0x80000000;
+        const int ob = whole || k0 + k_b < K ? row * ldb + k_b : (int)0x80000000;
+        int8_t *to = lds + stage * STAGE + wave * 1024;
 #pragma unroll
-    for (int u = 0; u < LA; ++u) {
-        const int r = (u * NW + wave) * 8 + lane / 8;
-        k_a[u] = ((lane & 7) ^ swizzle_a(r)) * 16;
-        off_a[u] = r < rows_a ? r * (int)p.lda + k_a[u] : (int)0x80000000;
-    }
+        for (int u = 0; u < LA; ++u) src_a.copy16(to + u * NW * 1024, oa + u * NW * 8 * lda, k0);
 #pragma unroll
-    for (int u = 0; u < LB; ++u) {
-        const int r = (u * NW + wave) * 8 + lane / 8;
-        k_b[u] = ((lane & 7) ^ swizzle_b<TN>(r)) * 16;
-        off_b[u] = r < rows_b ? r * (int)p.ldb + k_b[u] : (int)0x80000000;
-    }
-    const Source src_a(A, rows_a, p.lda, K), src_b(B, rows_b, p.ldb, K);
-    auto copy = [&](int k0, int8_t *stage) {
-        const bool whole = k0 + BK <= K;
-#pragma unroll
-        for (int u = 0; u < LA; ++u)
-            src_a.copy16(stage + (u * NW + wave) * 1024, whole || k0 + k_a[u] < K ? off_a[u] : (int)0x80000000, k0);
-#pragma unroll
-        for (int u = 0; u < LB; ++u)
-            src_b.copy16(stage + BM * BK + (u * NW + wave) * 1024, whole || k0 + k_b[u] < K ? off_b[u] : (int)0x80000000,
-                         k0);
+        for (int u = 0; u < LB; ++u) src_b.copy16(to + BM * BK + u * NW * 1024, ob + u * NW * 8 * ldb, k0);
     };
     i32x4 in_a[DMA ? 1 : LA], in_b[DMA ? 1 : LB];
-    auto load = [&](int k0) {
-        const bool whole = k0 + BK <= K;
-#pragma unroll
-        for (int u = 0; u < LA; ++u) {
-            in_a[u] = i32x4{0, 0, 0, 0};
-            if (off_a[u] >= 0 && (whole || k0 + k_a[u] < K)) {
-                const int8_t *row = A + (off_a[u] - k_a[u]);
-                in_a[u] = whole ? *reinterpret_cast<const i32x4_u *>(row + k0 + k_a[u])
-                                : own_bytes(chunk(row, k0 + k_a[u], K), k0 + k_a[u], K);
+    auto load = [&]<bool WHOLE>(int kb) {
+        const int k0 = kb * BK;
+        const bool whole = WHOLE || k0 + BK <= K;
+        auto from = [&](const int8_t *base, int r, int rows, int ld, int k, bool left) {
+            i32x4 v = {0, 0, 0, 0};
+            if (r < rows && (whole || k < K)) {
+                const int8_t *at = base + (int64_t)r * ld;
+                v = whole ? *reinterpret_cast<const i32x4_u *>(at + k) : chunk(at, k, K);
+                if (left && !whole) v = own_bytes(v, k, K);
             }
-        }
+            return v;
+        };
 #pragma unroll
-        for (int u = 0; u < LB; ++u) {
-            in_b[u] = i32x4{0, 0, 0, 0};
-            if (off_b[u] >= 0 && (whole || k0 + k_b[u] < K)) {
-                const int8_t *row = B + (off_b[u] - k_b[u]);
-                in_b[u] = whole ? *reinterpret_cast<const i32x4_u *>(row + k0 + k_b[u]) : chunk(row, k0 + k_b[u], K);
-            }
-        }
+        for (int u = 0; u < LA; ++u) in_a[u] = from(A, row + u * NW * 8, rows_a, lda, k0 + k_a, true);
+#pragma unroll
+        for (int u = 0; u < LB; ++u) in_b[u] = from(B, row + u * NW * 8, rows_b, ldb, k0 + k_b, false);
     };
-    auto put = [&](int8_t *stage) {
+    auto put = [&](int stage) {
+        int8_t *to = lds + stage * STAGE + wave * 1024 + lane * 16;
 #pragma unroll
-        for (int u = 0; u < LA; ++u)
-            *reinterpret_cast<i32x4 *>(stage + (u * NW + wave) * 1024 + lane * 16) = in_a[u];
+        for (int u = 0; u < LA; ++u) *reinterpret_cast<i32x4 *>(to + u * NW * 1024) = in_a[u];
 #pragma unroll
-        for (int u = 0; u < LB; ++u)
-            *reinterpret_cast<i32x4 *>(stage + BM * BK + (u * NW + wave) * 1024 + lane * 16) = in_b[u];
+        for (int u = 0; u < LB; ++u) *reinterpret_cast<i32x4 *>(to + BM * BK + u * NW * 1024) = in_b[u];
     };
-    auto barrier = [] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // this wave's reads of LDS are done, and its copies of all but the newest
+    // `later` blocks have landed: the barrier then says so of every wave's
+    auto barrier = [&](int later) {
+        if (STAGES > 3 && later >= 2)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STAGES > 3 ? 2 * L : 0) : "memory");
+        else if (STAGES > 2 && later >= 1)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STAGES > 2 ? L : 0) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-
-    i32x4 acc[TM][TN] = {};
-    auto multiply = [&](const int8_t *stage) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 a[TM], b[TN];
-#pragma unroll
-            for (int u = 0; u < TM; ++u) {
-                const int r = (wm * TM + u) * 16 + i;
-                a[u] = *reinterpret_cast<const i32x4 *>(stage + r * BK + ((h * 4 + g) ^ swizzle_a(r)) * 16);
+    // The bytes of A's rows past K that were copied with the last chunk are
+    // zeroed: what the same bytes of B hold then has no part.
+    auto cut = [&](int kb, int stage) {
+        if (DMA && K % 16 != 0 && kb == blocks - 1) {
+            for (int r = threadIdx.x; r < BM; r += NW * 64) {
+                const int k = K - kb * BK;
+                int8_t *c = lds + stage * STAGE + r * BK + (k / 16 ^ swizzle_a(r)) * 16;
+                for (int j = k % 16; j < 16; ++j) c[j] = 0;
             }
-#pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                const int r = wn * TN * 16 + b_row<TN>(t, i);
-                b[t] = *reinterpret_cast<const i32x4 *>(stage + BM * BK + r * BK + ((h * 4 + g) ^ swizzle_b<TN>(r)) * 16);
-            }
-#pragma unroll
-            for (int u = 0; u < TM; ++u)
-#pragma unroll
-                for (int t = 0; t < TN; ++t)
-                    acc[u][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[t], a[u], acc[u][t], 0, 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
         }
     };
 
-    const int blocks = (K + BK - 1) / BK;
+    struct Half {
+        i32x4 a[TM], b[TN];
+    };
+    const int at_a = (wm * TM * 16 + i) * BK, at_b = BM * BK + (wn * TN * 16 + b_row<TN>(0, i)) * BK;
+    const int c_a = swizzle_a(i), c_b = swizzle_b<TN>(b_row<TN>(0, i));
+    auto read = [&](Half &f, int stage, int h) {
+        const int8_t *pa = lds + stage * STAGE + at_a + ((h * 4 + g) ^ c_a) * 16;
+        const int8_t *pb = lds + stage * STAGE + at_b + ((h * 4 + g) ^ c_b) * 16;
+#pragma unroll
+        for (int t = 0; t < TN; ++t) f.b[t] = *reinterpret_cast<const i32x4 *>(pb + t * 4 * BK);
+#pragma unroll
+        for (int u = 0; u < TM; ++u) f.a[u] = *reinterpret_cast<const i32x4 *>(pa + u * 16 * BK);
+    };
+    i32x4 acc[TM][TN] = {};
+    auto multiply = [&](const Half &f) {
+#pragma unroll
+        for (int u = 0; u < TM; ++u)
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                acc[u][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[t], f.a[u], acc[u][t], 0, 0, 0);
+    };
+
+    float factor[(BM + 2 * BN + NW * 64 - 1) / (NW * 64)];
+#pragma unroll
+    for (int j = 0; j < (BM + 2 * BN + NW * 64 - 1) / (NW * 64); ++j) {
+        const int e = threadIdx.x + j * NW * 64;
+        const float *from = e < BM ? p.sa + min(m0 + e, p.M - 1) : e < BM + BN ? p.sb + min(n0 + e - BM, p.N - 1)
+                            : p.bias && e < BM + 2 * BN ? p.bias + min(n0 + e - BM - BN, p.N - 1) : nullptr;
+        factor[j] = from ? *from : 0.f;
+    }
+    auto keep_factors = [&] {
+#pragma unroll
+        for (int j = 0; j < (BM + 2 * BN + NW * 64 - 1) / (NW * 64); ++j)
+            if ((BM + 2 * BN) % (NW * 64) == 0 || threadIdx.x + j * NW * 64 < BM + 2 * BN)
+                factors[threadIdx.x + j * NW * 64] = factor[j];
+    };
+
+    Half f0, f1;
     if constexpr (DMA) {
-        copy(0, lds);
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            if (s < blocks) copy.template operator()<false>(s, s);
+        keep_factors();
+        barrier(blocks - 1 < STAGES - 1 ? blocks - 1 : STAGES - 1);
     } else {
-        load(0);
-        put(lds);
+        load.template operator()<false>(0);
+        put(0);
+        keep_factors();
+        barrier(0);
+        if (blocks > 1) load.template operator()<false>(1);
     }
-    for (int kb = 0; kb < blocks; ++kb) {
-        int8_t *now = lds + (kb & 1) * STAGE, *next = lds + (~kb & 1) * STAGE;
-        barrier();
-        if (DMA && kb + 1 == blocks && K % 16 != 0) {
-            // the bytes of A's rows past K, copied with the last chunk, are
-            // zeroed: what the same bytes of B hold then has no part
-            for (int r = threadIdx.x; r < BM; r += NW * 64) {
-                const int k = K - kb * BK;
-                int8_t *c = now + r * BK + (k / 16 ^ swizzle_a(r)) * 16;
-                for (int j = k % 16; j < 16; ++j) c[j] = 0;
+    cut(0, 0);
+    read(f0, 0, 0);
+    int now = 0;
+    // a half's reads of LDS go between the products of the half before
+    auto interleave = [] {
+#pragma unroll
+        for (int j = 0; j < TM + TN; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
+        }
+    };
+    // One block; MIDDLE: blocks up to kb + STAGES exist, and are whole.
+    auto step = [&]<bool MIDDLE>(int kb) {
+        const int next = now + 1 == STAGES ? 0 : now + 1;
+        read(f1, now, 1);
+        multiply(f0);
+        interleave();
+        if (MIDDLE || kb + 1 < blocks) {
+            if constexpr (!DMA) put(next);
+            // blocks kb + 2 .. kb + STAGES - 1 may still be on their way
+            const int later = blocks - kb - 2;
+            barrier(MIDDLE || later >= STAGES - 2 ? STAGES - 2 : later);
+            if (!MIDDLE) cut(kb + 1, next);
+            if constexpr (DMA) {
+                if (MIDDLE || kb + STAGES < blocks) copy.template operator()<MIDDLE>(kb + STAGES, now);
+            } else {
+                if (MIDDLE || kb + 2 < blocks) load.template operator()<MIDDLE>(kb + 2);
             }
-            barrier();
+            read(f0, next, 0);
         }
-        if (kb + 1 < blocks) {
-            if constexpr (DMA)
-                copy((kb + 1) * BK, next);
-            else
-                load((kb + 1) * BK);
-        }
-        multiply(now);
-        if (!DMA && kb + 1 < blocks) put(next);
-    }
+        multiply(f1);
+        interleave();
+        now = next;
+    };
+    int kb = 0;
+    for (; (kb + STAGES + 1) * BK <= K; ++kb) step.template operator()<true>(kb);
+    for (; kb < blocks; ++kb) step.template operator()<false>(kb);
 
     // lane: row u 16 + i of the wave's part, 4 TN columns from g 4 TN on
+    const int ml = wm * TM * 16 + i, nl = wn * TN * 16 + g * (4 * TN);
+    float sb[4 * TN], bias[4 * TN];
 #pragma unroll
-    for (int u = 0; u < TM; ++u)
+    for (int j = 0; j < 4 * TN; ++j) {
+        sb[j] = factors[BM + nl + j];
+        bias[j] = factors[BM + BN + nl + j];
+    }
 #pragma unroll
-        for (int t = 0; t < TN; ++t)
-            store4<T>(p, m0 + (wm * TM + u) * 16 + i, n0 + wn * TN * 16 + g * (4 * TN) + t * 4, acc[u][t]);
+    for (int u = 0; u < TM; ++u) {
+        const float sa = factors[ml + u * 16];
+        const int m = m0 + ml + u * 16, n = n0 + nl;
+        T *c = (T *)p.C + (int64_t)m * p.ldc + n;
+        if (m >= p.M) continue;
+        constexpr int E = 4 * TN < 16 / (int)sizeof(T) ? 4 * TN : 16 / (int)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 4 * TN; j += E) {
+            typename Pack<T, E>::V v;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                v[e] = (T)fmaf((float)acc[u][(j + e) / 4][(j + e) % 4], sa * sb[j + e], bias[j + e]);
+            if (n + j + E <= p.N) {
+                *reinterpret_cast<typename Pack<T, E>::U *>(c + j) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (n + j + e < p.N) c[j + e] = v[e];
+            }
+        }
+    }
 }
 
 // K == 0: the bias, or zeros.
@@ -303,15 +392,17 @@ __global__ void __launch_bounds__(256) gemm_i8_empty_kernel(Args p)
 
 // ---------------------------------------------------------------- launches
 
-template <typename T, int BM, int BN, int WM, int WN>
+constexpr int64_t kMostLd = 1 << 22;  // of gemm_i8_tile_kernel
+
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
 void launch_tile(const Args &a, bool dma, hipStream_t s)
 {
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
     const dim3 grid((unsigned)(tiles_m * tiles_n)), block(WM * WN * 64);
     if (dma)
-        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, true>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
+        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, STAGES, true>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
     else
-        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, false>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
+        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, 2, false>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
 }
 
 template <typename T>
@@ -325,12 +416,12 @@ int launch(const Args &a, hipStream_t s)
         return PK_OK;
     }
     const bool dma = ((uintptr_t)a.A | (uintptr_t)a.B | (uintptr_t)a.lda | (uintptr_t)a.ldb) % 4 == 0;
-    if (a.M > 64 && a.lda <= 1 << 22 && a.ldb <= 1 << 22) {
+    if (a.M > 64 && a.lda <= kMostLd && a.ldb <= kMostLd) {
         if ((int64_t)a.M * a.N >= 256 * 256 * 128) {
-            launch_tile<T, 256, 256, 2, 4>(a, dma, s);
+            launch_tile<T, 256, 256, 2, 4, 2>(a, dma, s);
             pk::api_ran(dma ? "gemm_i8_256x256" : "gemm_i8_256x256_unaligned");
         } else {
-            launch_tile<T, 128, 128, 2, 2>(a, dma, s);
+            launch_tile<T, 128, 128, 2, 2, 4>(a, dma, s);
             pk::api_ran(dma ? "gemm_i8_128x128" : "gemm_i8_128x128_unaligned");
         }
         return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
