@@ -323,7 +323,8 @@ typedef enum { PK_F32 = 0, PK_BF16 = 1, PK_F16 = 2 } pk_dtype;
 
 /*
  * Rows to 8 bits: for each row z of x, with a = max |z|,
- *   q = rint(z * (127 / a))  (ties to even, |q| <= 127),  scale = a / 127.
+ *   q = rint(z * (127 / a))  (ties to even, |q| <= 127),  scale = a / 127,
+ * in fp32, the factor as 127 * (1 / a).
  * A row with a < 127 * 2^-126 (a row of zeros) gets q = 0 and scale = 0; a row
  * that holds an infinity or a NaN gets q = 0 and that infinity or NaN as its
  * scale, so that it reads back, and multiplies, as NaN.

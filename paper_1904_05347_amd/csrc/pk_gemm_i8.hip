@@ -21,34 +21,16 @@ struct Args {
     int M, N, K;
 };
 
-// Four neighbouring elements of a row of C from n on.
-template <typename T>
-__device__ __forceinline__ void store4(const Args &p, int m, int n, const i32x4 &acc)
-{
-    if (m >= p.M || n >= p.N) return;
-    const float sa = p.sa[m];
-    T *c = (T *)p.C + (int64_t)m * p.ldc + n;
-    typename Pack<T, 4>::V v;
-    if (n + 4 <= p.N) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (T)((float)acc[r] * (sa * p.sb[n + r]) + (p.bias ? p.bias[n + r] : 0.f));
-        *reinterpret_cast<typename Pack<T, 4>::U *>(c) = v;
-        return;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (n + r < p.N) c[r] = (T)((float)acc[r] * (sa * p.sb[n + r]) + (p.bias ? p.bias[n + r] : 0.f));
-}
-
 // ------------------------------------------------------------ few rows of A
 //
-// A work-group makes 16 MT rows x 16 NT columns of C; its waves share K in
-// blocks of 128 and add their sums through LDS.  Operands go from memory to the
-// registers the matrix instruction reads: nothing is staged.
-// v_mfma_i32_16x16x64_i8 takes 16 bytes a lane from row lane % 16 of each
-// operand; which k they are does not matter as long as both operands agree, so
-// lane / 16 takes 32 neighbouring bytes of a block for two instructions, and a
-// row's 128 bytes are read whole.
+// A work-group makes 8 rows x 8 columns of C; its waves share K in blocks of
+// 128 and add their sums through LDS.  Operands go from memory to the registers
+// the matrix instruction reads: nothing is staged.
+// v_mfma_i32_16x16x64_i8 multiplies 16 rows of each operand, 64 bytes of each; a
+// load that follows it touches half of 16 memory lines, which runs at half the
+// rate of 8 whole ones.  So its 16 rows are the two halves of the 128 bytes of 8
+// rows, of either operand: of its 16 x 16 sums those count whose halves are the
+// same, and the two 8 x 8 parts are added at the end.
 
 // 16 bytes of a row from k on.  At the row's end the last 16 are read instead
 // (both operands do, so the k still agree); the first `drop` of them belong to
@@ -75,45 +57,57 @@ __device__ __forceinline__ i32x4 own_bytes(i32x4 v, int k, int K)
     return v;
 }
 
-template <typename T, int MT, int NT, int WAVES>
+template <typename T, int WAVES, int U>
 __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 {
-    __shared__ i32x4 part[WAVES][MT * NT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * (16 * NT), m0 = blockIdx.y * (16 * MT);
-    const int8_t *pa[MT], *pb[NT];  // rows beyond the last are the last: their sums are not stored
+    __shared__ i32x4 part[WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4, K = p.K;
+    const int n0 = blockIdx.x * 8, m0 = blockIdx.y * 8;
+    // rows beyond the last are the last: their sums are not stored
+    const int8_t *pa = p.A + (int64_t)min(m0 + i % 8, p.M - 1) * p.lda, *pb = p.B + (int64_t)min(n0 + i % 8, p.N - 1) * p.ldb;
+    // the scales of this lane's row and columns, before they are needed
+    const int m = min(m0 + i % 8, p.M - 1), n = n0 + g % 2 * 4;
+    const float sa = p.sa[m];
+    float sb[4], bias[4];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) pa[t] = p.A + (int64_t)min(m0 + t * 16 + i, p.M - 1) * p.lda;
+    for (int r = 0; r < 4; ++r) {
+        sb[r] = p.sb[min(n + r, p.N - 1)];
+        bias[r] = p.bias ? p.bias[min(n + r, p.N - 1)] : 0.f;
+    }
+    i32x4 acc = {0, 0, 0, 0};
+    auto blocks = [&]<int V, bool WHOLE>(int k0) {
+        i32x4 a[V], b[V];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) pb[t] = p.B + (int64_t)min(n0 + t * 16 + i, p.N - 1) * p.ldb;
-    i32x4 acc[MT][NT] = {};
-    for (int k0 = wave * 128; k0 < p.K; k0 += WAVES * 128) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = k0 + g * 32 + h * 16;
-            i32x4 a[MT], b[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) b[t] = chunk(pb[t], k, p.K);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) a[t] = own_bytes(chunk(pa[t], k, p.K), k, p.K);
-#pragma unroll
-            for (int u = 0; u < MT; ++u)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    acc[u][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[t], a[u], acc[u][t], 0, 0, 0);
+        for (int v = 0; v < V; ++v) {
+            const int k = k0 + v * (WAVES * 128) + (i / 8 * 4 + g) * 16;
+            b[v] = WHOLE ? *reinterpret_cast<const i32x4_u *>(pb + k) : chunk(pb, k, K);
+            a[v] = WHOLE ? *reinterpret_cast<const i32x4_u *>(pa + k) : own_bytes(chunk(pa, k, K), k, K);
         }
-    }
 #pragma unroll
-    for (int u = 0; u < MT; ++u)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) part[wave][u * NT + t][lane] = acc[u][t];
+        for (int v = 0; v < V; ++v) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[v], a[v], acc, 0, 0, 0);
+    };
+    int k0 = wave * 128;
+    for (; k0 + (U - 1) * (WAVES * 128) + 128 <= K; k0 += U * WAVES * 128) blocks.template operator()<U, true>(k0);
+    for (; k0 + 128 <= K; k0 += WAVES * 128) blocks.template operator()<1, true>(k0);
+    if (k0 < K) blocks.template operator()<1, false>(k0);
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int q = wave; q < MT * NT; q += WAVES) {
-        i32x4 s = part[0][q][lane];
+    // lane: row i % 8, columns g 4 to g 4 + 3 of the first half's sums (g < 2, i < 8)
+    if (wave > 0 || g >= 2 || i >= 8 || m0 + i >= p.M || n >= p.N) return;
+    i32x4 s = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += part[w][q][lane];
-        store4<T>(p, m0 + q / NT * 16 + i, n0 + q % NT * 16 + g * 4, s);
+    for (int w = 0; w < WAVES; ++w) s += part[w][lane] + part[w][lane + 2 * 16 + 8];
+    typename Pack<T, 4>::V v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (T)fmaf((float)s[r], sa * sb[r], bias[r]);
+    T *c = (T *)p.C + (int64_t)m * p.ldc + n;
+    if (n + 4 <= p.N) {
+        *reinterpret_cast<typename Pack<T, 4>::U *>(c) = v;
+        return;
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (n + r < p.N) c[r] = v[r];
 }
 
 // ------------------------------------------------------------- many rows of A
@@ -165,29 +159,36 @@ struct Source {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                      :
                      : "s"(at), "v"(off), "s"(rs), "s"(k)
-                     : "memory", "m0");
+                     : "memory");
     }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int STAGES, bool DMA>
-__global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, int tiles_m, int tiles_n, int group_m)
+template <typename T, int BM, int BN, int WM, int WN, int KG, int STAGES, bool DMA>
+__global__ void __launch_bounds__(KG * WM * WN * 64, 2)
+    gemm_i8_tile_kernel(Args p, int tiles_m, int tiles_n, int group_m)
 {
     constexpr int BK = 128, NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, STAGE = (BM + BN) * BK;
     constexpr int LA = BM / (8 * NW), LB = BN / (8 * NW), L = LA + LB;  // copies of 16 bytes a lane and block
+    constexpr int THREADS = KG * NW * 64;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM * WM * 16 == BM && TN * WN * 16 == BN, "whole copies");
     static_assert(DMA ? (STAGES - 2) * L < 64 : STAGES == 2, "copies in flight are counted in six bits");
     static_assert(BM <= 256 && BN <= 256, "offsets in a tile are 32-bit for leading dimensions up to kMostLd");
-    __shared__ __attribute__((aligned(16))) int8_t lds[STAGES * STAGE];
+    static_assert((KG - 1) * BM * BN * 4 <= KG * STAGES * STAGE, "sums of the other groups fit the stages");
+    __shared__ __attribute__((aligned(16))) int8_t lds_all[KG * STAGES * STAGE];
     __shared__ __attribute__((aligned(16))) float factors[BM + 2 * BN];  // the scales of the tile's rows and columns, the bias
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15,
-              g = lane >> 4;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave_all / NW, wave = wave_all % NW;
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn;
     pk::tile_of_ints(tiles_m, tiles_n, group_m, pk::xcd_tile(blockIdx.x, tiles_m * tiles_n, 8), tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, K = p.K, blocks = (K + BK - 1) / BK;
+    const int m0 = tm * BM, n0 = tn * BN, K = p.K;
     const int lda = (int)p.lda, ldb = (int)p.ldb;
     const int8_t *A = p.A + (int64_t)m0 * p.lda, *B = p.B + (int64_t)n0 * p.ldb;
     const int rows_a = p.M - m0, rows_b = p.N - n0;
+    // this group's blocks: `count` from `first` on, at most `per`, the number of steps of every group
+    const int blocks = (K + BK - 1) / BK, per = (blocks + KG - 1) / KG, first = group * per;
+    const int count = KG == 1 ? blocks : max(0, min(per, blocks - first));
+    int8_t *const lds = lds_all + group * (STAGES * STAGE);
 
     // copy u of this lane: row (u NW + wave) 8 + lane / 8 of the tile, chunk position lane % 8;
     // the swizzles do not depend on u
@@ -195,8 +196,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, i
     const int k_a = ((lane & 7) ^ swizzle_a(row)) * 16, k_b = ((lane & 7) ^ swizzle_b<TN>(row)) * 16;
     static_assert(8 * NW % (8 * TN) == 0, "swizzle_b");
     const Source src_a(A, rows_a, lda, K), src_b(B, rows_b, ldb, K);
-    auto copy = [&]<bool WHOLE>(int kb, int stage) {
-        const int k0 = kb * BK;
+    auto copy = [&]<bool WHOLE>(int j, int stage) {
+        const int k0 = (first + j) * BK;
         const bool whole = WHOLE || k0 + BK <= K;
         const int oa = whole || k0 + k_a < K ? row * lda + k_a : (int)0x80000000;
         const int ob = whole || k0 + k_b < K ? row * ldb + k_b : (int)0x80000000;
@@ -206,23 +207,34 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, i
 #pragma unroll
         for (int u = 0; u < LB; ++u) src_b.copy16(to + BM * BK + u * NW * 1024, ob + u * NW * 8 * ldb, k0);
     };
+    // The bytes of A's rows past K that were copied with the last chunk are
+    // zeroed: what the same bytes of B hold then has no part.
+    auto cut = [&](int j, int stage) {
+        const int left = K - (first + j) * BK - k_a;  // of this lane's chunks
+        if (left > 0 && left < 16) {
+            int8_t *c = lds + stage * STAGE + wave * 1024 + lane * 16;
+#pragma unroll
+            for (int u = 0; u < LA; ++u)
+                for (int e = left; e < 16; ++e) c[u * NW * 1024 + e] = 0;
+        }
+    };
     i32x4 in_a[DMA ? 1 : LA], in_b[DMA ? 1 : LB];
-    auto load = [&]<bool WHOLE>(int kb) {
-        const int k0 = kb * BK;
+    auto load = [&]<bool WHOLE>(int j) {
+        const int k0 = (first + j) * BK;
         const bool whole = WHOLE || k0 + BK <= K;
-        auto from = [&](const int8_t *base, int r, int rows, int ld, int k, bool left) {
-            i32x4 v = {0, 0, 0, 0};
-            if (r < rows && (whole || k < K)) {
-                const int8_t *at = base + (int64_t)r * ld;
-                v = whole ? *reinterpret_cast<const i32x4_u *>(at + k) : chunk(at, k, K);
-                if (left && !whole) v = own_bytes(v, k, K);
+        auto from = [&](i32x4 &in, const int8_t *base, int r, int rows, int ld, int k, bool left) {
+            const int8_t *at = base + (int64_t)min(r, rows - 1) * ld;  // rows beyond the last: their sums are not stored
+            if (whole) {
+                in = *reinterpret_cast<const i32x4_u *>(at + k);
+            } else {
+                in = k < K ? chunk(at, k, K) : i32x4{0, 0, 0, 0};
+                if (left) in = own_bytes(in, k, K);
             }
-            return v;
         };
 #pragma unroll
-        for (int u = 0; u < LA; ++u) in_a[u] = from(A, row + u * NW * 8, rows_a, lda, k0 + k_a, true);
+        for (int u = 0; u < LA; ++u) from(in_a[u], A, row + u * NW * 8, rows_a, lda, k0 + k_a, true);
 #pragma unroll
-        for (int u = 0; u < LB; ++u) in_b[u] = from(B, row + u * NW * 8, rows_b, ldb, k0 + k_b, false);
+        for (int u = 0; u < LB; ++u) from(in_b[u], B, row + u * NW * 8, rows_b, ldb, k0 + k_b, false);
     };
     auto put = [&](int stage) {
         int8_t *to = lds + stage * STAGE + wave * 1024 + lane * 16;
@@ -231,31 +243,22 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, i
 #pragma unroll
         for (int u = 0; u < LB; ++u) *reinterpret_cast<i32x4 *>(to + BM * BK + u * NW * 1024) = in_b[u];
     };
-    // this wave's reads of LDS are done, and its copies of all but the newest
-    // `later` blocks have landed: the barrier then says so of every wave's
-    auto barrier = [&](int later) {
-        if (STAGES > 3 && later >= 2)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STAGES > 3 ? 2 * L : 0) : "memory");
+    // this wave's copies of all but the newest `later` blocks have landed
+    auto landed = [&](int later) {
+        if (STAGES > 5 && later >= 4)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 5 ? 4 * L : 0) : "memory");
+        else if (STAGES > 3 && later >= 2)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 3 ? 2 * L : 0) : "memory");
         else if (STAGES > 2 && later >= 1)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STAGES > 2 ? L : 0) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 2 ? L : 0) : "memory");
         else
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    // this wave's accesses of LDS are done: the barrier then says so of every wave's
+    auto barrier = [] {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-    };
-    // The bytes of A's rows past K that were copied with the last chunk are
-    // zeroed: what the same bytes of B hold then has no part.
-    auto cut = [&](int kb, int stage) {
-        if (DMA && K % 16 != 0 && kb == blocks - 1) {
-            for (int r = threadIdx.x; r < BM; r += NW * 64) {
-                const int k = K - kb * BK;
-                int8_t *c = lds + stage * STAGE + r * BK + (k / 16 ^ swizzle_a(r)) * 16;
-                for (int j = k % 16; j < 16; ++j) c[j] = 0;
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
     };
 
     struct Half {
@@ -279,73 +282,100 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_i8_tile_kernel(Args p, i
             for (int t = 0; t < TN; ++t)
                 acc[u][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[t], f.a[u], acc[u][t], 0, 0, 0);
     };
-
-    float factor[(BM + 2 * BN + NW * 64 - 1) / (NW * 64)];
-#pragma unroll
-    for (int j = 0; j < (BM + 2 * BN + NW * 64 - 1) / (NW * 64); ++j) {
-        const int e = threadIdx.x + j * NW * 64;
-        const float *from = e < BM ? p.sa + min(m0 + e, p.M - 1) : e < BM + BN ? p.sb + min(n0 + e - BM, p.N - 1)
-                            : p.bias && e < BM + 2 * BN ? p.bias + min(n0 + e - BM - BN, p.N - 1) : nullptr;
-        factor[j] = from ? *from : 0.f;
-    }
-    auto keep_factors = [&] {
-#pragma unroll
-        for (int j = 0; j < (BM + 2 * BN + NW * 64 - 1) / (NW * 64); ++j)
-            if ((BM + 2 * BN) % (NW * 64) == 0 || threadIdx.x + j * NW * 64 < BM + 2 * BN)
-                factors[threadIdx.x + j * NW * 64] = factor[j];
-    };
-
-    Half f0, f1;
-    if constexpr (DMA) {
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s)
-            if (s < blocks) copy.template operator()<false>(s, s);
-        keep_factors();
-        barrier(blocks - 1 < STAGES - 1 ? blocks - 1 : STAGES - 1);
-    } else {
-        load.template operator()<false>(0);
-        put(0);
-        keep_factors();
-        barrier(0);
-        if (blocks > 1) load.template operator()<false>(1);
-    }
-    cut(0, 0);
-    read(f0, 0, 0);
-    int now = 0;
     // a half's reads of LDS go between the products of the half before
     auto interleave = [] {
 #pragma unroll
         for (int j = 0; j < TM + TN; ++j) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, TM * TN > TM + TN ? TM * TN / (TM + TN) : 1, 0);
         }
     };
-    // One block; MIDDLE: blocks up to kb + STAGES exist, and are whole.
-    auto step = [&]<bool MIDDLE>(int kb) {
+
+    constexpr int FACTORS = (BM + 2 * BN + THREADS - 1) / THREADS;
+    float factor[FACTORS];
+#pragma unroll
+    for (int j = 0; j < FACTORS; ++j) {
+        const int e = threadIdx.x + j * THREADS;
+        const float *from = e < BM ? p.sa + min(m0 + e, p.M - 1) : e < BM + BN ? p.sb + min(n0 + e - BM, p.N - 1)
+                            : p.bias && e < BM + 2 * BN ? p.bias + min(n0 + e - BM - BN, p.N - 1) : nullptr;
+        factor[j] = from ? *from : 0.f;
+    }
+
+    Half f0, f1;
+    if constexpr (DMA) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            if (s < count) copy.template operator()<false>(s, s);
+    } else if (count > 0) {
+        load.template operator()<false>(0);
+        put(0);
+    }
+#pragma unroll
+    for (int j = 0; j < FACTORS; ++j)
+        if ((BM + 2 * BN) % THREADS == 0 || threadIdx.x + j * THREADS < BM + 2 * BN)
+            factors[threadIdx.x + j * THREADS] = factor[j];
+    if constexpr (DMA) {
+        landed(count - 1 < STAGES - 1 ? count - 1 : STAGES - 1);
+        cut(0, 0);
+    }
+    barrier();
+    if (!DMA && count > 1) load.template operator()<false>(1);
+    if (count > 0) read(f0, 0, 0);
+    int now = 0;
+    // One block; MIDDLE: the group's blocks up to j + STAGES exist, and are whole.
+    auto step = [&]<bool MIDDLE>(int j) {
         const int next = now + 1 == STAGES ? 0 : now + 1;
-        read(f1, now, 1);
-        multiply(f0);
-        interleave();
-        if (MIDDLE || kb + 1 < blocks) {
-            if constexpr (!DMA) put(next);
-            // blocks kb + 2 .. kb + STAGES - 1 may still be on their way
-            const int later = blocks - kb - 2;
-            barrier(MIDDLE || later >= STAGES - 2 ? STAGES - 2 : later);
-            if (!MIDDLE) cut(kb + 1, next);
-            if constexpr (DMA) {
-                if (MIDDLE || kb + STAGES < blocks) copy.template operator()<MIDDLE>(kb + STAGES, now);
-            } else {
-                if (MIDDLE || kb + 2 < blocks) load.template operator()<MIDDLE>(kb + 2);
-            }
-            read(f0, next, 0);
+        if (MIDDLE || j < count) {
+            read(f1, now, 1);
+            multiply(f0);
+            interleave();
         }
-        multiply(f1);
-        interleave();
+        if (MIDDLE || j + 1 < per) {
+            if constexpr (DMA) {
+                // blocks j + 2 .. j + STAGES - 1 may still be on their way
+                const int later = count - j - 2;
+                landed(MIDDLE || later >= STAGES - 2 ? STAGES - 2 : later);
+                if (!MIDDLE) cut(j + 1, next);
+            } else {
+                if (MIDDLE || j + 1 < count) put(next);
+            }
+            barrier();
+            if constexpr (DMA) {
+                if (MIDDLE || j + STAGES < count) copy.template operator()<MIDDLE>(j + STAGES, now);
+            } else {
+                if (MIDDLE || j + 2 < count) load.template operator()<MIDDLE>(j + 2);
+            }
+            if (MIDDLE || j + 1 < count) read(f0, next, 0);
+        }
+        if (MIDDLE || j < count) {
+            multiply(f1);
+            interleave();
+        }
         now = next;
     };
-    int kb = 0;
-    for (; (kb + STAGES + 1) * BK <= K; ++kb) step.template operator()<true>(kb);
-    for (; kb < blocks; ++kb) step.template operator()<false>(kb);
+    int j = 0;
+    for (const int whole = min(count, K / BK - first) - STAGES; j < whole; ++j) step.template operator()<true>(j);
+    for (; j < per; ++j) step.template operator()<false>(j);
+
+    if constexpr (KG > 1) {
+        // the groups' sums are added in the first one's registers
+        i32x4 *const sums = (i32x4 *)lds_all;
+        barrier();
+        if (group > 0) {
+#pragma unroll
+            for (int u = 0; u < TM; ++u)
+#pragma unroll
+                for (int t = 0; t < TN; ++t) sums[(((group - 1) * NW + wave) * (TM * TN) + u * TN + t) * 64 + lane] = acc[u][t];
+        }
+        barrier();
+        if (group > 0) return;
+#pragma unroll
+        for (int o = 0; o < KG - 1; ++o)
+#pragma unroll
+            for (int u = 0; u < TM; ++u)
+#pragma unroll
+                for (int t = 0; t < TN; ++t) acc[u][t] += sums[((o * NW + wave) * (TM * TN) + u * TN + t) * 64 + lane];
+    }
 
     // lane: row u 16 + i of the wave's part, 4 TN columns from g 4 TN on
     const int ml = wm * TM * 16 + i, nl = wn * TN * 16 + g * (4 * TN);
@@ -393,16 +423,115 @@ __global__ void __launch_bounds__(256) gemm_i8_empty_kernel(Args p)
 // ---------------------------------------------------------------- launches
 
 constexpr int64_t kMostLd = 1 << 22;  // of gemm_i8_tile_kernel
+constexpr int kMostSide = 1 << 17;    // rows and columns of C of one launch
 
-template <typename T, int BM, int BN, int WM, int WN, int STAGES>
-void launch_tile(const Args &a, bool dma, hipStream_t s)
+template <typename T, int BM, int BN, int WM, int WN, int KG, int STAGES, bool DMA>
+void launch_tile(const Args &a, hipStream_t s)
 {
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
-    const dim3 grid((unsigned)(tiles_m * tiles_n)), block(WM * WN * 64);
-    if (dma)
-        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, STAGES, true>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
-    else
-        hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, 2, false>), grid, block, 0, s, a, tiles_m, tiles_n, 4);
+    // tiles of four tile rows run together: an XCD's 32 CUs then share the rows of A and B that they read
+    hipLaunchKernelGGL((gemm_i8_tile_kernel<T, BM, BN, WM, WN, KG, STAGES, DMA>), dim3((unsigned)(tiles_m * tiles_n)),
+                       dim3(KG * WM * WN * 64), 0, s, a, tiles_m, tiles_n, 4);
+}
+
+template <typename T>
+void launch_rows(const Args &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((gemm_i8_rows_kernel<T, 8, 4>), dim3((unsigned)((a.N + 7) / 8), (unsigned)((a.M + 7) / 8)),
+                       dim3(512), 0, s, a);
+}
+
+// ---------------------------------------------------------------- choice
+//
+// The configuration of the least predicted time.  A configuration's time in us is
+//   base + round * ceil(x / resident) + steps * max(least * ceil(x / resident), block * x),
+// x = the tiles of the fullest CU, resident = its work-groups at once, steps = the
+// 128-byte blocks of K that a group of waves goes through one after the other: a
+// block takes `least` where the CU waits for memory, `block` where its
+// work-groups share it.  The figures are fitted to timed calls of each
+// configuration over M 1 to 8192, N and K 64 to 16384 (the logarithms' least
+// squares, those counting most that a choice could take).
+struct Config {
+    const char *name;
+    int bm, bn, kg, resident;
+    float base, round, least, block;
+};
+
+// rows that start at multiples of four bytes: copied straight into LDS
+const Config kAligned[] = {
+    {"gemm_i8_256x256", 256, 256, 1, 1, 0.00f, 5.94f, 1.449f, 0.050f},
+    {"gemm_i8_128x256", 128, 256, 1, 1, 0.00f, 5.45f, 0.752f, 0.677f},
+    {"gemm_i8_128x128", 128, 128, 1, 1, 0.00f, 4.47f, 0.467f, 0.050f},
+    {"gemm_i8_64x128", 64, 128, 1, 2, 0.38f, 3.58f, 0.255f, 0.299f},
+    {"gemm_i8_64x64_k2", 64, 64, 2, 1, 1.28f, 2.72f, 0.382f, 0.050f},
+    {"gemm_i8_32x64_k2", 32, 64, 2, 2, 1.76f, 2.06f, 0.268f, 0.291f},
+    {"gemm_i8_32x32_k2", 32, 32, 2, 2, 1.95f, 1.94f, 0.207f, 0.199f},
+    {"gemm_i8_16x16_k4", 16, 16, 4, 2, 2.08f, 1.40f, 0.229f, 0.196f},
+    {"gemm_i8_rows", 8, 8, 8, 4, 2.56f, 0.00f, 0.368f, 0.300f},
+};
+// any other alignment: through registers
+const Config kUnaligned[] = {
+    {"gemm_i8_128x256_any", 128, 256, 1, 1, 0.00f, 5.11f, 1.526f, 0.050f},
+    {"gemm_i8_128x128_any", 128, 128, 1, 2, 0.44f, 3.68f, 0.100f, 1.001f},
+    {"gemm_i8_64x64_any", 64, 64, 1, 4, 0.42f, 2.86f, 0.593f, 0.395f},
+    {"gemm_i8_64x64_k2_any", 64, 64, 2, 2, 2.40f, 1.40f, 0.100f, 0.907f},
+    {"gemm_i8_32x32_k4_any", 32, 32, 4, 2, 2.05f, 1.43f, 0.340f, 0.870f},
+    {"gemm_i8_16x16_k8_any", 16, 16, 8, 2, 2.43f, 0.75f, 0.347f, 0.853f},
+    {"gemm_i8_rows", 8, 8, 8, 4, 2.45f, 0.00f, 0.189f, 0.700f},
+};
+
+template <typename T>
+void launch_config(const Config *c, const Args &a, hipStream_t s)
+{
+    if (c >= kUnaligned && c < kUnaligned + 7) {
+        switch (c - kUnaligned) {
+        case 0: return launch_tile<T, 128, 256, 2, 4, 1, 2, false>(a, s);
+        case 1: return launch_tile<T, 128, 128, 2, 4, 1, 2, false>(a, s);
+        case 2: return launch_tile<T, 64, 64, 2, 4, 1, 2, false>(a, s);
+        case 3: return launch_tile<T, 64, 64, 2, 2, 2, 2, false>(a, s);
+        case 4: return launch_tile<T, 32, 32, 2, 2, 4, 2, false>(a, s);
+        case 5: return launch_tile<T, 16, 16, 1, 1, 8, 2, false>(a, s);
+        default: return launch_rows<T>(a, s);
+        }
+    }
+    switch (c - kAligned) {
+    case 0: return launch_tile<T, 256, 256, 2, 4, 1, 2, true>(a, s);
+    case 1: return launch_tile<T, 128, 256, 2, 4, 1, 3, true>(a, s);
+    case 2: return launch_tile<T, 128, 128, 2, 4, 1, 4, true>(a, s);
+    case 3: return launch_tile<T, 64, 128, 2, 4, 1, 3, true>(a, s);
+    case 4: return launch_tile<T, 64, 64, 2, 2, 2, 3, true>(a, s);
+    case 5: return launch_tile<T, 32, 64, 1, 4, 2, 3, true>(a, s);
+    case 6: return launch_tile<T, 32, 32, 2, 2, 2, 4, true>(a, s);
+    case 7: return launch_tile<T, 16, 16, 1, 1, 4, 4, true>(a, s);
+    default: return launch_rows<T>(a, s);
+    }
+}
+
+float predicted_us(const Config &c, const Args &a)
+{
+    constexpr int kCUs = 256;
+    const int64_t tiles = (int64_t)((a.M + c.bm - 1) / c.bm) * ((a.N + c.bn - 1) / c.bn);
+    const int64_t x = (tiles + kCUs - 1) / kCUs, rounds = (x + c.resident - 1) / c.resident;
+    const int steps = ((a.K + 127) / 128 + c.kg - 1) / c.kg;
+    const float least = c.least * (float)rounds, block = c.block * (float)x;
+    return c.base + c.round * (float)rounds + (float)steps * (least > block ? least : block);
+}
+
+const Config *choose(const Args &a)
+{
+    const bool dma = ((uintptr_t)a.A | (uintptr_t)a.B | (uintptr_t)a.lda | (uintptr_t)a.ldb) % 4 == 0;
+    const Config *from = dma ? kAligned : kUnaligned, *rows = dma ? kAligned + 8 : kUnaligned + 6;
+    if (a.lda > kMostLd || a.ldb > kMostLd) return rows;
+    const Config *best = nullptr;
+    float least = 0.f;
+    for (const Config *c = from; c <= rows; ++c) {
+        if (c == rows && a.M > c->bm) break;  // it would read B again for every eight rows
+        const float t = predicted_us(*c, a);
+        if (best && t >= least) continue;
+        best = c;
+        least = t;
+    }
+    return best;
 }
 
 template <typename T>
@@ -415,21 +544,24 @@ int launch(const Args &a, hipStream_t s)
         pk::api_ran("gemm_i8_empty");
         return PK_OK;
     }
-    const bool dma = ((uintptr_t)a.A | (uintptr_t)a.B | (uintptr_t)a.lda | (uintptr_t)a.ldb) % 4 == 0;
-    if (a.M > 64 && a.lda <= kMostLd && a.ldb <= kMostLd) {
-        if ((int64_t)a.M * a.N >= 256 * 256 * 128) {
-            launch_tile<T, 256, 256, 2, 4, 2>(a, dma, s);
-            pk::api_ran(dma ? "gemm_i8_256x256" : "gemm_i8_256x256_unaligned");
-        } else {
-            launch_tile<T, 128, 128, 2, 2, 4>(a, dma, s);
-            pk::api_ran(dma ? "gemm_i8_128x128" : "gemm_i8_128x128_unaligned");
+    // a launch's grid holds the tiles of at most kMostSide rows and columns
+    const Config *c = nullptr;
+    for (int m = 0; m < a.M; m += kMostSide)
+        for (int n = 0; n < a.N; n += kMostSide) {
+            Args part = a;
+            part.M = a.M - m < kMostSide ? a.M - m : kMostSide;
+            part.N = a.N - n < kMostSide ? a.N - n : kMostSide;
+            part.A += m * a.lda;
+            part.B += n * a.ldb;
+            part.sa += m;
+            part.sb += n;
+            if (a.bias) part.bias += n;
+            part.C = (T *)a.C + m * a.ldc + n;
+            c = choose(part);
+            launch_config<T>(c, part, s);
+            if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
         }
-        return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
-    }
-    hipLaunchKernelGGL((gemm_i8_rows_kernel<T, 1, 1, 8>), dim3((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 15) / 16)),
-                       dim3(512), 0, s, a);
-    if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
-    pk::api_ran("gemm_i8_16x16");
+    pk::api_ran(c->name);
     return PK_OK;
 }
 

@@ -1,7 +1,7 @@
 // pk_rows_i8.hip -- rows of a matrix to 8-bit integers with one scale a row,
 // alone or as the end of the operator that makes the row, and back.
 //
-// Row z becomes q = rint(z * (127 / a)) and scale = a / 127 with a = max |z|.
+// Row z becomes q = rint(z * (127 * (1 / a))) and scale = a / 127 with a = max |z|.
 // What z is:
 //   PLAIN   the input;
 //   NORM    h * w, h = x (+ residual, rounded to its type: what is stored), and
@@ -15,7 +15,7 @@
 #include "pk_i8.hpp"
 #include "pk_i8_checks.hpp"
 
-#pragma clang fp contract(off)  // z * (127 / a) is rounded before it is rounded to an integer
+#pragma clang fp contract(off)  // z times that factor is rounded before it is rounded to an integer
 
 namespace {
 
@@ -36,12 +36,28 @@ struct RowArgs {
     float eps;
 };
 
-// g * sigmoid(2 u) with u = g / 2 (silu) or the tanh form of gelu's
-// sqrt(2 / pi) (g + 0.044715 g^3): 1 / 2 (1 + tanh u) is sigmoid(2 u).
+// g / (1 + exp(-t)) with t = g (silu) or twice the argument of gelu's tanh,
+// 2 sqrt(2 / pi) (g + 0.044715 g^3): 1 / 2 (1 + tanh u) is 1 / (1 + exp(-2 u)).
+// The exponential and the reciprocal are the hardware's, within a unit in the
+// last place each; log2(e) is in the constants.
 __device__ __forceinline__ float activate(float g, int act)
 {
-    const float t = act == PK_ACT_SILU ? g : 1.5957691216057308f * (g + 0.044715f * g * g * g);
-    return g / (1.f + expf(-t));
+    constexpr float log2e = 1.4426950408889634f, c = 1.5957691216057308f * 1.4426950408889634f;
+    const float t = act == PK_ACT_SILU ? -log2e * g : g * fmaf(-0.044715f * c, g * g, -c);
+    return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t));
+}
+
+// v of every lane combined by op, in every lane; `none` leaves v as it is.
+template <typename Op>
+__device__ __forceinline__ int across_wave(int v, int none, Op op)
+{
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0xb1, 0xf, 0xf, false));   // lane ^ 1
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0x4e, 0xf, 0xf, false));   // lane ^ 2
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0x141, 0xf, 0xf, false));  // mirrored in 8
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0x140, 0xf, 0xf, false));  // mirrored in 16
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0x142, 0xa, 0xf, false));  // lane 15 and 47 to the next 16
+    v = op(v, __builtin_amdgcn_update_dpp(none, v, 0x143, 0xc, 0xf, false));  // lane 31 to the upper half
+    return __builtin_amdgcn_readlane(v, 63);
 }
 
 // What one work-item reads of E neighbouring elements.
@@ -62,6 +78,9 @@ struct Chunk {
             if (MODE == NORM) w = *reinterpret_cast<const UW *>(pw + e);
             return;
         }
+        x = y = (typename Pack<T>::V)(T)0.f;
+        w = (typename Pack<W, E>::V)(W)0.f;
+        if (e >= N) return;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const bool in = e + j < N;
@@ -159,11 +178,11 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rows_i8_kernel(RowArgs 
         reduce(k, v);
     }
 
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        if (MODE == NORM) ss += __shfl_xor(ss, d);
-        am = max(am, (unsigned)__shfl_xor((int)am, d));
-    }
+    if (MODE == NORM)
+        ss = __int_as_float(across_wave(__float_as_int(ss), 0, [](int a, int b) {
+            return __float_as_int(__int_as_float(a) + __int_as_float(b));
+        }));
+    am = (unsigned)across_wave((int)am, 0, [](int a, int b) { return (int)max((unsigned)a, (unsigned)b); });
     if constexpr (TPR > 64) {
         __shared__ float s_ss[WAVES];
         __shared__ unsigned s_am[WAVES];
@@ -186,7 +205,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rows_i8_kernel(RowArgs 
     // reads back as NaN.
     const float a = __uint_as_float(am);
     const bool live = a >= 127.f * 0x1p-126f && a < __builtin_inff();
-    const float inv = live ? 127.f / a : 0.f;
+    const float inv = live ? 127.f * (1.f / a) : 0.f;
     if (t == 0) {
         float s = a;
         if (live && MODE == NORM) s = a * (1.f / sqrtf(ss / (float)N + p.eps));
@@ -238,22 +257,34 @@ constexpr int64_t kMostRows = 1 << 22;  // of one launch: a grid holds fewer tha
 template <typename T, typename W, int MODE>
 int launch_rows(const RowArgs &a, hipStream_t s)
 {
-    // the fewest registers that hold a row; short rows get one wave each
     constexpr int E = 16 / (int)sizeof(T);
     const int chunks = (a.N + E - 1) / E;
 #define PK_ROWS(TPR, VPT)                                                                                           \
     hipLaunchKernelGGL((rows_i8_kernel<T, W, MODE, TPR, VPT>), dim3((unsigned)(TPR < 256 ? (a.M + 3) / 4 : a.M)),     \
                        dim3(TPR < 256 ? 256 : TPR), 0, s, a)
+    // The fewest registers that hold a row.  Many rows: the fewest work-items that
+    // do, a wave for a short row (bf16 norm, 16384 x 2048: one wave 39.5 us, four
+    // 41.7; 8192 x 4096: four waves 39.0, eight 40.9), until the values of a row
+    // leave too few of them on a CU (8192 x 8192 gated: eight waves 64.1, four
+    // 67.2; fp32 rows of it: sixteen waves 57.6, four 66.0).  Few rows: more
+    // work-items, for the latency (1024 x 4096: eight waves 8.5 us, four 8.9).
+    const bool few = a.M <= 1024;
     if (chunks <= 64)
         PK_ROWS(64, 1);
     else if (chunks <= 128)
         PK_ROWS(64, 2);
-    else if (chunks <= 256)
+    else if (chunks <= 256 && few)
         PK_ROWS(256, 1);
+    else if (chunks <= 256)
+        PK_ROWS(64, 4);
+    else if (chunks <= 512 && few)
+        PK_ROWS(512, 1);
     else if (chunks <= 512)
         PK_ROWS(256, 2);
     else if (chunks <= 1024)
-        PK_ROWS(256, 4);
+        PK_ROWS(512, 2);
+    else if (chunks <= 2048)
+        PK_ROWS(1024, 2);
     else
         PK_ROWS(1024, 4);
 #undef PK_ROWS
