@@ -18,11 +18,14 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -336,6 +339,23 @@ const at::Tensor *vec(PyObject *o, int64_t n, at::ScalarType type, const at::Ten
     return t;
 }
 
+// A new tensor on that device.  Made without torch's dispatcher where the device
+// is the current one (0.5 us a tensor instead of 1.0, and a call makes up to three):
+// no mode is active here that could have a say.
+at::Tensor fresh(at::IntArrayRef size, at::IntArrayRef stride, at::ScalarType type, const at::Tensor &like)
+{
+    if (like.device().index() != c10::hip::current_device())
+        return at::empty_strided(size, stride, like.options().dtype(type));
+    return at::Tensor(at::detail::empty_strided_generic(size, stride,
+                                                        c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get(),
+                                                        c10::DispatchKeySet(c10::DispatchKey::CUDA), type));
+}
+
+at::Tensor fresh_matrix(int64_t M, int64_t N, at::ScalarType type, const at::Tensor &like)
+{
+    return fresh({M, N}, {std::max<int64_t>(N, 1), 1}, type, like);
+}
+
 bool same_shape(const at::Tensor &t, int64_t M, int64_t N, const at::Tensor &like)
 {
     return t.dim() == 2 && t.size(0) == M && t.size(1) == N && t.device() == like.device();
@@ -352,14 +372,14 @@ bool rows_out(PyObject *out, PyObject *scale, int64_t M, int64_t N, const at::Te
 {
     if (out == Py_None) {
         r->ld = std::max<int64_t>(1, (N + 15) / 16 * 16);
-        r->q = at::empty_strided({M, N}, {r->ld, 1}, like.options().dtype(at::kChar));
+        r->q = fresh({M, N}, {r->ld, 1}, at::kChar, like);
     } else {
         const at::Tensor *t = matrix_i8(out, &r->ld);
         if (!t || !same_shape(*t, M, N, like)) return false;
         r->q = *t;
     }
     if (scale == Py_None) {
-        r->scale = at::empty({M}, like.options().dtype(at::kFloat));
+        r->scale = fresh({M}, {1}, at::kFloat, like);
     } else {
         const at::Tensor *t = vec(scale, M, at::kFloat, like);
         if (!t) return false;
@@ -427,7 +447,7 @@ PyObject *py_rmsnorm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         res = matrix(args[2], &dr, &ldr);
         if (!res || dr != dt || !same_shape(*res, M, N, *x)) Py_RETURN_NONE;
         if (args[4] == Py_None) {
-            sum = at::empty({M, N}, x->options());
+            sum = fresh_matrix(M, N, x->scalar_type(), *x);
             lds = std::max<int64_t>(N, 1);
         } else {
             const at::Tensor *t = matrix(args[4], &dr, &lds);
@@ -488,7 +508,7 @@ bool float_out(PyObject *out, PyObject *dtype, at::ScalarType standard, int64_t 
     if (out == Py_None) {
         const at::ScalarType type = dtype == Py_None ? standard : ((THPDtype *)dtype)->scalar_type;
         if ((*code = dtype_code(type)) < 0) return false;
-        *t = at::empty({M, N}, like.options().dtype(type));
+        *t = fresh_matrix(M, N, type, like);
         *ld = std::max<int64_t>(N, 1);
         return true;
     }
