@@ -285,6 +285,8 @@ int launch_rows(const RowArgs &a, hipStream_t s)
         PK_ROWS(256, 2);
     else if (chunks <= 1024)
         PK_ROWS(512, 2);
+    else if (chunks <= 1536)
+        PK_ROWS(512, 3);
     else if (chunks <= 2048)
         PK_ROWS(1024, 2);
     else
