@@ -32,6 +32,9 @@ struct Args {
 // rate of 8 whole ones.  So its 16 rows are the two halves of the 128 bytes of 8
 // rows, of either operand: of its 16 x 16 sums those count whose halves are the
 // same, and the two 8 x 8 parts are added at the end.
+// Bound by the latency of a launch and of memory while B is small, by reading B
+// beyond that: one row, 4096 x 4096 4.9 us (a launch 2 to 3; reading B at a large
+// copy's rate 3.3), 8192 x 8192 12.3 us (5.5 TB/s).  Each eight rows read B again.
 
 // 16 bytes of a row from k on.  At the row's end the last 16 are read instead
 // (both operands do, so the k still agree); the first `drop` of them belong to
@@ -126,7 +129,19 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 //
 // A row's eight 16-byte chunks lie in LDS with their position's low bits
 // exchanged by the row's, so that the sixteen rows a wave reads at once, 128
-// bytes apart, lie in different banks.
+// bytes apart, lie in different banks (no conflicts counted).
+//
+// Where there are few tiles, KG groups of waves share K, each with stages of its
+// own, and add their sums through LDS: half the steps that follow one another
+// (32 x 4096 x 4096: 7.2 us in two groups of 32 x 32, 8.0 in one).
+//
+// What bounds it.  256 x 256, 8192^3: 400 us, 2750 TOP/s: the matrix cores are busy
+// for two thirds of the time at the 1.9 GHz that the power leaves; the same loop
+// without the copies takes 330 us, with copies that stay in L2 377.  128 x 128 and
+// less: the 64 bytes a clock that a CU reads (4096 x 4096 weights: 1024 rows 20.8 us,
+// 512 13.8, 256 10.1), then the latency of a launch, the first block and the
+// stores (32 rows 5.9 us).  Through registers a load from an odd address runs at
+// half the rate, and so do the products: 4096^3 115 us, 60 copied.
 
 // Which row of the wave's 16 TN rows of B element `i` of its tile `t` is: the
 // accumulators of P tiles, 4 P in a lane, are neighbours in a row of C (P such
@@ -153,12 +168,14 @@ struct Source {
     // the wave's 64 lanes' 16 bytes at off + k (k < K), one after the other to
     // `to`; zeros for off < 0.  Written out, because the compiler would wait for
     // every such copy before the next read of LDS, whichever stage that reads;
-    // the kernel's own waits are at its barriers.  A copy's use of m0 comes one
-    // wait state after it is set.
+    // the kernel's own waits are at its barriers.  The compiler does not see what
+    // the copy has to keep from the instructions before it either: m0 is read one
+    // wait state after it is set, scalar operands five after a vector instruction
+    // that may have made them.  m0 has no other use here.
     __device__ __forceinline__ void copy16(int8_t *to, int off, int k) const
     {
         const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                      :
                      : "s"(at), "v"(off), "s"(rs), "s"(k)
                      : "memory");

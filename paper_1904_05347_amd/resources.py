@@ -41,13 +41,15 @@ def parse(path: str = RESOURCE_LOG):
 
 
 def demangle(names):
+    # c++filt does not know the codes of the two 16-bit types: others of the same meaning
+    names = [n.replace("DF16b", "u6__bf16").replace("DF16_", "Dh") for n in names]
     res = subprocess.run(["c++filt"], input="\n".join(names), capture_output=True, text=True, check=True)
     return res.stdout.splitlines()
 
 
 def short(name: str) -> str:
     """pk::(anonymous namespace)::direct_tiled_kernel<8, 1, 2, 1>(pk::KernelArgs) -> direct_tiled_kernel<8, 1, 2, 1>"""
-    name = name.replace("pk::(anonymous namespace)::", "").replace("pk::", "")
+    name = name.replace("(anonymous namespace)::", "").replace("pk::", "")
     if name.startswith("void "):
         name = name[5:]
     depth, out = 0, []
