@@ -1,4 +1,5 @@
-"""Parameterized fp32 GEMM and NHWC convolution forward for AMD MI355X (gfx950).
+"""Parameterized fp32 GEMM and NHWC convolution forward for AMD MI355X (gfx950),
+and the operators of a dense layer on 8-bit integers (``*_i8``).
 
 The compute path is libpk.so (hand-written HIP kernels behind the C-ABI in
 include/pk.h); this package only marshals arguments into it.
