@@ -314,8 +314,9 @@ int pk_tune_reset(void);
  *
  * Conventions beside the common ones: matrices are row-major with a leading
  * dimension in elements; floating elements have one of the types below and
- * their type's alignment, 8-bit ones any address and leading dimension (rows
- * that start at multiples of 16 bytes are read fastest).  Dimensions and
+ * their type's alignment, 8-bit ones any address and leading dimension (a
+ * product reads rows that start at multiples of 128 bytes fastest, then those
+ * at multiples of four).  Dimensions and
  * leading dimensions up to 2^30 (else PK_ERR_NOT_SUPPORTED).  Results are
  * deterministic, and the calls need no workspace.
  */

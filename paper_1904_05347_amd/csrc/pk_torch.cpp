@@ -362,7 +362,7 @@ bool same_shape(const at::Tensor &t, int64_t M, int64_t N, const at::Tensor &lik
 }
 
 // The 8-bit output and its scales: the caller's, or new ones whose rows start
-// at multiples of 16 bytes.
+// at multiples of 16 bytes, long ones at memory lines of 128.
 struct RowsOut {
     at::Tensor q, scale;
     int64_t ld;
@@ -371,7 +371,8 @@ struct RowsOut {
 bool rows_out(PyObject *out, PyObject *scale, int64_t M, int64_t N, const at::Tensor &like, RowsOut *r)
 {
     if (out == Py_None) {
-        r->ld = std::max<int64_t>(1, (N + 15) / 16 * 16);
+        const int64_t step = N >= 1024 ? 128 : 16;
+        r->ld = std::max<int64_t>(1, (N + step - 1) / step * step);
         r->q = fresh({M, N}, {r->ld, 1}, at::kChar, like);
     } else {
         const at::Tensor *t = matrix_i8(out, &r->ld);

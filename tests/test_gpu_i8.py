@@ -418,3 +418,17 @@ def test_refusals(monkeypatch):
     with pytest.raises(P) as e:
         pk.gemm_i8(k, k, v[:2], v[:2])
     assert e.value.status == binding.PK_ERR_NOT_SUPPORTED
+
+
+def test_new_outputs_rows_start_at_memory_lines(monkeypatch):
+    """Through either marshalling; the bytes behind a row are not part of it."""
+    torch, pk = require_gpu()
+    from paper_1904_05347_amd import binding
+    native = binding._native or binding._load_native()
+    for N, ld in ((1, 16), (333, 336), (1008, 1008), (1023, 1024), (1024, 1024), (1025, 1152), (5003, 5120)):
+        x = _rand(torch, N, 3, N, "bf16")
+        for marshalling in (native, _Declines()):
+            monkeypatch.setattr(binding, "_native", marshalling)
+            for q in (pk.quantize_i8(x)[0], pk.rmsnorm_i8(x, torch.ones(N, device="cuda"))[0], pk.gated_i8(x, x)[0]):
+                assert q.shape == (3, N) and q.stride() == (ld, 1) and q.data_ptr() % 16 == 0
+        monkeypatch.setattr(binding, "_native", native)
