@@ -318,7 +318,8 @@ int pk_tune_reset(void);
  * product reads rows that start at multiples of 128 bytes fastest, then those
  * at multiples of four).  Dimensions and
  * leading dimensions up to 2^30 (else PK_ERR_NOT_SUPPORTED).  Results are
- * deterministic, and the calls need no workspace.
+ * deterministic, and the calls need no workspace.  Forced configurations and
+ * splits do not apply to them.
  */
 typedef enum { PK_F32 = 0, PK_BF16 = 1, PK_F16 = 2 } pk_dtype;
 

@@ -140,8 +140,9 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 // without the copies takes 330 us, with copies that stay in L2 377.  128 x 128 and
 // less: the 64 bytes a clock that a CU reads (4096 x 4096 weights: 1024 rows 20.8 us,
 // 512 13.8, 256 10.1), then the latency of a launch, the first block and the
-// stores (32 rows 5.9 us).  Through registers a load from an odd address runs at
-// half the rate, and so do the products: 4096^3 115 us, 60 copied.
+// stores (32 rows 5.9 us).  128 bytes of a row that start inside a memory line are
+// two lines: operands whose rows start at multiples of 16 bytes but not of 128
+// take up to 1.3 times as long, those at odd addresses twice (4096^3 115 us, 60).
 
 // Which row of the wave's 16 TN rows of B element `i` of its tile `t` is: the
 // accumulators of P tiles, 4 P in a lane, are neighbours in a row of C (P such
