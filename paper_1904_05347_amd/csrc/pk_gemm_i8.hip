@@ -9,6 +9,7 @@ namespace {
 using pk::bf16;
 using pk::f16;
 using pk::Pack;
+using pk::rounded;
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 i32x4_u __attribute__((aligned(1)));
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
     for (int w = 0; w < WAVES; ++w) s += part[w][lane] + part[w][lane + 2 * 16 + 8];
     typename Pack<T, 4>::V v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = (T)fmaf((float)s[r], sa * sb[r], bias[r]);
+    for (int r = 0; r < 4; ++r) v[r] = rounded<T>(fmaf((float)s[r], sa * sb[r], bias[r]));
     T *c = (T *)p.C + (int64_t)m * p.ldc + n;
     if (n + 4 <= p.N) {
         *reinterpret_cast<typename Pack<T, 4>::U *>(c) = v;
@@ -435,7 +436,7 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
         auto value = [&](int q) {
             V v;
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = (T)fmaf((float)acc[u][q * P + e / 4][e % 4], sa * sb[q][e], bias[q][e]);
+            for (int e = 0; e < E; ++e) v[e] = rounded<T>(fmaf((float)acc[u][q * P + e / 4][e % 4], sa * sb[q][e], bias[q][e]));
             return v;
         };
         if constexpr (TN / P % 2 == 0 && sizeof(V) == 16) {

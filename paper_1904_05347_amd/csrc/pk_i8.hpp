@@ -21,6 +21,17 @@ struct Pack {
     typedef V U __attribute__((aligned(sizeof(T))));
 };
 
+// An fp32 result in T.  The compiler would fold an fp16 conversion and the
+// operation before it into one instruction, which leaves out the rounding to
+// fp32, for some elements of a lane and not for others: a result's last bit would
+// depend on its column and on the tile.
+template <typename T>
+__device__ __forceinline__ T rounded(float x)
+{
+    if constexpr (sizeof(T) == 2 && !__is_same(T, bf16)) asm("" : "+v"(x));
+    return (T)x;
+}
+
 inline int dtype_size(int dtype)
 {
     return dtype == PK_F32 ? 4 : dtype == PK_BF16 || dtype == PK_F16 ? 2 : 0;

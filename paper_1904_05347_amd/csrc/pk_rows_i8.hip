@@ -26,6 +26,7 @@ namespace {
 using pk::bf16;
 using pk::f16;
 using pk::Pack;
+using pk::rounded;
 
 enum { PLAIN, NORM, GATED };
 
@@ -249,10 +250,10 @@ __global__ void __launch_bounds__(256) dequantize_i8_kernel(const int8_t *q, int
         if (e + E <= N) {
             const typename Pack<int8_t, E>::V b = *reinterpret_cast<const typename Pack<int8_t, E>::U *>(pq + e);
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = (T)((float)b[j] * s);
+            for (int j = 0; j < E; ++j) v[j] = rounded<T>((float)b[j] * s);
         } else {
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = e + j < N ? (T)((float)pq[e + j] * s) : (T)0.f;
+            for (int j = 0; j < E; ++j) v[j] = e + j < N ? rounded<T>((float)pq[e + j] * s) : (T)0.f;
         }
         put(px, e, N, v);
     }

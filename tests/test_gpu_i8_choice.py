@@ -43,6 +43,24 @@ def test_product(M, N, K, aligned, unaligned):
             assert torch.equal(d, (want * 2.0 ** -10 + 1).float().to(dtype))
 
 
+@pytest.mark.parametrize("M,N,K,aligned,unaligned", SIZES)
+def test_one_rounding_from_32_bits(M, N, K, aligned, unaligned):
+    """Results in 16 bits are those in 32 bits rounded once more, whatever the tile and the column."""
+    torch, pk = require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(7)
+    sa, sb = torch.rand(M, generator=g, device="cuda") * 2.0 ** -6, torch.rand(N, generator=g, device="cuda")
+    bias = torch.rand(N, generator=g, device="cuda")
+    for ld in ((K + 15) // 16 * 16, K | 1):
+        a, b = _int8(torch, 1, M, K, ld), _int8(torch, 2, N, K, ld)
+        for given in (None, bias):
+            c = pk.gemm_i8(a, b, sa, sb, bias=given, dtype=torch.float32)
+            for dtype in (torch.bfloat16, torch.float16):
+                assert torch.equal(pk.gemm_i8(a, b, sa, sb, bias=given, dtype=dtype), c.to(dtype))
+        back = pk.dequantize_i8(a, sa)
+        for dtype in (torch.bfloat16, torch.float16):
+            assert torch.equal(pk.dequantize_i8(a, sa, dtype=dtype), back.to(dtype))
+
+
 def test_every_configuration_is_chosen():
     src = open(os.path.join(ROOT, "paper_1904_05347_amd", "csrc", "pk_gemm_i8.hip")).read()
     names = set(re.findall(r'\{"gemm_i8_(\w+)", \d+', src))
