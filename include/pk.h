@@ -318,7 +318,7 @@ int pk_tune_reset(void);
  * product reads rows that start at multiples of 128 bytes fastest, then those
  * at multiples of four).  Dimensions and
  * leading dimensions up to 2^30 (else PK_ERR_NOT_SUPPORTED).  Results are
- * deterministic, and the calls need no workspace.  Forced configurations and
+ * deterministic, and no call needs a workspace.  Forced configurations and
  * splits do not apply to them.
  */
 typedef enum { PK_F32 = 0, PK_BF16 = 1, PK_F16 = 2 } pk_dtype;
@@ -388,6 +388,29 @@ int pk_dequantize_i8(const int8_t *q, int64_t ldq, const float *scale, int64_t M
 int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
                const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
                void *C, int dtype, int64_t ldc, void *stream);
+
+/*
+ * Bytes of device workspace that lets pk_gemm_i8_ws lay out rows of A or B
+ * that start at addresses other than multiples of four (nothing is read); 0
+ * where they do not, and where the product is faster without.  At most 1 GiB.
+ */
+size_t pk_gemm_i8_workspace_bytes_for(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda,
+                                      const int8_t *B, int64_t ldb);
+
+/*
+ * pk_gemm_i8 with a workspace (the same operation, arguments, quick returns
+ * and result, bit for bit; error positions as there, then 14 = workspace).
+ *   workspace    optional device buffer of workspace_bytes, 16-byte aligned;
+ *                with at least pk_gemm_i8_workspace_bytes_for() the rows of
+ *                operands that start at odd addresses are copied there first,
+ *                to whole memory lines.  NULL, too small or misaligned: they
+ *                are read where they are.  It must not overlap another
+ *                argument.  Contents on return are unspecified.  Two calls
+ *                that overlap in time must not share a workspace.
+ */
+int pk_gemm_i8_ws(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
+                  const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
+                  void *C, int dtype, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static text for a status code. */
 const char *pk_status_string(int status);

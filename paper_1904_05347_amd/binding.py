@@ -97,6 +97,9 @@ SIGNATURES = {
     "pk_gated_i8": (ctypes.c_int, [_p, _i64, _p, _i64, ctypes.c_int, ctypes.c_int, _i64, _i64, _p, _i64, _p, _p]),
     "pk_dequantize_i8": (ctypes.c_int, [_p, _i64, _p, _i64, _i64, _p, ctypes.c_int, _i64, _p]),
     "pk_gemm_i8": (ctypes.c_int, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _p, ctypes.c_int, _i64, _p]),
+    "pk_gemm_i8_workspace_bytes_for": (ctypes.c_size_t, [_i64, _i64, _i64, _p, _i64, _p, _i64]),
+    "pk_gemm_i8_ws": (ctypes.c_int, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _p, ctypes.c_int, _i64,
+                                     _p, ctypes.c_size_t, _p]),
     "pk_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "pk_last_invalid_param": (ctypes.c_int, []),
     "pk_last_config_name": (ctypes.c_char_p, []),
@@ -138,7 +141,7 @@ EXT_PATH = os.path.join(HERE, "_pk_torch.so")
 _NATIVE_ENTRIES = ("pk_sgemm_ws", "pk_sgemm_workspace_bytes_for", "pk_conv2d_fwd", "pk_conv2d_workspace_bytes_for",
                    "pk_conv2d_out_dims", "pk_conv2d_same_pads", "pk_conv2d_winograd_tile_fwd",
                    "pk_conv2d_winograd_tile_workspace_bytes", "pk_quantize_i8", "pk_rmsnorm_i8", "pk_gated_i8",
-                   "pk_dequantize_i8", "pk_gemm_i8")
+                   "pk_dequantize_i8", "pk_gemm_i8_ws", "pk_gemm_i8_workspace_bytes_for")
 _native = None
 
 
@@ -655,15 +658,18 @@ def dequantize_i8(q, scale, dtype=None, out=None):
     return out
 
 
-def gemm_i8(a, b, a_scale, b_scale, bias=None, dtype=None, out=None):
+def gemm_i8(a, b, a_scale, b_scale, bias=None, dtype=None, out=None, workspace=None):
     """Product of 8-bit integers with a scale for each row of either side:
     out[m, n] = a_scale[m] * b_scale[n] * sum_k a[m, k] * b[n, k] + bias[n].
 
     ``a`` is M x K (tokens), ``b`` N x K (a row is an output channel), both int8
     row-major views with unit column stride; the sum is exact.  The result is
     rounded once, to ``dtype`` (that of ``out``, or bfloat16, when None).
+    workspace (a float32 device tensor) lets rows that start at odd addresses be
+    laid out first, which changes no bit of the result; when None, one of the
+    size the library asks for is allocated.
     """
-    r = (_native or _load_native()).gemm_i8(a, b, a_scale, b_scale, bias, dtype, out)
+    r = (_native or _load_native()).gemm_i8(a, b, a_scale, b_scale, bias, dtype, out, workspace)
     if r is not None:
         return r
     import torch
@@ -685,9 +691,20 @@ def gemm_i8(a, b, a_scale, b_scale, bias=None, dtype=None, out=None):
     dt = _dtype_code(out.dtype, "out")
     if tuple(out.shape) != (M, N):
         raise ValueError("out must be %d x %d" % (M, N))
-    _check(load().pk_gemm_i8(M, N, K, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
-                             None if bias is None else bias.data_ptr(), out.data_ptr(), dt, _ld_2d(out, "out"),
-                             _stream_handle(a)), "pk_gemm_i8")
+    ldc = _ld_2d(out, "out")
+    if workspace is None:
+        need = load().pk_gemm_i8_workspace_bytes_for(M, N, K, a.data_ptr(), lda, b.data_ptr(), ldb)
+        if need:
+            workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=a.device)
+    ws_ptr, ws_bytes = None, 0
+    if workspace is not None:
+        _check_cuda(workspace, "workspace", torch.float32, a)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * 4
+    _check(load().pk_gemm_i8_ws(M, N, K, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
+                                None if bias is None else bias.data_ptr(), out.data_ptr(), dt, ldc, ws_ptr, ws_bytes,
+                                _stream_handle(a)), "pk_gemm_i8_ws")
     return out
 
 

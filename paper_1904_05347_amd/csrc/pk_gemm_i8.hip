@@ -143,7 +143,8 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 // 512 13.8, 256 10.1), then the latency of a launch, the first block and the
 // stores (32 rows 5.9 us).  128 bytes of a row that start inside a memory line are
 // two lines: operands whose rows start at multiples of 16 bytes but not of 128
-// take up to 1.3 times as long, those at odd addresses twice (4096^3 115 us, 60).
+// take up to 1.3 times as long, those at odd addresses twice (4096^3 114 us, 57):
+// with a workspace larger products copy such rows to whole lines first.
 
 // Which row of the wave's 16 TN rows of B element `i` of its tile `t` is: the
 // accumulators of P tiles, 4 P in a lane, are neighbours in a row of C (P such
@@ -465,6 +466,55 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
     }
 }
 
+// ------------------------------------------------- rows laid out at memory lines
+
+// Rows that start anywhere, copied to rows of whole memory lines, once, where a
+// product would read them several times at twice the lines.  A wave takes 2048
+// bytes of a row, a lane 16 at a time (1024 bytes a wave take the same, loads
+// past the cache 5 % of the product longer: its reader finds the rest there).
+// The last 16 bytes of a row are filled up with zeros.  Bound by memory: 2330 +
+// 5318 rows of 6724 bytes 17 us, 6.0 TB/s read and written, some of it in cache;
+// a few MB take a launch and its latency, 3 to 6 us.  4096^3 of odd rows: 70 us,
+// 114 as they lie.
+struct Rows {
+    const int8_t *from;
+    int64_t ld;
+    int8_t *to;
+    int rows;
+};
+struct Layout {
+    Rows a, b;  // rows == 0: the operand stays where it is
+    int64_t ld;
+    int K, parts;  // parts of 2048 bytes of a row
+};
+
+__global__ void __launch_bounds__(256) gemm_i8_lay_out_kernel(Layout p)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t row = wave / p.parts;
+    const int part = (int)(wave - row * p.parts);
+    const bool of_b = row >= p.a.rows;
+    if (of_b) row -= p.a.rows;
+    if (of_b && row >= p.b.rows) return;
+    const int8_t *from = of_b ? p.b.from + row * p.b.ld : p.a.from + row * p.a.ld;
+    int8_t *to = (of_b ? p.b.to : p.a.to) + row * p.ld;
+    i32x4 v[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int k = part * 2048 + u * 1024 + lane * 16;
+        if (k >= p.K) continue;
+        v[u] = *reinterpret_cast<const i32x4_u *>(from + (k + 16 <= p.K ? k : p.K - 16));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int k = part * 2048 + u * 1024 + lane * 16, late = k + 16 - p.K;
+        if (k >= p.K) continue;
+        if (late > 0) v[u] = __builtin_bit_cast(i32x4, __builtin_bit_cast(unsigned __int128, v[u]) >> (8 * late));
+        *reinterpret_cast<i32x4 *>(to + k) = v[u];
+    }
+}
+
 // K == 0: the bias, or zeros.
 template <typename T>
 __global__ void __launch_bounds__(256) gemm_i8_empty_kernel(Args p)
@@ -479,6 +529,7 @@ __global__ void __launch_bounds__(256) gemm_i8_empty_kernel(Args p)
 // ---------------------------------------------------------------- launches
 
 constexpr int64_t kMostLd = 1 << 22;  // of gemm_i8_tile_kernel
+constexpr int kMostK = 131071;         // 128 * 128 * K stays below 2^31
 constexpr int kMostSide = 1 << 17;    // rows and columns of C of one launch
 
 template <typename T, int BM, int BN, int WM, int WN, int KG, int STAGES, bool DMA>
@@ -576,20 +627,58 @@ float predicted_us(const Config &c, const Args &a)
     return c.base + c.round * (float)rounds + share * (float)steps * (least > block ? least : block);
 }
 
-const Config *choose(const Args &a)
+bool rows_of_words(const int8_t *at, int64_t ld) { return ((uintptr_t)at | (uintptr_t)ld) % 4 == 0; }
+
+const Config *choose(const Args &a, float *us = nullptr)
 {
-    const bool dma = ((uintptr_t)a.A | (uintptr_t)a.B | (uintptr_t)a.lda | (uintptr_t)a.ldb) % 4 == 0;
+    const bool dma = rows_of_words(a.A, a.lda) && rows_of_words(a.B, a.ldb);
     const Config *from = dma ? kAligned : kUnaligned, *rows = dma ? kAligned + 8 : kUnaligned + 6;
-    if (a.lda > kMostLd || a.ldb > kMostLd) return rows;
-    const Config *best = from;
-    float least = predicted_us(*from, a);
-    for (const Config *c = from + 1; c <= rows; ++c) {
+    const Config *best = a.lda > kMostLd || a.ldb > kMostLd ? rows : from;
+    float least = predicted_us(*best, a);
+    for (const Config *c = best + 1; c <= rows; ++c) {
         const float t = predicted_us(*c, a);
         if (t >= least) continue;
         best = c;
         least = t;
     }
+    if (us) *us = least;
     return best;
+}
+
+constexpr int64_t kMostLayout = (int64_t)1 << 30;  // bytes of workspace
+
+// Bytes of workspace for the rows of A, B or both laid out at memory lines, and
+// what is laid out; 0 where they stay.  Only rows at other addresses than
+// multiples of four: those at multiples of 4 or 16 lose less than the copy takes
+// (2330 x 5318 x 6724: 97 and 95 us, at lines 81, laid out first 98).  Rows under
+// a K-block have nothing to gain.  The copy is predicted as 3 us and 0.3 us a
+// megabyte, at 300 sizes of odd rows: the choice takes 0.5 % longer than the
+// better of both at each size, 9 % less than never laying out, 7 % more at worst.
+size_t layout_of(const Args &a, Layout *p)
+{
+    *p = {};
+    if (rows_of_words(a.A, a.lda) && rows_of_words(a.B, a.ldb)) return 0;
+    if (a.K < 128) return 0;
+    Args laid = a;
+    p->ld = ((int64_t)a.K + 127) & ~(int64_t)127;
+    p->K = a.K;
+    p->parts = (a.K + 2047) / 2048;
+    if (!rows_of_words(a.A, a.lda)) {
+        p->a = {a.A, a.lda, nullptr, a.M};
+        laid.A = nullptr;
+        laid.lda = p->ld;
+    }
+    if (!rows_of_words(a.B, a.ldb)) {
+        p->b = {a.B, a.ldb, nullptr, a.N};
+        laid.B = nullptr;
+        laid.ldb = p->ld;
+    }
+    const int64_t bytes = ((int64_t)p->a.rows + p->b.rows) * p->ld;
+    if (bytes > kMostLayout) return 0;
+    float as_it_is, after;
+    choose(a, &as_it_is);
+    choose(laid, &after);
+    return after + 3.f + 0.3e-6f * (float)bytes < as_it_is ? (size_t)bytes : 0;
 }
 
 template <typename T>
@@ -625,9 +714,19 @@ int launch(const Args &a, hipStream_t s)
 
 }  // namespace
 
-extern "C" int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
-                          const int8_t *B, int64_t ldb, const float *b_scale, const float *bias, void *C, int dtype,
-                          int64_t ldc, void *stream)
+extern "C" size_t pk_gemm_i8_workspace_bytes_for(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda,
+                                                 const int8_t *B, int64_t ldb)
+{
+    using namespace pk::checks;
+    if (M <= 0 || N <= 0 || K <= 0 || short_ld(lda, K) || short_ld(ldb, K)) return 0;
+    if (too_large({M, N, lda, ldb}) || K > kMostK) return 0;
+    Layout p;
+    return layout_of({A, B, nullptr, nullptr, nullptr, nullptr, lda, ldb, 0, (int)M, (int)N, (int)K, false}, &p);
+}
+
+extern "C" int pk_gemm_i8_ws(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
+                             const int8_t *B, int64_t ldb, const float *b_scale, const float *bias, void *C, int dtype,
+                             int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
 {
     using namespace pk;
     using namespace pk::checks;
@@ -641,7 +740,7 @@ extern "C" int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int6
     if (!size) return api_invalid(12);
     if (short_ld(ldc, N)) return api_invalid(13);
     if (M == 0 || N == 0) return PK_OK;
-    if (too_large({M, N, lda, ldb, ldc}) || K > 131071) return PK_ERR_NOT_SUPPORTED;
+    if (too_large({M, N, lda, ldb, ldc}) || K > kMostK) return PK_ERR_NOT_SUPPORTED;
     if (misaligned(bias, 4)) return api_invalid(10);
     if (!C || misaligned(C, size)) return api_invalid(11);
     const Span sc = span(C, M, N, ldc, size);
@@ -659,7 +758,36 @@ extern "C" int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int6
     // a larger one is written past it (8192^3 to bf16 398 us, 407 through it;
     // 4096 x 16384 x 4096 217 and 229; 8192 x 4096 x 1024, 67 MB, 42.4 and 40.1)
     const bool beyond_cache = M * N * size > (int64_t)96 << 20;
-    const Args a = {A, B, a_scale, b_scale, bias, C, lda, ldb, ldc, (int)M, (int)N, (int)K, beyond_cache};
+    Args a = {A, B, a_scale, b_scale, bias, C, lda, ldb, ldc, (int)M, (int)N, (int)K, beyond_cache};
     hipStream_t s = (hipStream_t)stream;
+    Layout p;
+    const size_t need = workspace && !misaligned(workspace, 16) ? layout_of(a, &p) : 0;
+    if (need && need <= workspace_bytes) {
+        const Span ws = {(uintptr_t)workspace, (uintptr_t)workspace + need};
+        if (overlap(ws, sc) || overlap(ws, span(A, M, K, lda, 1)) || overlap(ws, span(B, N, K, ldb, 1)) ||
+            overlap(ws, span(a_scale, 1, M, M, 4)) || overlap(ws, span(b_scale, 1, N, N, 4)) ||
+            (bias && overlap(ws, span(bias, 1, N, N, 4))))
+            return api_invalid(14);
+        int8_t *to = (int8_t *)workspace;
+        if (p.a.rows) {
+            a.A = p.a.to = to;
+            a.lda = p.ld;
+            to += p.a.rows * p.ld;
+        }
+        if (p.b.rows) {
+            a.B = p.b.to = to;
+            a.ldb = p.ld;
+        }
+        const int64_t waves = ((int64_t)p.a.rows + p.b.rows) * p.parts;
+        hipLaunchKernelGGL(gemm_i8_lay_out_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p);
+        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    }
     return dtype == PK_F32 ? launch<float>(a, s) : dtype == PK_BF16 ? launch<bf16>(a, s) : launch<f16>(a, s);
+}
+
+extern "C" int pk_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda, const float *a_scale,
+                          const int8_t *B, int64_t ldb, const float *b_scale, const float *bias, void *C, int dtype,
+                          int64_t ldc, void *stream)
+{
+    return pk_gemm_i8_ws(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, C, dtype, ldc, nullptr, 0, stream);
 }

@@ -50,7 +50,8 @@ decltype(&pk_quantize_i8) f_quantize_i8;
 decltype(&pk_rmsnorm_i8) f_rmsnorm_i8;
 decltype(&pk_gated_i8) f_gated_i8;
 decltype(&pk_dequantize_i8) f_dequantize_i8;
-decltype(&pk_gemm_i8) f_gemm_i8;
+decltype(&pk_gemm_i8_ws) f_gemm_i8;
+decltype(&pk_gemm_i8_workspace_bytes_for) f_gemm_i8_workspace_bytes;
 PyObject *f_check;  // binding._check(status, entry point): raises
 
 // The answer to a status other than PK_OK.
@@ -115,7 +116,7 @@ bool workspace_for(PyObject *given, size_t need, const at::Tensor &like, at::Ten
         *ptr = w->data_ptr();
         *bytes = (size_t)w->numel() * 4;
     } else if (need) {
-        *own = at::empty({(int64_t)((need + 3) / 4)}, like.options());
+        *own = at::empty({(int64_t)((need + 3) / 4)}, like.options().dtype(at::kFloat));
         *ptr = own->data_ptr();
         *bytes = (size_t)own->numel() * 4;
     }
@@ -544,28 +545,36 @@ PyObject *py_dequantize_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// gemm_i8(a, b, a_scale, b_scale, bias, dtype, out)
+// gemm_i8(a, b, a_scale, b_scale, bias, dtype, out, workspace)
 PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     int dt;
     int64_t lda, ldb, ldc;
-    at::Tensor c;
-    if (nargs != 7 || modes_active()) Py_RETURN_NONE;
+    at::Tensor c, own;
+    if (nargs != 8 || modes_active()) Py_RETURN_NONE;
     const at::Tensor *a = matrix_i8(args[0], &lda), *b = matrix_i8(args[1], &ldb), *bias = nullptr;
     if (!a || !b || a->size(1) != b->size(1) || a->device() != b->device()) Py_RETURN_NONE;
     const int64_t M = a->size(0), N = b->size(0), K = a->size(1);
     const at::Tensor *sa = vec(args[2], M, at::kFloat, *a), *sb = vec(args[3], N, at::kFloat, *a);
     if (!sa || !sb || (args[4] != Py_None && !(bias = vec(args[4], N, at::kFloat, *a)))) Py_RETURN_NONE;
     if (!float_out(args[6], args[5], at::kBFloat16, M, N, *a, &c, &dt, &ldc)) Py_RETURN_NONE;
+    const int8_t *pa = (const int8_t *)a->data_ptr(), *pb = (const int8_t *)b->data_ptr();
+    const size_t need = args[7] == Py_None ? f_gemm_i8_workspace_bytes(M, N, K, pa, lda, pb, ldb) : 0;
+    void *ws;
+    size_t ws_bytes;
+    if (args[7] != Py_None) {
+        const at::Tensor *w = plain(args[7]);
+        if (!w || !w->is_contiguous() || w->device() != a->device()) Py_RETURN_NONE;
+    }
+    if (!workspace_for(args[7], need, *a, &own, &ws, &ws_bytes)) Py_RETURN_NONE;
     void *stream = stream_of(*a);
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_gemm_i8(M, N, K, (const int8_t *)a->data_ptr(), lda, (const float *)sa->data_ptr(),
-                   (const int8_t *)b->data_ptr(), ldb, (const float *)sb->data_ptr(),
-                   bias ? (const float *)bias->data_ptr() : nullptr, c.data_ptr(), dt, ldc, stream);
+    st = f_gemm_i8(M, N, K, pa, lda, (const float *)sa->data_ptr(), pb, ldb, (const float *)sb->data_ptr(),
+                   bias ? (const float *)bias->data_ptr() : nullptr, c.data_ptr(), dt, ldc, ws, ws_bytes, stream);
     Py_END_ALLOW_THREADS
-    if (st != PK_OK) return refused(st, "pk_gemm_i8");
+    if (st != PK_OK) return refused(st, "pk_gemm_i8_ws");
     return given_or(args[6], std::move(c));
     END_HANDLE_TH_ERRORS
 }
@@ -574,9 +583,9 @@ PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 // function that raises for a status.
 PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    constexpr int kEntries = 13;
+    constexpr int kEntries = 14;
     if (nargs != kEntries + 1) {
-        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of thirteen entry points and a function");
+        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of fourteen entry points and a function");
         return nullptr;
     }
     void *p[kEntries];
@@ -600,6 +609,7 @@ PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     f_gated_i8 = (decltype(f_gated_i8))p[10];
     f_dequantize_i8 = (decltype(f_dequantize_i8))p[11];
     f_gemm_i8 = (decltype(f_gemm_i8))p[12];
+    f_gemm_i8_workspace_bytes = (decltype(f_gemm_i8_workspace_bytes))p[13];
     Py_INCREF(args[kEntries]);
     Py_XSETREF(f_check, args[kEntries]);
     Py_RETURN_NONE;

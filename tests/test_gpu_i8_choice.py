@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
-# (M, N, K, configuration of aligned rows, of rows that start at any byte)
+# (M, N, K, configuration of aligned rows, of rows that start at any byte and stay there)
 SIZES = [(3000, 4100, 1500, "256x256", "128x256_any"), (2300, 2700, 777, "128x256", "128x256_any"), (675, 3052, 775, "128x128", "128x128_any"),
          (1800, 2100, 1100, "128x128", "128x128_any"), (700, 1500, 700, "64x128", "64x64_any"), (986, 519, 649, "64x64_k2", "64x64_k2_any"),
          (1327, 395, 954, "64x64_k2", "64x64_k2_any"), (500, 900, 1300, "32x64_k2", "32x32_k4_any"), (332, 784, 260, "32x64_k2", "64x64_any"),
@@ -31,16 +31,18 @@ def _int8(torch, seed, rows, cols, ld):
 def test_product(M, N, K, aligned, unaligned):
     torch, pk = require_gpu()
     one = torch.ones(max(M, N), device="cuda")
+    none = torch.empty(0, device="cuda")  # no workspace
     for ld, want_name in (((K + 15) // 16 * 16, aligned), ((K + 3) // 4 * 4, aligned), (K | 1, unaligned)):
         a, b = _int8(torch, 1, M, K, ld), _int8(torch, 2, N, K, ld)
         want = a.double() @ b.double().t().contiguous()
-        c = pk.gemm_i8(a, b, one[:M], one[:N], dtype=torch.float32)
+        c = pk.gemm_i8(a, b, one[:M], one[:N], dtype=torch.float32, workspace=none)
         assert pk.last_config_name() == "gemm_i8_" + want_name
         assert torch.equal(c.double(), want)
         for dtype in (torch.bfloat16, torch.float16):
             small = one * 2.0 ** -10
-            d = pk.gemm_i8(a, b, small[:M], one[:N], bias=one[:N], dtype=dtype)
+            d = pk.gemm_i8(a, b, small[:M], one[:N], bias=one[:N], dtype=dtype, workspace=none)
             assert torch.equal(d, (want * 2.0 ** -10 + 1).float().to(dtype))
+        assert torch.equal(c, pk.gemm_i8(a, b, one[:M], one[:N], dtype=torch.float32))
 
 
 @pytest.mark.parametrize("M,N,K,aligned,unaligned", SIZES)

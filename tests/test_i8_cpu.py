@@ -86,6 +86,35 @@ def test_gemm_arguments(lib):
     assert lib.pk_last_config_name() == b""
 
 
+def test_gemm_workspace_arguments(lib):
+    good = dict(M=4, N=5, K=6, A=FAKE, lda=6, sa=2 * FAKE, B=3 * FAKE, ldb=6, sb=4 * FAKE, bias=5 * FAKE, C=6 * FAKE,
+                dtype=0, ldc=5, workspace=None, workspace_bytes=0)
+    _cases(lib, lib.pk_gemm_i8_ws, good, [("M", -1, 1), ("lda", 5, 5), ("A", None, 4), ("C", None, 11), ("dtype", 3, 12), ("ldc", 4, 13)],
+           [("lda", 1 << 31)])
+    # a product whose rows are laid out: 4096 + 4096 rows of 4097 bytes, 16 MiB each operand and the result
+    at = [(8 + i) << 28 for i in range(7)]
+    big = dict(M=4096, N=4096, K=4097, A=at[0], lda=4097, sa=at[1], B=at[2], ldb=4097, sb=at[3], bias=at[4], C=at[5],
+               dtype=0, ldc=4096, workspace=at[6], workspace_bytes=1 << 28)
+    need = lib.pk_gemm_i8_workspace_bytes_for(4096, 4096, 4097, at[0], 4097, at[2], 4097)
+    assert need == 8192 * 4224
+    overlapping = [(name, at[i] - need + 16) for i, name in enumerate(("A", "sa", "B", "sb", "bias", "C"))]
+    _cases(lib, lib.pk_gemm_i8_ws, big, [("workspace", w, 14) for _, w in overlapping], [])
+
+
+def test_gemm_workspace_query(lib):
+    def need(M, N, K, lda, ldb, A=FAKE, B=3 * FAKE):
+        return lib.pk_gemm_i8_workspace_bytes_for(M, N, K, A, lda, B, ldb)
+    assert need(4096, 4096, 4096, 4096, 4096) == need(4096, 4096, 4096, 4100, 4100) == 0
+    assert need(4096, 4096, 4096, 4097, 4096) == need(4096, 4096, 4096, 4096, 4097) == 4096 * 4096
+    assert need(4096, 4096, 4096, 4096, 4096, A=FAKE + 1) == 4096 * 4096
+    assert need(4096, 4096, 4001, 4001, 4003) == 8192 * 4096
+    assert need(1, 4096, 4096, 4097, 4097) == need(64, 64, 64, 65, 65) == need(8192, 8192, 127, 127, 127) == 0
+    for bad in ((-1, 9, 9, 9, 9), (9, 0, 9, 9, 9), (9, 9, 0, 9, 9), (4096, 4096, 4001, 4000, 4001), (4096, 4096, 4001, 4001, 1 << 31),
+                (4096, 4096, 131073, 131073, 131073)):
+        assert need(*bad) == 0
+    assert 0 < need(200000, 4096, 5001, 5001, 5001) <= 1 << 30 and need(1 << 20, 4096, 5001, 5001, 5001) == 0
+
+
 def test_tensors_on_the_cpu_are_refused(lib):
     import torch
 
