@@ -2,6 +2,10 @@
 // conv2d_winograd and the 8-bit operators) marshalled natively: torch tensors in, one C-ABI call on the
 // current stream, the output tensor out.
 //
+// Every pointer is read before the interpreter lock is released: data_ptr()
+// throws for a tensor without a storage, and an exception must not leave the
+// part that runs without the lock.
+//
 // Why: a 64 x 64 x 64 product takes the GPU 4 us, the C-ABI call 0.8 us and
 // its launch 2.9 us, but marshalled in Python (attribute reads, two ctypes
 // calls, the allocations) a call took 12.5 us of host time, and that was the
@@ -308,12 +312,13 @@ int dtype_code(at::ScalarType t)
     return t == at::kFloat ? PK_F32 : t == at::kBFloat16 ? PK_BF16 : t == at::kHalf ? PK_F16 : -1;
 }
 
-// A plain strided tensor on a GPU, or NULL.
+// A plain strided tensor on a GPU, or NULL.  A transform's wrapper (torch.func)
+// has the type and answers of a plain tensor, but no storage.
 const at::Tensor *on_gpu(PyObject *o)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.layout() == at::kStrided ? &t : nullptr;
+    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
 }
 
 // A plain matrix of float32, bfloat16 or float16, with its code and leading dimension.
@@ -342,7 +347,7 @@ const at::Tensor *vec(PyObject *o, int64_t n, at::ScalarType type, const at::Ten
 
 // A new tensor on that device.  Made without torch's dispatcher where the device
 // is the current one (0.5 us a tensor instead of 1.0, and a call makes up to three):
-// no mode is active here that could have a say.
+// no mode is active here that could have a say, and every operand has a storage.
 at::Tensor fresh(at::IntArrayRef size, at::IntArrayRef stride, at::ScalarType type, const at::Tensor &like)
 {
     if (like.device().index() != c10::hip::current_device())
@@ -417,11 +422,13 @@ PyObject *py_quantize_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (nargs != 3 || modes_active()) Py_RETURN_NONE;
     const at::Tensor *x = matrix(args[0], &dt, &ldx);
     if (!x || !rows_out(args[1], args[2], x->size(0), x->size(1), *x, &r)) Py_RETURN_NONE;
-    void *stream = stream_of(*x);
+    void *stream = stream_of(*x), *px = x->data_ptr();
+    const int64_t M = x->size(0), N = x->size(1);
+    int8_t *q = (int8_t *)r.q.data_ptr();
+    float *scale = (float *)r.scale.data_ptr();
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_quantize_i8(x->data_ptr(), dt, x->size(0), x->size(1), ldx, (int8_t *)r.q.data_ptr(), r.ld,
-                       (float *)r.scale.data_ptr(), stream);
+    st = f_quantize_i8(px, dt, M, N, ldx, q, r.ld, scale, stream);
     Py_END_ALLOW_THREADS
     if (st != PK_OK) return refused(st, "pk_quantize_i8");
     return pair(args[1], args[2], std::move(r));
@@ -458,12 +465,13 @@ PyObject *py_rmsnorm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         }
     }
     if (!rows_out(args[5], args[6], M, N, *x, &r)) Py_RETURN_NONE;
-    void *stream = stream_of(*x);
+    void *stream = stream_of(*x), *px = x->data_ptr(), *pr = res ? res->data_ptr() : nullptr, *pw = w->data_ptr(),
+         *ps = res ? sum.data_ptr() : nullptr;
+    int8_t *q = (int8_t *)r.q.data_ptr();
+    float *scale = (float *)r.scale.data_ptr();
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_rmsnorm_i8(x->data_ptr(), dt, M, N, ldx, res ? res->data_ptr() : nullptr, ldr, w->data_ptr(), wt, eps,
-                      res ? sum.data_ptr() : nullptr, lds, (int8_t *)r.q.data_ptr(), r.ld,
-                      (float *)r.scale.data_ptr(), stream);
+    st = f_rmsnorm_i8(px, dt, M, N, ldx, pr, ldr, pw, wt, eps, ps, lds, q, r.ld, scale, stream);
     Py_END_ALLOW_THREADS
     if (st != PK_OK) return refused(st, "pk_rmsnorm_i8");
     PyObject *a = given_or(args[5], std::move(r.q)), *b = a ? given_or(args[6], std::move(r.scale)) : nullptr;
@@ -490,11 +498,13 @@ PyObject *py_gated_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     const at::Tensor *gate = matrix(args[0], &dt, &ldg), *up = matrix(args[1], &du, &ldu);
     if (act < 0 || !gate || !up || du != dt || !same_shape(*up, gate->size(0), gate->size(1), *gate)) Py_RETURN_NONE;
     if (!rows_out(args[3], args[4], gate->size(0), gate->size(1), *gate, &r)) Py_RETURN_NONE;
-    void *stream = stream_of(*gate);
+    void *stream = stream_of(*gate), *pg = gate->data_ptr(), *pu = up->data_ptr();
+    const int64_t M = gate->size(0), N = gate->size(1);
+    int8_t *q = (int8_t *)r.q.data_ptr();
+    float *scale = (float *)r.scale.data_ptr();
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_gated_i8(gate->data_ptr(), ldg, up->data_ptr(), ldu, dt, act, gate->size(0), gate->size(1),
-                    (int8_t *)r.q.data_ptr(), r.ld, (float *)r.scale.data_ptr(), stream);
+    st = f_gated_i8(pg, ldg, pu, ldu, dt, act, M, N, q, r.ld, scale, stream);
     Py_END_ALLOW_THREADS
     if (st != PK_OK) return refused(st, "pk_gated_i8");
     return pair(args[3], args[4], std::move(r));
@@ -534,11 +544,12 @@ PyObject *py_dequantize_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     const int64_t M = q->size(0), N = q->size(1);
     const at::Tensor *scale = vec(args[1], M, at::kFloat, *q);
     if (!scale || !float_out(args[3], args[2], at::kFloat, M, N, *q, &x, &dt, &ldx)) Py_RETURN_NONE;
-    void *stream = stream_of(*q);
+    void *stream = stream_of(*q), *px = x.data_ptr();
+    const int8_t *pq = (const int8_t *)q->data_ptr();
+    const float *ps = (const float *)scale->data_ptr();
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_dequantize_i8((const int8_t *)q->data_ptr(), ldq, (const float *)scale->data_ptr(), M, N, x.data_ptr(), dt,
-                         ldx, stream);
+    st = f_dequantize_i8(pq, ldq, ps, M, N, px, dt, ldx, stream);
     Py_END_ALLOW_THREADS
     if (st != PK_OK) return refused(st, "pk_dequantize_i8");
     return given_or(args[3], std::move(x));
@@ -568,11 +579,12 @@ PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         if (!w || !w->is_contiguous() || w->device() != a->device()) Py_RETURN_NONE;
     }
     if (!workspace_for(args[7], need, *a, &own, &ws, &ws_bytes)) Py_RETURN_NONE;
-    void *stream = stream_of(*a);
+    void *stream = stream_of(*a), *pc = c.data_ptr();
+    const float *psa = (const float *)sa->data_ptr(), *psb = (const float *)sb->data_ptr(),
+                *pbias = bias ? (const float *)bias->data_ptr() : nullptr;
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = f_gemm_i8(M, N, K, pa, lda, (const float *)sa->data_ptr(), pb, ldb, (const float *)sb->data_ptr(),
-                   bias ? (const float *)bias->data_ptr() : nullptr, c.data_ptr(), dt, ldc, ws, ws_bytes, stream);
+    st = f_gemm_i8(M, N, K, pa, lda, psa, pb, ldb, psb, pbias, pc, dt, ldc, ws, ws_bytes, stream);
     Py_END_ALLOW_THREADS
     if (st != PK_OK) return refused(st, "pk_gemm_i8_ws");
     return given_or(args[6], std::move(c));
