@@ -18,6 +18,7 @@
 // row of 4096: 2.6 us).
 #include "pk_i8.hpp"
 #include "pk_i8_checks.hpp"
+#include "pk_rows_i8_launch.hpp"
 
 #pragma clang fp contract(off)  // z times that factor is rounded before it is rounded to an integer
 
@@ -25,8 +26,11 @@ namespace {
 
 using pk::bf16;
 using pk::f16;
+using pk::kMostRows;
 using pk::Pack;
 using pk::rounded;
+using pk::rows_group;
+using pk::rows_groups;
 
 enum { PLAIN, NORM, GATED };
 
@@ -145,11 +149,11 @@ __device__ __forceinline__ void quantized(int8_t *q, int e, int N, const float *
 
 // TPR work-items a row, VPT 16-byte chunks of it in each one's registers.
 template <typename T, typename W, int MODE, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rows_i8_kernel(RowArgs p)
+__global__ void __launch_bounds__(rows_group(TPR)) rows_i8_kernel(RowArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T), WAVES = TPR / 64, STEP = TPR * E;
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * (TPR < 256 ? 256 / TPR : 1) + threadIdx.x / TPR;
+    const int64_t row = (int64_t)blockIdx.x * (rows_group(TPR) / TPR) + threadIdx.x / TPR;
     if (row >= p.M) return;  // TPR < 256: whole waves, and no barrier below
     const T *px = (const T *)p.x + row * p.ldx;
     const T *py = p.y ? (const T *)p.y + row * p.ldy : nullptr;
@@ -261,16 +265,14 @@ __global__ void __launch_bounds__(256) dequantize_i8_kernel(const int8_t *q, int
 
 // ---------------------------------------------------------------- launches
 
-constexpr int64_t kMostRows = 1 << 22;  // of one launch: a grid holds fewer than 2^32 work-items
-
 template <typename T, typename W, int MODE>
 int launch_rows(const RowArgs &a, hipStream_t s)
 {
     constexpr int E = 16 / (int)sizeof(T);
     const int chunks = (a.N + E - 1) / E;
 #define PK_ROWS(TPR, VPT)                                                                                           \
-    hipLaunchKernelGGL((rows_i8_kernel<T, W, MODE, TPR, VPT>), dim3((unsigned)(TPR < 256 ? (a.M + 3) / 4 : a.M)),     \
-                       dim3(TPR < 256 ? 256 : TPR), 0, s, a)
+    hipLaunchKernelGGL((rows_i8_kernel<T, W, MODE, TPR, VPT>), dim3((unsigned)rows_groups(a.M, TPR)),                  \
+                       dim3(rows_group(TPR)), 0, s, a)
     // The fewest registers that hold a row.  Many rows: the fewest work-items that
     // do, a wave for a short row (bf16 norm, 16384 x 2048: one wave 39.5 us, four
     // 41.7; 8192 x 4096: four waves 39.0, eight 40.9), until the values of a row
@@ -340,15 +342,16 @@ int launch_dequantize(const int8_t *q, int64_t ldq, const float *scale, void *x,
     }
     const int M = (int)rows;
     if (N <= 64 * E) {
-        hipLaunchKernelGGL((dequantize_i8_kernel<T, 64>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, s, q, ldq, scale,
-                           (T *)x, ldx, M, N, N);
+        hipLaunchKernelGGL((dequantize_i8_kernel<T, 64>), dim3((unsigned)rows_groups(M, 64)), dim3(256), 0, s, q, ldq,
+                           scale, (T *)x, ldx, M, N, N);
     } else {
         // a work-item's share is four chunks, so that their loads are in flight
         // together (more where the grid's second dimension would not hold them)
         constexpr int SHARE = 4 * 256 * E;
         const int span = (N / SHARE / 32768 + 1) * SHARE;
-        hipLaunchKernelGGL((dequantize_i8_kernel<T, 256>), dim3((unsigned)M, (unsigned)((N - 1) / span + 1)), dim3(256),
-                           0, s, q, ldq, scale, (T *)x, ldx, M, N, span);
+        hipLaunchKernelGGL((dequantize_i8_kernel<T, 256>),
+                           dim3((unsigned)rows_groups(M, 256), (unsigned)((N - 1) / span + 1)), dim3(256), 0, s, q, ldq,
+                           scale, (T *)x, ldx, M, N, span);
     }
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
