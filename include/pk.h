@@ -344,8 +344,9 @@ int pk_quantize_i8(const void *x, int dtype, int64_t M, int64_t N, int64_t ldx,
  * The factor 1 / sqrt(...) is common to a row and goes into its scale alone:
  * q = rint(z * (127 / a)) for z = h * weight and a = max |z|, scale =
  * a / sqrt(...) / 127; the rules for zeros, infinities and NaN are applied to
- * z.  The mean is taken in fp32: rows whose sum of squares passes its range
- * have scale 0.
+ * z, in fp32: a product h * weight above its range is an infinity.  So is the
+ * mean's sum of squares, and such a row has scale 0 (|h| of 1e18 and more).
+ * Below its range the sum loses nothing, with any eps.
  *   residual      M x N or NULL.
  *   weight        N elements of weight_dtype, which is `dtype` or PK_F32.
  *   eps           >= 0.
