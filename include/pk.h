@@ -359,7 +359,8 @@ int pk_rmsnorm_i8(const void *x, int dtype, int64_t M, int64_t N, int64_t ldx,
                   void *stream);
 
 /*
- * Gated activation to 8 bits: rows of act(gate) * up, computed in fp32.
+ * Gated activation to 8 bits: rows of act(gate) * up, computed in fp32 (the
+ * activation down to its least subnormal).
  *   PK_ACT_SILU   act(g) = g / (1 + exp(-g))
  *   PK_ACT_GELU   act(g) = g / 2 * (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)))
  * gate and up are M x N; the two halves of one M x 2N product are two views of

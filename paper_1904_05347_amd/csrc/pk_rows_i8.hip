@@ -45,15 +45,20 @@ struct RowArgs {
     float eps;
 };
 
-// g / (1 + exp(-t)) with t = g (silu) or twice the argument of gelu's tanh,
-// 2 sqrt(2 / pi) (g + 0.044715 g^3): 1 / 2 (1 + tanh u) is 1 / (1 + exp(-2 u)).
-// The exponential and the reciprocal are the hardware's, within a unit in the
-// last place each; log2(e) is in the constants.
-__device__ __forceinline__ float activate(float g, int act)
+// act(g) = g q / (1 + q): q = exp(g) (silu) or exp of twice the argument of gelu's
+// tanh, 2 sqrt(2 / pi) (g + 0.044715 g^3): 1 / 2 (1 + tanh u) is
+// exp(2 u) / (1 + exp(2 u)).  q is made as h^2, h = 2^s, and the factors are
+// multiplied one by one, so that nothing before the result leaves the 32 bits'
+// range: the activation falls to the least subnormal as its formula does.  From
+// 2^60 on q / (1 + q) is 1.  The exponential and the reciprocal are the hardware's,
+// within a unit in the last place each; log2(e) / 2 is in the constants.
+template <int ACT>
+__device__ __forceinline__ float activate(float g)
 {
     constexpr float log2e = 1.4426950408889634f, c = 1.5957691216057308f * 1.4426950408889634f;
-    const float t = act == PK_ACT_SILU ? -log2e * g : g * fmaf(-0.044715f * c, g * g, -c);
-    return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t));
+    const float s = fminf(ACT == PK_ACT_SILU ? 0.5f * log2e * g : g * fmaf(0.5f * 0.044715f * c, g * g, 0.5f * c), 30.f);
+    const float h = __builtin_amdgcn_exp2f(s);
+    return g * __builtin_amdgcn_rcpf(fmaf(h, h, 1.f)) * h * h;
 }
 
 // v of every lane combined by op, in every lane; `none` leaves v as it is.
@@ -103,10 +108,16 @@ struct Chunk {
     // z of these elements; NORM: h replaces x
     __device__ __forceinline__ void values(bool added, int act, float *z)
     {
+        if (MODE == GATED && act == PK_ACT_SILU) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) z[j] = activate<PK_ACT_SILU>((float)x[j]) * (float)y[j];
+        } else if (MODE == GATED) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) z[j] = activate<PK_ACT_GELU>((float)x[j]) * (float)y[j];
+        }
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             if (MODE == PLAIN) z[j] = (float)x[j];
-            if (MODE == GATED) z[j] = activate((float)x[j], act) * (float)y[j];
             if (MODE == NORM) {
                 if (added) x[j] = (T)((float)x[j] + (float)y[j]);
                 z[j] = (float)x[j] * (float)w[j];
@@ -132,12 +143,16 @@ __device__ __forceinline__ void put(T *p, int e, int N, const typename Pack<T>::
 // number and NaN above infinity, so a NaN is not lost in the maximum.
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// q as the lowest byte of z * inv + 1.5 2^23, whose units are integers: the
+// addition rounds to the nearest, ties to even.
 template <int E>
 __device__ __forceinline__ void quantized(int8_t *q, int e, int N, const float *z, float inv)
 {
-    typename Pack<int8_t, E>::V v;
+    typename Pack<int8_t, E>::V v = (typename Pack<int8_t, E>::V)(int8_t)0;
+    if (inv != 0.f) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) v[j] = inv != 0.f ? (int8_t)(int)rintf(z[j] * inv) : (int8_t)0;
+        for (int j = 0; j < E; ++j) v[j] = (int8_t)__float_as_uint(z[j] * inv + 0x1.8p23f);
+    }
     if (e + E <= N) {
         *reinterpret_cast<typename Pack<int8_t, E>::U *>(q + e) = v;
         return;

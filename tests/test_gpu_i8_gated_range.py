@@ -1,0 +1,75 @@
+"""The gated activation where 1 + exp(-t) leaves the 32 bits' range or its reciprocal
+does: gates far below zero, whose small activation a large `up` brings back."""
+import numpy as np
+import pytest
+
+from tests import i8_plain as plain
+from tests.gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+def _f64(t):
+    import torch
+    torch.cuda.synchronize()
+    return t.detach().double().cpu().numpy()
+
+
+def _want(gate, up, name):
+    """gated_rows' bounds, and the rounding of an activation below the normal
+    numbers: half of 2^-149."""
+    a, t = plain.act(gate, name)
+    with np.errstate(all="ignore"):
+        small = np.where(a != 0, 2.0 ** -150 / np.abs(a), 0.0)
+    return plain.rows(a * up, rel=(7 + 6 * np.minimum(np.abs(t), 200.0)) * plain.U32 + np.minimum(small, 1.0))
+
+
+@pytest.mark.parametrize("act,lo,hi", [("silu", -103.0, -80.0), ("gelu", -11.2, -9.0)])
+@pytest.mark.parametrize("up", [3.0, -2e10, 1e30, -3e37])
+def test_a_gate_a_row(act, lo, hi, up):
+    torch, pk = require_gpu()
+    gate = torch.linspace(lo, hi, 693, device="cuda")[:, None]
+    ups = torch.full_like(gate, up)
+    q, s = pk.gated_i8(gate, ups, activation=act)
+    want = _want(_f64(gate), _f64(ups), act)
+    if up == 3.0:   # rows that end up beside the least scale are either way
+        clear = np.abs(np.abs(plain.act(_f64(gate), act)[0][:, 0] * up) / plain.LEAST - 1) > 1e-3
+        q, s, want = q[torch.from_numpy(clear).cuda()], s[torch.from_numpy(clear).cuda()], tuple(w[clear] for w in want)
+    plain.check_rows(_f64(q), _f64(s), want, (act, up))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_beyond_every_number(act):
+    """Activations that round to zero, and infinite gates: zero times infinity below, infinity above."""
+    torch, pk = require_gpu()
+    inf = float("inf")
+    g = torch.tensor([-150.0, -1e3, -1e5, -1e10, -1e19, -1e25, -3.4e38], device="cuda")[:, None]
+    q, s = pk.gated_i8(g, torch.full_like(g, 3e38), activation=act)
+    assert (q == 0).all() and (s == 0).all()
+    g = torch.tensor([90.0, 1e3, 1e10, 1e25, 3e38], device="cuda")[:, None]
+    q, s = pk.gated_i8(g, torch.ones_like(g), activation=act)
+    plain.check_rows(_f64(q), _f64(s), plain.rows(_f64(g)), act)
+    g = torch.tensor([inf, -inf, float("nan")], device="cuda")[:, None]
+    q, s = pk.gated_i8(g, torch.ones_like(g), activation=act)
+    assert (q == 0).all() and s[0] == inf and torch.isnan(s[1:]).all()
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("M,N", [(3, 7), (4, 512), (3, 1030), (2, 4097), (3, 16390), (1, 70001), (1101, 1500)])
+def test_among_ordinary_gates(M, N, kind):
+    """A few gates far below zero in rows of ordinary ones, whose `up` makes them count."""
+    torch, pk = require_gpu()
+    T = getattr(torch, kind)
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    big = 6e4 if kind == "float16" else 1e30
+    for act, far in (("silu", -92.0), ("gelu", -10.9)):
+        gate = torch.randn((M, N), generator=g, device="cuda") - 4
+        up = torch.randn((M, N), generator=g, device="cuda")
+        there = torch.rand((M, N), generator=g, device="cuda") < 0.01
+        there[:, N // 2] = True
+        gate = torch.where(there, far + gate, gate)
+        # the ordinary ones at the size of the others
+        up = torch.where(there, up.sign() * big, up * (1e-6 if kind == "float16" else 1e-9))
+        gate, up = gate.to(T), up.to(T)
+        q, s = pk.gated_i8(gate, up, activation=act)
+        plain.check_rows(_f64(q), _f64(s), _want(_f64(gate), _f64(up), act), (M, N, kind, act))
