@@ -50,15 +50,30 @@ struct RowArgs {
 // exp(2 u) / (1 + exp(2 u)).  q is made as h^2, h = 2^s, and the factors are
 // multiplied one by one, so that nothing before the result leaves the 32 bits'
 // range: the activation falls to the least subnormal as its formula does.  From
-// 2^60 on q / (1 + q) is 1.  The exponential and the reciprocal are the hardware's,
-// within a unit in the last place each; log2(e) / 2 is in the constants.
+// 2^57 on q / (1 + q) is 1.  The exponential and the reciprocal are the hardware's,
+// within a unit in the last place each.
+//   silu: s = g log2(e) / 2 is rounded, by up to |s| / 2 units of exp's result
+// (65 half units of the activation at -83); what the rounding left out goes into
+// one of the factors, exp(g - 2 ln(2) s) = 1 + that (at most 4 half units).
+//   gelu: the polynomial's own rounding is of that size and stays: fp32 has the
+// cube to three roundings, whatever is done with it.
 template <int ACT>
 __device__ __forceinline__ float activate(float g)
 {
-    constexpr float log2e = 1.4426950408889634f, c = 1.5957691216057308f * 1.4426950408889634f;
-    const float s = fminf(ACT == PK_ACT_SILU ? 0.5f * log2e * g : g * fmaf(0.5f * 0.044715f * c, g * g, 0.5f * c), 30.f);
-    const float h = __builtin_amdgcn_exp2f(s);
-    return g * __builtin_amdgcn_rcpf(fmaf(h, h, 1.f)) * h * h;
+    if constexpr (ACT == PK_ACT_SILU) {
+        const float most = fminf(g, 40.f), s = 0.72134752f * most;
+        // 2 ln(2) in two parts, the first rounded to fp32
+        constexpr double two_ln2 = 1.3862943611198906;
+        constexpr float hi = (float)two_ln2, lo = (float)(two_ln2 - (double)hi);
+        const float left = fmaf(s, -lo, fmaf(s, -hi, most));
+        const float h = __builtin_amdgcn_exp2f(s), k = fmaf(h, left, h);
+        return g * __builtin_amdgcn_rcpf(fmaf(h, k, 1.f)) * h * k;
+    } else {
+        // log2(e) / 2 is in the constants
+        constexpr float c = 0.5f * 1.5957691216057308f * 1.4426950408889634f;
+        const float h = __builtin_amdgcn_exp2f(fminf(g * fmaf(0.044715f * c, g * g, c), 30.f));
+        return g * __builtin_amdgcn_rcpf(fmaf(h, h, 1.f)) * h * h;
+    }
 }
 
 // v of every lane combined by op, in every lane; `none` leaves v as it is.

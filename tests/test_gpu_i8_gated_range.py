@@ -73,3 +73,20 @@ def test_among_ordinary_gates(M, N, kind):
         gate, up = gate.to(T), up.to(T)
         q, s = pk.gated_i8(gate, up, activation=act)
         plain.check_rows(_f64(q), _f64(s), _want(_f64(gate), _f64(up), act), (M, N, kind, act))
+
+
+@pytest.mark.parametrize("up", [1.0, -1e30])
+def test_silu_holds_its_last_bits(up):
+    """However far below zero the gate is, SiLU is within 12 half units: the two
+    factors of the exponential have 2 and 3, 1 + q, the reciprocal and the three
+    products that make the activation 1, 2 and 3, and the product with `up` has 1."""
+    torch, pk = require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for lo, hi in ((-87.0, -40.0), (-40.0, -10.0), (-10.0, 0.0), (0.0, 90.0)):
+        gate = lo + (hi - lo) * torch.rand((4000, 1), generator=g, device="cuda")
+        if up == 1.0:
+            gate = gate.clamp(min=-80.0)   # above the least scale
+        ups = torch.full_like(gate, up)
+        q, s = pk.gated_i8(gate, ups)
+        z = plain.act(_f64(gate), "silu")[0] * _f64(ups)
+        plain.check_rows(_f64(q), _f64(s), plain.rows(z, rel=12 * plain.U32), (lo, hi, up))
