@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
     constexpr int THREADS = KG * NW * 64;
     constexpr int P = TN * (int)sizeof(T) < 4 ? TN : 4 / (int)sizeof(T);  // tiles of a 16-byte store
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM * WM * 16 == BM && TN * WN * 16 == BN, "whole copies");
-    static_assert(DMA ? (STAGES - 2) * L < 64 : STAGES == 2, "copies in flight are counted in six bits");
+    static_assert(DMA ? STAGES <= 4 && (STAGES - 2) * L < 64 : STAGES == 2, "copies in flight are counted in six bits");
     static_assert(BM <= 256 && BN <= 256, "offsets in a tile are 32-bit for leading dimensions up to kMostLd");
     static_assert((KG - 1) * BM * BN * 4 <= KG * STAGES * STAGE, "sums of the other groups fit the stages");
     __shared__ __attribute__((aligned(16))) int8_t lds_all[KG * STAGES * STAGE];
@@ -268,9 +268,7 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
     };
     // this wave's copies of all but the newest `later` blocks have landed
     auto landed = [&](int later) {
-        if (STAGES > 5 && later >= 4)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 5 ? 4 * L : 0) : "memory");
-        else if (STAGES > 3 && later >= 2)
+        if (STAGES > 3 && later >= 2)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 3 ? 2 * L : 0) : "memory");
         else if (STAGES > 2 && later >= 1)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STAGES > 2 ? L : 0) : "memory");
