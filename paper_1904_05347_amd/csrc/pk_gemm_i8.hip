@@ -172,15 +172,15 @@ struct Source {
     // `to`; zeros for off < 0.  Written out, because the compiler would wait for
     // every such copy before the next read of LDS, whichever stage that reads;
     // the kernel's own waits are at its barriers.  The compiler does not see what
-    // the copy has to keep from the instructions before it either: m0 is read one
-    // wait state after it is set, scalar operands five after a vector instruction
-    // that may have made them.  m0 has no other use here.
+    // the copy has to keep from the instructions before it either: m0, where `to` is
+    // passed, is read one wait state after it is set, scalar operands five after a
+    // vector instruction that may have made them.
     __device__ __forceinline__ void copy16(int8_t *to, int off, int k) const
     {
         const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+        asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                      :
-                     : "s"(at), "v"(off), "s"(rs), "s"(k)
+                     : "{m0}"(at), "v"(off), "s"(rs), "s"(k)
                      : "memory");
     }
 };
