@@ -20,7 +20,7 @@ struct Args {
     void *C;
     int64_t lda, ldb, ldc;
     int M, N, K;
-    bool beyond_cache;  // C is too large to be kept for its reader
+    bool beyond_cache;  // C is written past the last-level cache
 };
 
 // ------------------------------------------------------------ few rows of A
@@ -414,54 +414,65 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
             bias[q][e] = factors[BM + BN + nl + q * 16 * P + e];
         }
     typedef typename Pack<T, E>::V V;
-    auto store = [&](int m, int n, const V &v) {
-        if (m >= p.M) return;
-        T *c = (T *)p.C + (int64_t)m * p.ldc + n;
-        if (n + E <= p.N) {
-            if (p.beyond_cache)
-                __builtin_nontemporal_store(v, reinterpret_cast<typename Pack<T, E>::U *>(c));
-            else
-                *reinterpret_cast<typename Pack<T, E>::U *>(c) = v;
-        } else {
+    // all of the part's results, by stores of one kind
+    auto store_all = [&]<bool BEYOND_CACHE>() {
+        // the compiler would make one plain store of both kinds' branches
+        if (BEYOND_CACHE) asm volatile("");
+        auto store = [&](int m, int n, const V &v) {
+            if (m >= p.M) return;
+            T *c = (T *)p.C + (int64_t)m * p.ldc + n;
+            if (n + E <= p.N) {
+                if constexpr (BEYOND_CACHE)
+                    __builtin_nontemporal_store(v, reinterpret_cast<typename Pack<T, E>::U *>(c));
+                else
+                    *reinterpret_cast<typename Pack<T, E>::U *>(c) = v;
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (n + e < p.N) c[e] = v[e];
+                for (int e = 0; e < E; ++e)
+                    if (n + e < p.N) c[e] = v[e];
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < TM; ++u) {
+            const float sa = factors[ml + u * 16];
+            const int m = m0 + ml + u * 16, n = n0 + nl;
+            auto value = [&](int q) {
+                V v;
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = rounded<T>(fmaf((float)acc[u][q * P + e / 4][e % 4], sa * sb[q][e], bias[q][e]));
+                return v;
+            };
+            if constexpr (TN / P % 2 == 0 && sizeof(V) == 16) {
+                // Four lanes' stores are 64 neighbouring bytes.  Neighbouring lanes
+                // exchange halves, so that a store has eight lanes' 128 bytes, a
+                // memory line, of every other row.
+                const bool odd = i & 1;
+#pragma unroll
+                for (int q = 0; q < TN / P; q += 2) {
+                    const i32x4 lo = __builtin_bit_cast(i32x4, value(q)), hi = __builtin_bit_cast(i32x4, value(q + 1));
+                    i32x4 first, second;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int got = __builtin_amdgcn_update_dpp(0, odd ? lo[w] : hi[w], 0xb1, 0xf, 0xf, false);
+                        first[w] = odd ? got : lo[w];
+                        second[w] = odd ? hi[w] : got;
+                    }
+                    const int at = n + (q + odd) * 16 * P;
+                    store(m - odd, at, __builtin_bit_cast(V, first));
+                    store(m - odd + 1, at, __builtin_bit_cast(V, second));
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < TN / P; ++q) store(m, n + q * 16 * P, value(q));
+            }
         }
     };
-#pragma unroll
-    for (int u = 0; u < TM; ++u) {
-        const float sa = factors[ml + u * 16];
-        const int m = m0 + ml + u * 16, n = n0 + nl;
-        auto value = [&](int q) {
-            V v;
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = rounded<T>(fmaf((float)acc[u][q * P + e / 4][e % 4], sa * sb[q][e], bias[q][e]));
-            return v;
-        };
-        if constexpr (TN / P % 2 == 0 && sizeof(V) == 16) {
-            // Four lanes' stores are 64 neighbouring bytes.  Neighbouring lanes
-            // exchange halves, so that a store has eight lanes' 128 bytes, a
-            // memory line, of every other row.
-            const bool odd = i & 1;
-#pragma unroll
-            for (int q = 0; q < TN / P; q += 2) {
-                const i32x4 lo = __builtin_bit_cast(i32x4, value(q)), hi = __builtin_bit_cast(i32x4, value(q + 1));
-                i32x4 first, second;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int got = __builtin_amdgcn_update_dpp(0, odd ? lo[w] : hi[w], 0xb1, 0xf, 0xf, false);
-                    first[w] = odd ? got : lo[w];
-                    second[w] = odd ? hi[w] : got;
-                }
-                const int at = n + (q + odd) * 16 * P;
-                store(m - odd, at, __builtin_bit_cast(V, first));
-                store(m - odd + 1, at, __builtin_bit_cast(V, second));
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < TN / P; ++q) store(m, n + q * 16 * P, value(q));
-        }
-    }
+    // smaller tiles are for smaller results; the second form's registers made the
+    // compiler wait for all copies in the loop of some (256 x 4096 x 4096 13.2 us, 9.6)
+    if (BM * BN >= 128 * 128 && p.beyond_cache)
+        store_all.template operator()<true>();
+    else
+        store_all.template operator()<false>();
 }
 
 // ------------------------------------------------- rows laid out at memory lines
@@ -643,6 +654,21 @@ const Config *choose(const Args &a, float *us = nullptr)
     return best;
 }
 
+// Is C written past the last-level cache, of 256 MB?  Only whole memory lines can
+// be (parts of lines take twice as long: 4832 x 12370 x 536 to fp32, rows at
+// multiples of 8 bytes, 164 us, 77 through it), and only where C, of more than
+// 96 MB, would not stay there beside what this call and the ones around it read:
+// 8192 x 16384 x 1024 to bf16 143 us, 178 through it, and 209 and 239 with a reader
+// of C after it; 8192 x 8192 x 4096 to fp16 203 and 227; 8192^3 424 and 434.  Where
+// it would stay, through it is faster: 12288 x 4096 x 1024 to fp32 66 us, 73 past
+// it (with its reader 109 and 113).  The limit is fitted to 35 sizes.
+bool past_the_cache(int64_t M, int64_t N, int64_t K, const void *C, int size, int64_t ldc)
+{
+    if (((uintptr_t)C | (uintptr_t)(ldc * size)) % 128) return false;
+    const int64_t bytes = M * N * size;
+    return bytes > (int64_t)96 << 20 && bytes + 4 * K * (M + N) > (int64_t)280 << 20;
+}
+
 constexpr int64_t kMostLayout = (int64_t)1 << 30;  // bytes of workspace
 
 // Bytes of workspace for the rows of A, B or both laid out at memory lines, and
@@ -752,10 +778,7 @@ extern "C" int pk_gemm_i8_ws(int64_t M, int64_t N, int64_t K, const int8_t *A, i
             return api_invalid(11);
     }
     if (bias && overlap(sc, span(bias, 1, N, N, 4))) return api_invalid(11);
-    // Of the 256 MB that the last-level cache holds, C may take 96 beside A and B:
-    // a larger one is written past it (8192^3 to bf16 398 us, 407 through it;
-    // 4096 x 16384 x 4096 217 and 229; 8192 x 4096 x 1024, 67 MB, 42.4 and 40.1)
-    const bool beyond_cache = M * N * size > (int64_t)96 << 20;
+    const bool beyond_cache = past_the_cache(M, N, K, C, size, ldc);
     Args a = {A, B, a_scale, b_scale, bias, C, lda, ldb, ldc, (int)M, (int)N, (int)K, beyond_cache};
     hipStream_t s = (hipStream_t)stream;
     Layout p;
