@@ -528,6 +528,8 @@ def _check_cuda(t, what, dtype=None, like=None):
                         % (what, "a" if dtype is None else "a %s" % str(dtype).replace("torch.", "")))
     if like is not None and t.device != like.device:
         raise ValueError("%s must be on %s" % (what, like.device))
+    if t.is_neg():
+        raise ValueError("%s is a negative view: pass its resolve_neg()" % what)
 
 
 def _check_vector(t, n, what, dtype, like):

@@ -313,12 +313,13 @@ int dtype_code(at::ScalarType t)
 }
 
 // A plain strided tensor on a GPU, or NULL.  A transform's wrapper (torch.func)
-// has the type and answers of a plain tensor, but no storage.
+// has the type and answers of a plain tensor, but no storage; a negative view
+// (the imaginary part of a conjugate) has its values' negatives there.
 const at::Tensor *on_gpu(PyObject *o)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
+    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.is_neg() ? &t : nullptr;
 }
 
 // A plain matrix of float32, bfloat16 or float16, with its code and leading dimension.
