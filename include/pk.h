@@ -377,8 +377,9 @@ int pk_dequantize_i8(const int8_t *q, int64_t ldq, const float *scale, int64_t M
 /*
  * Product of 8-bit integers with a scale for each row of either side:
  *   C[m][n] = a_scale[m] * b_scale[n] * sum_k A[m][k] * B[n][k] + bias[n]
- * The sum is exact (32-bit integers); it is converted to fp32, scaled and added
- * to there, and rounded to `dtype` once.
+ * The sum is exact (32-bit integers); it is converted to fp32, multiplied by
+ * a_scale[m] * b_scale[n], which is formed first, and added to there, and rounded
+ * to `dtype` once.
  *   A, lda     M x K activations, lda >= max(1, K).     a_scale   M floats.
  *   B, ldb     N x K weights (a row is an output channel), ldb >= max(1, K).
  *   b_scale    N floats.      bias   N floats or NULL.

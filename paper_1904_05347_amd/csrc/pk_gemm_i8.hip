@@ -134,17 +134,21 @@ __global__ void __launch_bounds__(WAVES * 64) gemm_i8_rows_kernel(Args p)
 //
 // Where there are few tiles, KG groups of waves share K, each with stages of its
 // own, and add their sums through LDS: half the steps that follow one another
-// (32 x 4096 x 4096: 7.2 us in two groups of 32 x 32, 8.0 in one).
+// (32 x 4096 x 4096 in tiles of 32 x 32: 7.2 us in two groups, 8.0 in one; in tiles
+// of 16 x 16, four groups, 5.9).
 //
-// What bounds it.  256 x 256, 8192^3: 400 us, 2750 TOP/s: the matrix cores are busy
-// for two thirds of the time at the 1.9 GHz that the power leaves; the same loop
-// without the copies takes 330 us, with copies that stay in L2 377.  128 x 128 and
-// less: the 64 bytes a clock that a CU reads (4096 x 4096 weights: 1024 rows 20.8 us,
-// 512 13.8, 256 10.1), then the latency of a launch, the first block and the
-// stores (32 rows 5.9 us).  128 bytes of a row that start inside a memory line are
-// two lines: operands whose rows start at multiples of 16 bytes but not of 128
-// take up to 1.3 times as long, those at odd addresses twice (4096^3 114 us, 57):
-// with a workspace larger products copy such rows to whole lines first.
+// What bounds it.  256 x 256, 8192^3: 417 to 435 us from run to run, 2530 to 2640
+// TOP/s: the matrix cores are busy for two thirds of the time at the 1.9 GHz that the
+// power leaves; the same loop without the copies takes 330 us, with copies that stay
+// in L2 377.  128 x 128 and less (4096 x 4096 weights: 1024 rows 19.7 us, 512 13.4,
+// 256 9.5): the copies' arrival.  A CU reads 70 to 85 GB/s while it goes through K,
+// four fifths of it from L2, from which alone it reads 152 (105 to 110 from the
+// last-level cache); half of the waves' cycles are waits, and the matrix cores are
+// busy for 10 to 26 % of the time.  Fewer rows: the latency of a launch, the first
+// block and the stores (32 rows 5.9 us).  128 bytes of a row that start inside a
+// memory line are two lines: operands whose rows start at multiples of 16 bytes but
+// not of 128 take up to 1.3 times as long, those at odd addresses twice (4096^3 114
+// us, 53): with a workspace larger products copy such rows to whole lines first.
 
 // Which row of the wave's 16 TN rows of B element `i` of its tile `t` is: the
 // accumulators of P tiles, 4 P in a lane, are neighbours in a row of C (P such
@@ -483,8 +487,8 @@ __global__ void __launch_bounds__(KG * WM * WN * 64, 2)
 // past the cache 5 % of the product longer: its reader finds the rest there).
 // The last 16 bytes of a row are filled up with zeros.  Bound by memory: 2330 +
 // 5318 rows of 6724 bytes 17 us, 6.0 TB/s read and written, some of it in cache;
-// a few MB take a launch and its latency, 3 to 6 us.  4096^3 of odd rows: 70 us,
-// 114 as they lie.
+// a few MB take a launch and its latency, 3 to 6 us.  4096^3 of odd rows: 64 to 70
+// us, 114 as they lie.
 struct Rows {
     const int8_t *from;
     int64_t ld;

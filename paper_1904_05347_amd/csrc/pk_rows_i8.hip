@@ -12,10 +12,11 @@
 // The row's values stay in registers between the reduction and the rounding, so
 // every input is read once and every output written once; a row too long for
 // that has what is beyond read (and computed) twice.  Bound by memory: the norm of
-// 8192 x 4096 bf16 with a residual moves 235 MB in 40 us (5.9 TB/s; a plain copy
+// 8192 x 4096 bf16 with a residual moves 235 MB in 39 us (6.0 TB/s; a plain copy
 // reaches 5.0), the gated activation of 8192 x 8192 336 MB in 54 us, fp32 rows of
 // that 336 MB in 57 us; a few rows by the latency of a launch and of memory (one
-// row of 4096: 2.6 us).
+// row of 4096: 2.6 us).  Gated rows that the registers do not hold are computed
+// twice: 2048 x 53248 bf16, 545 MB in 143 us (3.8 TB/s).
 #include "pk_i8.hpp"
 #include "pk_i8_checks.hpp"
 #include "pk_rows_i8_launch.hpp"
