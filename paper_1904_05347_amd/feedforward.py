@@ -75,14 +75,15 @@ def main(argv=None):
         with torch.cuda.graph(graph):
             layer(x, r)
         start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        for _ in range(10):
+        # until times are steady: the first of a run would come out a fifth too long
+        for _ in range(500):
             graph.replay()
         start.record()
-        for _ in range(20):
+        for _ in range(100):
             graph.replay()
         end.record()
         torch.cuda.synchronize()
-        us = start.elapsed_time(end) / 20 * 1e3
+        us = start.elapsed_time(end) / 100 * 1e3
         print("%5d tokens, %d -> 2 x %d -> %d: %8.1f us, %7.1f TOP/s, %.3g off float64"
               % (tokens, a.dim, a.width, a.dim, us, 6e-6 * tokens * a.dim * a.width / us, off), flush=True)
 
