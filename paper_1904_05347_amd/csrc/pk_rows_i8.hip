@@ -50,19 +50,21 @@ struct RowArgs {
 // tanh, 2 sqrt(2 / pi) (g + 0.044715 g^3): 1 / 2 (1 + tanh u) is
 // exp(2 u) / (1 + exp(2 u)).  q is made as h^2, h = 2^s, and the factors are
 // multiplied one by one, so that nothing before the result leaves the 32 bits'
-// range: the activation falls to the least subnormal as its formula does.  From
-// 2^57 on q / (1 + q) is 1.  The exponential and the reciprocal are the hardware's,
-// within a unit in the last place each.
+// range: the activation falls to the least subnormal as its formula does.  Where
+// q / (1 + q) is 1, q is held at a power of two, so that the factors change no bit
+// of g: 2^60, and 2^28 (silu: at 28 ln(2) s is 14 and nothing is left).  The
+// exponential and the reciprocal are the hardware's, within a unit in the last
+// place each.
 //   silu: s = g log2(e) / 2 is rounded, by up to |s| / 2 units of exp's result
 // (65 half units of the activation at -83); what the rounding left out goes into
-// one of the factors, exp(g - 2 ln(2) s) = 1 + that (at most 4 half units).
+// one of the factors, exp(g - 2 ln(2) s) = 1 + that (6 half units of the activation).
 //   gelu: the polynomial's own rounding is of that size and stays: fp32 has the
 // cube to three roundings, whatever is done with it.
 template <int ACT>
 __device__ __forceinline__ float activate(float g)
 {
     if constexpr (ACT == PK_ACT_SILU) {
-        const float most = fminf(g, 40.f), s = 0.72134752f * most;
+        const float most = fminf(g, 0x1.3687aap+4f), s = 0.72134752f * most;
         // 2 ln(2) in two parts, the first rounded to fp32
         constexpr double two_ln2 = 1.3862943611198906;
         constexpr float hi = (float)two_ln2, lo = (float)(two_ln2 - (double)hi);

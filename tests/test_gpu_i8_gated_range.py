@@ -90,3 +90,17 @@ def test_silu_holds_its_last_bits(up):
         q, s = pk.gated_i8(gate, ups)
         z = plain.act(_f64(gate), "silu")[0] * _f64(ups)
         plain.check_rows(_f64(q), _f64(s), plain.rows(z, rel=12 * plain.U32), (lo, hi, up))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_large_gates_are_their_own_activation(act):
+    """Where q / (1 + q) rounds to 1 no bit of the gate changes, up to the largest number."""
+    torch, pk = require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    size = torch.rand((3000, 1), generator=g, device="cuda") * 36 + 2   # 10^2 to 10^38
+    gate = torch.cat([10.0 ** size, 20 + 80 * torch.rand((1000, 1), generator=g, device="cuda"),
+                      torch.full((1, 1), torch.finfo(torch.float32).max, device="cuda")])
+    gate = gate[torch.isfinite(gate)][:, None]
+    q, s = pk.gated_i8(gate, torch.ones_like(gate), activation=act)
+    same, scale = pk.quantize_i8(gate)
+    assert torch.equal(q, same) and torch.equal(s, scale) and torch.isfinite(s).all()
