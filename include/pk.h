@@ -14,7 +14,7 @@
  *
  * Conventions shared by every call:
  *   - Every tensor pointer is a DEVICE pointer, to fp32 data except in the
- *     8-bit operators.  The caller owns all memory; the library allocates no device memory and keeps no pointer
+ *     8-bit and the attention operators.  The caller owns all memory; the library allocates no device memory and keeps no pointer
  *     after a call returns.
  *   - Storage is row-major (C order).  A column-major caller maps onto the
  *     same call by swapping the operands: the column-major product
@@ -415,6 +415,153 @@ int pk_gemm_i8_ws(int64_t M, int64_t N, int64_t K, const int8_t *A, int64_t lda,
                   const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
                   void *C, int dtype, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Attention operators: what a network does with its queries, keys and values
+ * between the products of an attention layer, for PK_F32, PK_BF16 and PK_F16.
+ *
+ * Conventions beside the common ones: strides are in elements and may be any
+ * that are not negative; the channels of a head are contiguous; elements need
+ * their own type's alignment and no more (heads that start at multiples of 16
+ * bytes are read fastest).  An output's elements must all be distinct; it may
+ * be an input's memory where that is said.  Sizes and strides up to 2^30, heads up
+ * to 2^16, a cache's strides up to 2^40 (else PK_ERR_NOT_SUPPORTED); a cache as
+ * large as memory holds.  What the arrays of indices hold is not known to the call: an
+ * index that is out of range leaves out what it points to, as said for each,
+ * and nothing outside the tensors is read or written.
+ * Results are deterministic.
+ */
+
+/* Heads of M tokens: channel c of head h of token m at
+ * data[m * token_stride + h * head_stride + c]. */
+typedef struct {
+    void *data;
+    int64_t heads, token_stride, head_stride;
+} pk_heads;
+
+/* A paged cache of keys and values: channel c of head h at position i of page p
+ * at key[p * key_stride[0] + i * key_stride[1] + h * key_stride[2] + c]. */
+typedef struct {
+    void *key, *value;
+    int64_t pages, page_size, heads;
+    int64_t key_stride[3], value_stride[3];
+} pk_cache;
+
+/*
+ * Rotation of the first 2 * pairs channels of a head by its token's position:
+ * pair i, of channels (i, i + pairs), or (2i, 2i + 1) where interleaved, becomes
+ *   (a cos t - b sin t, b cos t + a sin t) * amplitude,  t = position * frequencies[i]
+ * and the other channels stay.  t is formed in 64 bits and reduced there:
+ * positions up to 2^40 lose nothing that 32 bits hold.  Contexts longer than a
+ * network was trained for are a matter of the frequencies and the amplitude.
+ */
+typedef struct {
+    const int64_t *positions;   /* M, on the device */
+    const double *frequencies;  /* `pairs`, on the device: radians a position */
+    int64_t pairs;
+    int interleaved;
+    float amplitude;
+} pk_rotation;
+
+/*
+ * Norm of each head and rotation, for queries and keys in one launch:
+ *   y = rotation(x * weight / sqrt(mean(x^2) + eps)), rounded once.
+ *   head_size     channels of a head, 1 <= head_size <= 256 (else PK_ERR_NOT_SUPPORTED).
+ *   q, k          either may be NULL (then its output and weight must be, too).
+ *   rotation      NULL: none.
+ *   q_weight, k_weight   head_size elements of weight_dtype, which is `dtype`
+ *                 or PK_F32; NULL: that side has no norm.
+ *   eps           >= 0.  The mean neither overflows nor underflows.
+ *   q_out, k_out  as many heads; an output may be its own input (same strides).
+ */
+int pk_rope_qk(int dtype, int64_t M, int64_t head_size, const pk_heads *q, const pk_heads *k,
+               const pk_rotation *rotation, const void *q_weight, const void *k_weight, int weight_dtype,
+               float eps, const pk_heads *q_out, const pk_heads *k_out, void *stream);
+
+/*
+ * Its gradients.  dq and dk are those of the outputs; q and k the inputs of the
+ * forward call, read only where there is a weight (else they may be NULL).  With
+ * g the gradient rotated back and n = 1 / sqrt(mean(x^2) + eps),
+ *   q_grad = n (g w) - x n^3 mean(g w x),   q_weight_grad = sum g x n over tokens and heads
+ * (g alone, and no weight's gradient, without a weight), summed in fp32 and
+ * rounded once, to `dtype` and weight_dtype.  q_grad may be dq's memory (same
+ * strides), k_grad dk's.  A weight's gradient is written whole (zeros for M = 0).
+ *   workspace     REQUIRED where a weight is given: a 16-byte aligned device
+ *                 buffer of pk_rope_qk_backward_workspace_bytes() (else
+ *                 PK_ERR_WORKSPACE; misaligned PK_ERR_INVALID_VALUE at 17).
+ *                 Contents on return are unspecified.  Two calls that overlap
+ *                 in time must not share it.
+ */
+size_t pk_rope_qk_backward_workspace_bytes(int64_t M, int64_t head_size);
+int pk_rope_qk_backward(int dtype, int64_t M, int64_t head_size, const pk_heads *dq, const pk_heads *dk,
+                        const pk_heads *q, const pk_heads *k, const pk_rotation *rotation,
+                        const void *q_weight, const void *k_weight, int weight_dtype, float eps,
+                        const pk_heads *q_grad, const pk_heads *k_grad, void *q_weight_grad, void *k_weight_grad,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Keys and values of new tokens into a paged cache, in one launch with what
+ * pk_rope_qk does to keys and queries: token m's key, normed and rotated, and its
+ * value, as it is, go to position slots[m] % page_size of page slots[m] /
+ * page_size.  A token whose slot is negative, or beyond the cache, is left out (a
+ * batch's padding); its query is not.  Slots in the cache must be distinct.
+ * Everything else in the cache stays.
+ *   q, q_out      the tokens' queries, or NULL.  q_out may be q (same strides).
+ *   k, v          cache->heads heads each, in the cache's type.
+ */
+int pk_cache_append(int dtype, int64_t M, int64_t head_size, const pk_heads *q, const pk_heads *k,
+                    const pk_heads *v, const pk_rotation *rotation, const void *q_weight,
+                    const void *k_weight, int weight_dtype, float eps, const pk_heads *q_out,
+                    const pk_cache *cache, const int64_t *slots, void *stream);
+
+/*
+ * Attention of drafted tokens over a paged cache.  Sequence b has the tokens
+ * starts[b] <= m < starts[b + 1] (t of them, at most `most`; those beyond are left
+ * out), and lengths[b] positions in the cache before them.  The keys and values
+ * of its tokens are in the cache already, at the positions after those, in their
+ * order.  For each of its tokens m = starts[b] + i and each query head h
+ *   out = sum_j p_j value_j,  p the softmax of  c tanh(scale * (q . key_j) / c)
+ * (c = cap; of scale * (q . key_j) for cap = 0), over the positions j that i sees:
+ * all j < lengths[b], and lengths[b] + e for the bits e of mask[m] (e < t); without
+ * a mask for e <= i.  So a tree's token has the bits of its ancestors and its own;
+ * one token, or a chain, needs no mask.  Head h reads the cache's head
+ * h / (q heads / cache heads).
+ * A row that sees nothing, or scores of -infinity alone, is zero and its lse
+ * -infinity.  What a row does not see takes no part in it, whatever it holds (NaN
+ * and infinities in a cache's unused places).
+ *   head_size     1 <= head_size <= 256 (else PK_ERR_NOT_SUPPORTED).
+ *   q             M tokens; a multiple of the cache's heads.
+ *   page_table    B rows of P pages, ld_table apart: position j of sequence b is
+ *                 position j % page_size of page page_table[b][j / page_size].
+ *                 Pages that the cache does not have, and positions beyond the
+ *                 row, are not seen.
+ *   lengths       B; negative ones count as 0.
+ *   starts        B + 1, ascending, from 0 to M; tokens that are in no sequence
+ *                 keep what `out` and `lse` hold.
+ *   most          1 <= most <= 64 (else PK_ERR_NOT_SUPPORTED).
+ *   mask          M words, or NULL.
+ *   cap           >= 0.
+ *   out           as many heads as q, distinct from every input but q, whose memory
+ *                 it may be (same strides).
+ *   lse           the logarithm of each row's sum of exponentials, M x q heads, rows
+ *                 ld_lse apart, or NULL.
+ *   workspace     optional 16-byte aligned device buffer (else
+ *                 PK_ERR_INVALID_VALUE at 19); with at least
+ *                 pk_attention_tree_workspace_bytes() long sequences are divided
+ *                 over the card and what its parts found is joined in a fixed order.
+ *                 NULL or too small: a sequence's head is one work-group's.  It must
+ *                 not overlap another argument.  Contents on return are unspecified.
+ *                 Two calls that overlap in time must not share it.
+ * 16-bit operands are multiplied exactly and summed in fp32, as are the softmax's
+ * statistics; its weights are multiplied by the values in 16 bits (fp32: in 32).
+ */
+size_t pk_attention_tree_workspace_bytes(int dtype, int64_t head_size, int64_t q_heads, int64_t heads,
+                                         int64_t B, int64_t P, int64_t page_size, int64_t most);
+int pk_attention_tree(int dtype, int64_t M, int64_t head_size, const pk_heads *q, const pk_cache *cache,
+                      const int32_t *page_table, int64_t B, int64_t P, int64_t ld_table,
+                      const int32_t *lengths, const int32_t *starts, int64_t most, const uint64_t *mask,
+                      float scale, float cap, const pk_heads *out, float *lse, int64_t ld_lse,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *pk_status_string(int status);
 
@@ -423,8 +570,8 @@ int pk_last_invalid_param(void);
 
 /* Name of the compiled configuration this thread's last pk_sgemm or
  * pk_conv2d_fwd call ran ("" after an error or an empty problem, "scale" for
- * C <- beta * C); of the 8-bit operators, the operator's name, with the tile
- * that pk_gemm_i8 ran.  Static storage. */
+ * C <- beta * C); of the 8-bit and the attention operators, the operator's
+ * name, with the tile that pk_gemm_i8 or the form that pk_attention_tree ran.  Static storage. */
 const char *pk_last_config_name(void);
 
 /*

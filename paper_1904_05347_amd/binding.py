@@ -58,6 +58,23 @@ class TuneResult(ctypes.Structure):
                 ("candidates", ctypes.c_int)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", _p), ("heads", _i64), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("key", _p), ("value", _p), ("pages", _i64), ("page_size", _i64), ("heads", _i64),
+                ("key_stride", _i64 * 3), ("value_stride", _i64 * 3)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("positions", _p), ("frequencies", _p), ("pairs", _i64), ("interleaved", ctypes.c_int),
+                ("amplitude", ctypes.c_float)]
+
+
+_heads_p, _cache_p, _rotation_p = (ctypes.POINTER(c) for c in (Heads, Cache, Rotation))
+
+
 # Every symbol include/pk.h declares, with its ctypes signature.
 SIGNATURES = {
     "pk_sgemm": (ctypes.c_int, [ctypes.c_char, ctypes.c_char, _i64, _i64, _i64, ctypes.c_float, _p, _i64,
@@ -100,6 +117,18 @@ SIGNATURES = {
     "pk_gemm_i8_workspace_bytes_for": (ctypes.c_size_t, [_i64, _i64, _i64, _p, _i64, _p, _i64]),
     "pk_gemm_i8_ws": (ctypes.c_int, [_i64, _i64, _i64, _p, _i64, _p, _p, _i64, _p, _p, _p, ctypes.c_int, _i64,
                                      _p, ctypes.c_size_t, _p]),
+    "pk_rope_qk": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _heads_p, _heads_p, _rotation_p, _p, _p, ctypes.c_int,
+                                  ctypes.c_float, _heads_p, _heads_p, _p]),
+    "pk_rope_qk_backward_workspace_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "pk_rope_qk_backward": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _heads_p, _heads_p, _heads_p, _heads_p, _rotation_p,
+                                           _p, _p, ctypes.c_int, ctypes.c_float, _heads_p, _heads_p, _p, _p,
+                                           _p, ctypes.c_size_t, _p]),
+    "pk_cache_append": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _heads_p, _heads_p, _heads_p, _rotation_p, _p, _p,
+                                       ctypes.c_int, ctypes.c_float, _heads_p, _cache_p, _p, _p]),
+    "pk_attention_tree_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int] + [_i64] * 7),
+    "pk_attention_tree": (ctypes.c_int, [ctypes.c_int, _i64, _i64, _heads_p, _cache_p, _p, _i64, _i64, _i64, _p, _p, _i64,
+                                         _p, ctypes.c_float, ctypes.c_float, _heads_p, _p, _i64,
+                                         _p, ctypes.c_size_t, _p]),
     "pk_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "pk_last_invalid_param": (ctypes.c_int, []),
     "pk_last_config_name": (ctypes.c_char_p, []),
@@ -708,6 +737,267 @@ def gemm_i8(a, b, a_scale, b_scale, bias=None, dtype=None, out=None, workspace=N
                                 None if bias is None else bias.data_ptr(), out.data_ptr(), dt, ldc, ws_ptr, ws_bytes,
                                 _stream_handle(a)), "pk_gemm_i8_ws")
     return out
+
+
+# ------------------------------------------------------- attention operators
+
+LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def _check_heads(t, what, like=None, shape=None):
+    """A tensor of tokens x heads x channels whose channels are contiguous, and its pk_heads."""
+    _check_cuda(t, what, None if like is None else like.dtype, like)
+    if t.dim() != 3 or (t.size(2) > 1 and t.stride(2) != 1):
+        raise ValueError("%s must be tokens x heads x channels with contiguous channels" % what)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s" % (what, " x ".join(map(str, shape))))
+    return Heads(t.data_ptr(), t.size(1), t.stride(0), t.stride(1))
+
+
+def _check_indices(t, what, shape, dtype, like):
+    _check_cuda(t, what, dtype, like)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor of %s" % (what, " x ".join(map(str, shape))))
+
+
+def _check_cache(key_cache, value_cache, like, heads=None):
+    for t, what in ((key_cache, "key_cache"), (value_cache, "value_cache")):
+        _check_cuda(t, what, like.dtype, like)
+        if t.dim() != 4 or (t.size(3) > 1 and t.stride(3) != 1):
+            raise ValueError("%s must be pages x positions x heads x channels with contiguous channels" % what)
+        if t.size(3) != like.size(2) or (heads is not None and t.size(2) != heads):
+            raise ValueError("%s has other heads" % what)
+    if key_cache.shape != value_cache.shape:
+        raise ValueError("key_cache and value_cache must have the same shape")
+    return Cache(key_cache.data_ptr(), value_cache.data_ptr(), key_cache.size(0), key_cache.size(1), key_cache.size(2),
+                 (_i64 * 3)(*key_cache.stride()[:3]), (_i64 * 3)(*value_cache.stride()[:3]))
+
+
+def _rotation(positions, frequencies, layout, amplitude, M, d, like):
+    import torch
+    if layout not in LAYOUTS:
+        raise ValueError("layout must be 'half' or 'interleaved'")
+    if frequencies is None:
+        if positions is not None:
+            raise ValueError("positions need frequencies")
+        return None
+    if positions is None:
+        raise ValueError("frequencies need positions")
+    _check_cuda(frequencies, "frequencies", torch.float64, like)
+    _check_vector(frequencies, frequencies.numel(), "frequencies", torch.float64, like)
+    if 2 * frequencies.numel() > d:
+        raise ValueError("%d frequencies rotate more than the %d channels" % (frequencies.numel(), d))
+    _check_vector(positions, M, "positions", torch.int64, like)
+    return Rotation(positions.data_ptr(), frequencies.data_ptr(), frequencies.numel(), LAYOUTS[layout], float(amplitude))
+
+
+def _norm_weights(q_weight, k_weight, d, like):
+    """The weights' type code and addresses."""
+    import torch
+    given = [w for w in (q_weight, k_weight) if w is not None]
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is None:
+            continue
+        _check_cuda(w, what, None, like)
+        if w.dtype not in (like.dtype, torch.float32):
+            raise TypeError("%s must have the heads' type or float32" % what)
+        _check_vector(w, d, what, given[0].dtype, like)
+    code = _dtype_code(given[0].dtype, "weight") if given else 0
+    return code, None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr()
+
+
+def _new_heads(t):
+    import torch
+    return torch.empty(tuple(t.shape), dtype=t.dtype, device=t.device)
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def rope_frequencies(pairs, base=10000.0, factor=1.0, original=None, low=1.0, high=4.0, device="cuda"):
+    """Radians a position of each of ``pairs`` pairs, float64: base ** (-i / pairs),
+    as ``rope_qk`` and ``cache_append`` take them.
+
+    ``factor`` > 1 stretches them for contexts that many times as long as the network
+    was trained for: all of them (frequencies / factor), or, where ``original`` (the
+    positions of a training context) is given, by the turns that a pair makes in such
+    a context: those of at most ``low`` turns are stretched, those of ``high`` turns and
+    more stay, those between are blended linearly in their turns."""
+    import math
+
+    import torch
+    if pairs < 0 or not base > 0 or not factor > 0 or not high > low:
+        raise ValueError("pairs >= 0, base > 0, factor > 0 and high > low are needed")
+    f = base ** (-torch.arange(pairs, dtype=torch.float64) / max(pairs, 1))
+    if original is None:
+        f = f / factor
+    else:
+        kept = ((f * (original / (2 * math.pi)) - low) / (high - low)).clamp(0, 1)
+        f = f * (kept + (1 - kept) / factor)
+    return f.to(device)
+
+
+def rope_qk(q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6, layout="half", amplitude=1.0,
+            q_out=None, k_out=None):
+    """Norm of each head and rotation by its token's position: ``(q', k')`` (see pk_rope_qk).
+
+    ``q`` is tokens x heads x channels, ``k`` the same with heads of its own or None
+    (float32, bfloat16 or float16; views of one projection's output will do).
+    ``positions`` (int64) has one for each token, ``frequencies`` (float64, see
+    ``rope_frequencies``) one for each pair, or both are None: no rotation.
+    ``layout`` tells the pairs: 'half' (i, i + pairs) or 'interleaved' (2i, 2i + 1);
+    channels from 2 * pairs on stay as they are.  ``q_weight`` and ``k_weight`` (the
+    heads' type or float32) are the norms' weights, None for no norm; ``amplitude``
+    multiplies what is rotated.  ``q_out`` may be ``q`` and ``k_out`` ``k``."""
+    import torch  # noqa: F401
+    hq = _check_heads(q, "q")
+    dt = _dtype_code(q.dtype, "q")
+    M, _, d = q.shape
+    hk = None if k is None else _check_heads(k, "k", q, (M, k.size(1) if k.dim() == 3 else 0, d))
+    if k is None and (k_weight is not None or k_out is not None):
+        raise ValueError("k_weight and k_out need k")
+    rot = _rotation(positions, frequencies, layout, amplitude, M, d, q)
+    wt, qw, kw = _norm_weights(q_weight, k_weight, d, q)
+    q_out = _new_heads(q) if q_out is None else q_out
+    oq = _check_heads(q_out, "q_out", q, q.shape)
+    ok = None
+    if k is not None:
+        k_out = _new_heads(k) if k_out is None else k_out
+        ok = _check_heads(k_out, "k_out", q, k.shape)
+    _check(load().pk_rope_qk(dt, M, d, hq, _ref(hk), _ref(rot), qw, kw, wt, float(eps), oq, _ref(ok), _stream_handle(q)),
+           "pk_rope_qk")
+    return q_out, k_out
+
+
+def rope_qk_backward(dq, dk, q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6, layout="half",
+                     amplitude=1.0, q_grad=None, k_grad=None):
+    """Gradients of ``rope_qk``: ``(q_grad, k_grad, q_weight_grad, k_weight_grad)``
+    from those of its outputs, ``dq`` and ``dk`` (None where k was), and its inputs
+    (see pk_rope_qk_backward).  q or k may be None where its side has no weight;
+    the weights' gradients are None there.  ``q_grad`` may be ``dq`` and ``k_grad``
+    ``dk``."""
+    import torch
+    hdq = _check_heads(dq, "dq")
+    dt = _dtype_code(dq.dtype, "dq")
+    M, _, d = dq.shape
+    hdk = None if dk is None else _check_heads(dk, "dk", dq, (M, dk.size(1) if dk.dim() == 3 else 0, d))
+    if dk is None and (k_weight is not None or k_grad is not None):
+        raise ValueError("k_weight and k_grad need dk")
+    ins = []
+    for t, w, like, what in ((q, q_weight, dq, "q"), (k, k_weight, dk, "k")):
+        if w is not None and t is None:
+            raise ValueError("%s_weight needs %s" % (what, what))
+        ins.append(None if w is None else _check_heads(t, what, like, like.shape))
+    rot = _rotation(positions, frequencies, layout, amplitude, M, d, dq)
+    wt, qw, kw = _norm_weights(q_weight, k_weight, d, dq)
+    q_grad = _new_heads(dq) if q_grad is None else q_grad
+    gq, gk = _check_heads(q_grad, "q_grad", dq, dq.shape), None
+    if dk is not None:
+        k_grad = _new_heads(dk) if k_grad is None else k_grad
+        gk = _check_heads(k_grad, "k_grad", dq, dk.shape)
+    wgrads = [None if w is None else torch.empty_like(w, memory_format=torch.contiguous_format) for w in (q_weight, k_weight)]
+    ws, ws_bytes = None, 0
+    if qw or kw:
+        ws_bytes = load().pk_rope_qk_backward_workspace_bytes(M, d)
+        ws = torch.empty(ws_bytes // 4, dtype=torch.float32, device=dq.device)
+    _check(load().pk_rope_qk_backward(dt, M, d, hdq, _ref(hdk), _ref(ins[0]), _ref(ins[1]), _ref(rot), qw, kw, wt, float(eps),
+                                      gq, _ref(gk), *[None if w is None else w.data_ptr() for w in wgrads],
+                                      None if ws is None else ws.data_ptr(), ws_bytes, _stream_handle(dq)),
+           "pk_rope_qk_backward")
+    return q_grad, k_grad, wgrads[0], wgrads[1]
+
+
+def cache_append(k, v, key_cache, value_cache, slots, positions=None, frequencies=None, k_weight=None, q=None,
+                 q_weight=None, eps=1e-6, layout="half", amplitude=1.0, q_out=None):
+    """Keys and values of new tokens into a paged cache, the keys normed and rotated
+    as ``rope_qk`` does; the tokens' queries too, where given, which are returned
+    (see pk_cache_append).
+
+    ``key_cache`` and ``value_cache`` are pages x positions x heads x channels, any
+    strides (a permuted view, the halves of one tensor); ``slots`` (int64) has a page
+    times the positions of a page plus the position in it for each token, those that
+    are negative or beyond the cache are left out, and the others must be distinct."""
+    import torch
+    hk = _check_heads(k, "k")
+    dt = _dtype_code(k.dtype, "k")
+    M, Hk, d = k.shape
+    hv = _check_heads(v, "v", k, k.shape)
+    hq = None if q is None else _check_heads(q, "q", k, (M, q.size(1) if q.dim() == 3 else 0, d))
+    if q is None and (q_weight is not None or q_out is not None):
+        raise ValueError("q_weight and q_out need q")
+    cache = _check_cache(key_cache, value_cache, k, Hk)
+    _check_vector(slots, M, "slots", torch.int64, k)
+    rot = _rotation(positions, frequencies, layout, amplitude, M, d, k)
+    wt, qw, kw = _norm_weights(q_weight, k_weight, d, k)
+    oq = None
+    if q is not None:
+        q_out = _new_heads(q) if q_out is None else q_out
+        oq = _check_heads(q_out, "q_out", k, q.shape)
+    _check(load().pk_cache_append(dt, M, d, _ref(hq), hk, hv, _ref(rot), qw, kw, wt, float(eps), _ref(oq), cache,
+                                  slots.data_ptr(), _stream_handle(k)), "pk_cache_append")
+    return q_out
+
+
+def attention_tree(q, key_cache, value_cache, page_table, lengths, starts, most, mask=None, scale=None, cap=0.0, out=None,
+                   lse=False, workspace=None):
+    """Attention of drafted tokens over a paged cache (see pk_attention_tree): each
+    sequence's tokens (one, a chain or a tree) over the positions before them and over
+    each other, their keys and values being in the cache already.
+
+    ``q`` is tokens x heads x channels, the tokens of sequence b being starts[b] to
+    starts[b + 1] - 1; ``lengths[b]`` positions of the cache are before them.
+    ``page_table`` (sequences x pages), ``lengths`` and ``starts`` are int32; ``most``, at
+    most 64, bounds the tokens of a sequence.  ``mask`` (int64, a word for each token):
+    bit e set where the token sees its sequence's token e; None: each sees itself and
+    those before it.  ``scale`` is channels ** -0.5 when None; ``cap`` > 0 bounds the
+    scores by cap * tanh(score / cap).  ``lse``: True, or a float32 tensor of tokens x
+    heads, for ``(out, lse)``.  ``out`` may be ``q``; a new one holds nothing in the rows
+    of tokens that are in no sequence.  workspace (a float32 device tensor) lets long
+    sequences be divided over the card; when None, one of the size that the library
+    asks for is allocated."""
+    import torch
+    hq = _check_heads(q, "q")
+    dt = _dtype_code(q.dtype, "q")
+    M, Hq, d = q.shape
+    cache = _check_cache(key_cache, value_cache, q)
+    Hk = cache.heads
+    if Hk < 1 or Hq % Hk:
+        raise ValueError("q's heads must be a multiple of the cache's")
+    _check_cuda(page_table, "page_table", torch.int32, q)
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be sequences x pages")
+    ld_table = _ld_2d(page_table, "page_table")
+    B, P = page_table.shape
+    _check_vector(lengths, B, "lengths", torch.int32, q)
+    _check_vector(starts, B + 1, "starts", torch.int32, q)
+    if mask is not None:
+        _check_vector(mask, M, "mask", torch.int64, q)
+    scale = max(d, 1) ** -0.5 if scale is None else float(scale)
+    out = _new_heads(q) if out is None else out
+    ho = _check_heads(out, "out", q, q.shape)
+    want, ld_lse = lse is not None and lse is not False, 0
+    if want:
+        lse = torch.empty((M, Hq), dtype=torch.float32, device=q.device) if lse is True else lse
+        _check_cuda(lse, "lse", torch.float32, q)
+        if tuple(lse.shape) != (M, Hq):
+            raise ValueError("lse must be %d x %d" % (M, Hq))
+        ld_lse = _ld_2d(lse, "lse")
+    if workspace is None:
+        need = load().pk_attention_tree_workspace_bytes(dt, d, Hq, Hk, B, P, cache.page_size, int(most))
+        if need:
+            workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=q.device)
+    ws_ptr, ws_bytes = None, 0
+    if workspace is not None:
+        _check_cuda(workspace, "workspace", torch.float32, q)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * 4
+    _check(load().pk_attention_tree(dt, M, d, hq, cache, page_table.data_ptr(), B, P, ld_table, lengths.data_ptr(),
+                                    starts.data_ptr(), int(most), None if mask is None else mask.data_ptr(), scale, float(cap),
+                                    ho, lse.data_ptr() if want else None, ld_lse, ws_ptr, ws_bytes, _stream_handle(q)),
+           "pk_attention_tree")
+    return (out, lse) if want else out
 
 
 def _tune_dict(r):

@@ -1,0 +1,698 @@
+// pk_attention.hip -- attention of drafted tokens over a paged cache.
+//
+//   o_i = sum_j p_ij v_j,  p_i the softmax over the j that row i sees of
+//   x_ij = c tanh(scale (q_i . k_j) / c)   (scale (q_i . k_j) without a cap c).
+//
+// One pass over the cache: each wave takes 32 positions at a time and keeps, for
+// each of its rows, the largest x so far, the sum of exponentials and the sum of
+// values weighted by them.  All rows that read one head of the cache (its tokens
+// times the query heads that share it) are columns of one product, so that K and V
+// are read once for them.
+//
+// Lanes.  x^T = K q^T and o^T = V^T p^T on the 16 x 16 matrix instruction, whose
+// operands hold 8 neighbours along the sum a lane: K's and q's rows are read as
+// they lie, 16 bytes a lane.  In x^T a lane has one row's (lane % 16) x of four
+// neighbouring positions, from two products of eight: the second product's operand,
+// without any exchange, where V^T takes its positions in the same order.  V^T comes
+// out of LDS transposed.
+#include "pk_attention_plan.hpp"
+#include "pk_heads_checks.hpp"
+#include "pk_i8.hpp"
+#include "pk_i8_checks.hpp"
+
+namespace {
+
+using namespace pk::attention;
+using pk::bf16;
+using pk::f16;
+using pk::Pack;
+using pk::rounded;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;       // of a work-group
+constexpr int kTile = 32;       // positions that a wave has in work
+constexpr int kUnit = kWaves * kTile;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+struct Args {
+    const void *q;
+    void *out;
+    const void *key, *value;
+    const int32_t *table, *lengths, *starts;
+    const uint64_t *mask;
+    float *lse, *parts;
+    int64_t q_token, q_head, out_token, out_head, lse_token, table_row;
+    int64_t key_page, key_place, key_head, value_page, value_place, value_head;
+    int64_t pages;
+    Shape shape;
+    int B, d, page_size, page_shift;  // page_shift: of a power of two, else -1
+    float scale, cap;  // scores are formed in powers of two: scale * log2(e), or scale / cap and cap * log2(e)
+};
+
+template <typename T>
+struct Eight {
+    typedef T V __attribute__((ext_vector_type(8)));
+};
+
+// Eight elements from p on, those from n on zero.
+template <typename T>
+__device__ __forceinline__ typename Eight<T>::V get8(const T *p, int n)
+{
+    typedef typename Eight<T>::V V;
+    V v = (V)(T)0.f;
+    if (n >= 8) {
+        typedef V U __attribute__((aligned(sizeof(T))));
+        return *reinterpret_cast<const U *>(p);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) v[j] = p[j];
+    return v;
+}
+
+// c += a b^T for 16 x 32 operands: lane l holds row l % 16, elements 8 (l / 16) on.
+__device__ __forceinline__ f32x4 product(Eight<bf16>::V a, Eight<bf16>::V b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 product(Eight<f16>::V a, Eight<f16>::V b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// fp32 has products of 4: eight of them, one for each element of the lanes
+__device__ __forceinline__ f32x4 product(Eight<float>::V a, Eight<float>::V b, f32x4 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// A wave's 32 rows of V in LDS.  Rows are padded so that the lanes of one read of a
+// column tile start at different banks: 8 apart in 16 bits, 4 in 32.
+template <typename T, int D>
+struct Staged {
+    static constexpr int kPad = sizeof(T) == 2 ? 16 : 4;
+    static constexpr int kRow = D + kPad;
+    static constexpr int kBytes = kTile * kRow * (int)sizeof(T);
+
+    // channels 16 n + lane % 16 of positions 4 (lane / 16) + 0..3 and those + 16
+    static __device__ __forceinline__ typename Eight<T>::V column(const T *s, int n, int lane)
+    {
+        typename Eight<T>::V v;
+        if constexpr (sizeof(T) == 2) {
+            typedef short S4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) S4 *P;
+            const T *p = s + (lane / 4) * kRow + n * 16 + (lane % 4) * 4;
+            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
+            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * kRow));
+            const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            v = __builtin_bit_cast(typename Eight<T>::V, both);
+        } else {
+            const T *p = s + (lane / 16) * 4 * kRow + n * 16 + lane % 16;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = p[j * kRow];
+                v[4 + j] = p[(16 + j) * kRow];
+            }
+        }
+        return v;
+    }
+};
+
+// tanh, to 2 units in the last place.  The exponential's form would lose digits
+// below 0.6: there x (1 + x^2 P(x^2)), P a least-squares fit whose error is 2^-30 of
+// the result.
+__device__ __forceinline__ float tanh_of(float x)
+{
+    const float y = fabsf(x), z = x * x;
+    float p = fmaf(z, 0.00231141f, -0.00836057f);
+    p = fmaf(z, p, 0.02177406f);
+    p = fmaf(z, p, -0.0539599f);
+    p = fmaf(z, p, 0.13333306f);
+    p = fmaf(z, p, -0.33333333f);
+    const float e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));  // infinite far out: 1 - 0
+    const float far = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e), x);
+    return y < 0.6f ? fmaf(x * z, p, x) : far;
+}
+
+// ------------------------------------------------------------------ the line of units
+
+constexpr int kThreads = kWaves * 64;
+
+struct Line {
+    int64_t ends[kThreads];  // units up to the end of each work-item's sequences
+    int64_t base;            // of the sequence found
+    int b;
+    int64_t waves[kThreads / 64];
+};
+
+__device__ __forceinline__ Sequence sequence_of(const Args &p, int b)
+{
+    return sequence(p.shape, p.starts[b], p.starts[b + 1], p.lengths[b]);
+}
+
+// Units of the whole call.  Each work-item adds up its own run of sequences.
+__device__ __forceinline__ int64_t measure(const Args &p, Line &s)
+{
+    const int t = threadIdx.x, run = (p.B + kThreads - 1) / kThreads;
+    int64_t sum = 0;
+    for (int b = t * run; b < (t + 1) * run && b < p.B; ++b) sum += sequence_of(p, b).cost(p.shape.heads);
+    for (int o = 1; o < 64; o *= 2) {
+        const int64_t v = __shfl_up(sum, o);
+        if (t % 64 >= o) sum += v;
+    }
+    if (t % 64 == 63) s.waves[t / 64] = sum;
+    __syncthreads();
+    int64_t before = 0, total = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+        if (w < t / 64) before += s.waves[w];
+        total += s.waves[w];
+    }
+    s.ends[t] = before + sum;
+    __syncthreads();
+    return total;
+}
+
+// The sequence that has unit u < total, and the units before it.
+__device__ __forceinline__ void find(const Args &p, Line &s, int64_t u, int &b, int64_t &base)
+{
+    const int t = threadIdx.x, run = (p.B + kThreads - 1) / kThreads;
+    const int64_t before = t ? s.ends[t - 1] : 0;
+    if (u >= before && u < s.ends[t]) {
+        int64_t at = before;
+        int i = t * run;
+        for (;; ++i) {
+            const int64_t c = sequence_of(p, i).cost(p.shape.heads);
+            if (u < at + c) break;
+            at += c;
+        }
+        s.b = i;
+        s.base = at;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(s.b);
+    base = s.base;
+}
+
+// The work-group's number on the line: neighbours on it share an XCD's L2.
+__device__ __forceinline__ int64_t rank_of(int64_t block, int64_t active)
+{
+    const int64_t x = block % 8, extra = active % 8;
+    return x * (active / 8) + (x < extra ? x : extra) + block / 8;
+}
+
+// A part's place in the workspace: `rows` x D sums, then maxima and sums of exponentials.
+template <int D>
+__device__ __forceinline__ float *part_of(const Args &p, int64_t group, int slot)
+{
+    return p.parts + (group * 2 + slot) * ((int64_t)p.shape.rows * (D + 2));
+}
+
+// Row r of an item's group: its token and query head.
+struct RowAt {
+    int64_t m;
+    int h;
+};
+__device__ __forceinline__ RowAt row_at(const Args &p, const Sequence &q, int head, int r)
+{
+    const int t = r / p.shape.group;
+    return {q.first + t, head * p.shape.group + (r - t * p.shape.group)};
+}
+
+// Four channels of a finished row, and its lse.
+template <typename T>
+__device__ __forceinline__ void finish(const Args &p, const Sequence &q, int head, int r, int c, f32x4 o, float l, float most)
+{
+    const RowAt at = row_at(p, q, head, r);
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that saw nothing
+    T *to = (T *)p.out + at.m * p.out_token + at.h * p.out_head + c;
+    typename Pack<T, 4>::V v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = rounded<T>(o[j] * inv);
+    if (c + 4 <= p.d) {
+        *reinterpret_cast<typename Pack<T, 4>::U *>(to) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < p.d) to[j] = v[j];
+    }
+    if (c == 0 && p.lse)
+        p.lse[at.m * p.lse_token + at.h] = l == 0.f ? -__builtin_inff() : (most + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// exp2(m - most), 0 for a part that saw nothing
+__device__ __forceinline__ float weight_of(float m, float most)
+{
+    return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - most);
+}
+
+// ------------------------------------------------------------------ the attention
+
+// NQ groups of 16 rows; the waves divide the positions.
+template <typename T, int D, int NQ>
+__global__ void __launch_bounds__(kThreads) attention_kernel(Args p)
+{
+    typedef typename Eight<T>::V V8;
+    constexpr int C = D / 32, N = D / 16, ROWS = 16 * NQ;
+    constexpr int kSum = ROWS * (D + 4) * 4;  // a wave's sums
+    constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
+    extern __shared__ __align__(16) char s_raw[];  // kWaves * kWave: too much to be static for the widest heads
+    __shared__ Line s_line;
+    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+    T *s_v = reinterpret_cast<T *>(s_raw + wave * kWave);
+
+    const int64_t total = measure(p, s_line);
+    const int64_t each = share(total, gridDim.x), active = (total + each - 1) / each;
+    if ((int64_t)blockIdx.x >= active) return;
+    const int64_t rank = rank_of(blockIdx.x, active), share_begin = rank * each;
+    const int64_t share_end = share_begin + each < total ? share_begin + each : total;
+    int b;
+    int64_t base;
+    find(p, s_line, share_begin, b, base);
+    Sequence seq = sequence_of(p, b);
+
+    for (int64_t u = share_begin; u < share_end;) {
+        while (u >= base + seq.cost(p.shape.heads)) {
+            base += seq.cost(p.shape.heads);
+            seq = sequence_of(p, ++b);
+        }
+        const int64_t item = (u - base) / seq.units, item_begin = base + item * seq.units, part_begin = u;
+        const int64_t part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
+        const int head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * ROWS;
+        const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
+        const int begin = (int)((part_begin - item_begin) * p.shape.unit);
+        const int end = p.shape.unit && (part_end - item_begin) * p.shape.unit < seq.keys
+                            ? (int)((part_end - item_begin) * p.shape.unit) : (int)seq.keys;
+        const int length = (int)seq.length;
+        const T *key = (const T *)p.key + head * p.key_head, *value = (const T *)p.value + head * p.value_head;
+        const int32_t *table = p.table + b * p.table_row;
+
+        // the rows, and which of the sequence's tokens each sees
+        V8 q[NQ][C];
+        uint64_t word[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int r = n * 16 + col;
+            word[n] = 0;
+            const T *at = (const T *)p.q;
+            if (r < rows) {
+                const RowAt row = row_at(p, seq, head, row0 + r);
+                at += row.m * p.q_token + row.h * p.q_head;
+                word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) q[n][c] = get8(at + c * 32 + g * 8, r < rows ? p.d - c * 32 - g * 8 : 0);
+        }
+
+        f32x4 o[NQ][N];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            m[n] = -__builtin_inff();
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
+        }
+
+        // where positions at + col and at + 16 + col lie: their pages' numbers
+        auto page_at = [&](int j) {
+            int page = -1;
+            if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
+            return (unsigned)page < (uint64_t)p.pages ? page : -1;
+        };
+        auto place_in = [&](int j) {
+            return p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
+        };
+        V8 kk[2][C], vv[2][C];
+        auto fetch = [&](int at, const int *page) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int place = place_in(at + h * 16 + col);
+                const T *pk = key, *pv = value;
+                if (page[h] >= 0) {
+                    pk += page[h] * p.key_page + place * p.key_place;
+                    pv += page[h] * p.value_page + place * p.value_place;
+                }
+#pragma unroll
+                for (int c = 0; c < C; ++c) kk[h][c] = get8(pk + c * 32 + g * 8, page[h] >= 0 ? p.d - c * 32 - g * 8 : 0);
+#pragma unroll
+                for (int c = 0; c < C; ++c) vv[h][c] = get8(pv + c * 32 + g * 8, page[h] >= 0 ? p.d - c * 32 - g * 8 : 0);
+            }
+        };
+        int at = begin + wave * kTile;
+        int page[2] = {page_at(at + col), page_at(at + 16 + col)};
+        if (at < end) fetch(at, page);
+        int next[2] = {page_at(at + kUnit + col), page_at(at + kUnit + 16 + col)};
+
+        for (; at < end; at += kUnit) {
+            // positions that hold something
+            const unsigned there = (unsigned)(__ballot(page[0] >= 0) & 0xffff) | (unsigned)(__ballot(page[1] >= 0) & 0xffff) << 16;
+            f32x4 x[NQ][2];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    x[n][h] = (f32x4)0.f;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) x[n][h] = product(kk[h][c], q[n][c], x[n][h]);
+                }
+            // V to LDS; a token's NaN or infinity is told from here on
+            bool odd = false;
+            const bool drafted = at + kTile > length;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    *reinterpret_cast<V8 *>(s_v + (h * 16 + col) * Staged<T, D>::kRow + c * 32 + g * 8) = vv[h][c];
+                    if (drafted) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) odd |= !(fabsf((float)vv[h][c][j]) < __builtin_inff());
+                    }
+                }
+            odd = __any(odd);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            // the next tile on its way
+            page[0] = next[0];
+            page[1] = next[1];
+            if (at + kUnit < end) fetch(at + kUnit, page);
+            next[0] = page_at(at + 2 * kUnit + col);
+            next[1] = page_at(at + 2 * kUnit + 16 + col);
+
+            V8 weight[NQ];
+            unsigned seen[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                seen[n] = there;
+                if (drafted) {
+                    const int off = length - at;  // the tile's first token
+                    seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
+                }
+                float most = -__builtin_inff(), s[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[e] = x[n][e / 4][e % 4] * p.scale;
+                    if (p.cap != 0.f) s[e] = tanh_of(s[e]) * p.cap;
+                }
+                if (seen[n] != ~0u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) s[e] = -__builtin_inff();
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, s[e]);
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                most = fmaxf(most, m[n]);
+                const float origin = most == -__builtin_inff() ? 0.f : most;
+                const float shrink = __builtin_amdgcn_exp2f(m[n] - origin);
+                m[n] = most;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[e] = __builtin_amdgcn_exp2f(s[e] - origin);
+                    sum += s[e];
+                    weight[n][e] = (T)s[e];
+                }
+                l[n] = fmaf(l[n], shrink, sum);
+#pragma unroll
+                for (int i = 0; i < N; ++i) o[n][i] *= shrink;
+            }
+            if (!odd) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const V8 v = Staged<T, D>::column(s_v, i, lane);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][i] = product(v, weight[n], o[n][i]);
+                }
+            } else {
+                // a NaN or an infinity reaches the rows that see it and no other: position by position
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    for (int from = 0; from < 4; ++from) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int j = e / 4 * 16 + from * 4 + e % 4;
+                            const float w = __shfl((float)weight[n][e], from * 16 + col);
+#pragma unroll 1
+                            for (int c = 0; c < N * 4; ++c) {
+                                const float v = (float)s_v[j * Staged<T, D>::kRow + (c / 4) * 16 + g * 4 + c % 4];
+                                const float add = seen[n] >> j & 1 ? w * v : 0.f;
+#pragma unroll
+                                for (int i = 0; i < N * 4; ++i)
+                                    if (i == c) o[n][i / 4][i % 4] += add;
+                            }
+                        }
+                    }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+
+        // the waves' sums together
+        float *s_o = reinterpret_cast<float *>(s_raw + wave * kWave);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+            if (g == 0) {
+                s_m[wave][n * 16 + col] = m[n];
+                s_l[wave][n * 16 + col] = l[n];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = o[n][i];
+        }
+        __syncthreads();
+        const bool whole = part_begin == item_begin && part_end == item_begin + seq.units;
+        float *part = whole ? nullptr : part_of<D>(p, rank, slot_of(part_begin, share_begin));
+        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            float most = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s_m[w][r]);
+            f32x4 sum = (f32x4)0.f;
+            float all = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = weight_of(s_m[w][r], most);
+                sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kWave + (r * (D + 4) + c) * 4) * f;
+                all += s_l[w][r] * f;
+            }
+            if (whole) {
+                if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
+            } else {
+                *reinterpret_cast<f32x4 *>(part + r * D + c) = sum;
+                if (c == 0) {
+                    part[ROWS * D + r] = most;
+                    part[ROWS * (D + 1) + r] = all;
+                }
+            }
+        }
+        __syncthreads();
+        u = part_end;
+    }
+}
+
+// Joins the parts of items that more than one work-group had, in the order of the
+// line.  A work-group for each border between shares; the first border in an item
+// does it.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) join_kernel(Args p, int groups)
+{
+    __shared__ Line s_line;
+    const int64_t total = measure(p, s_line);
+    const int64_t each = share(total, groups), border = ((int64_t)blockIdx.x + 1) * each;
+    if (border >= total) return;
+    int b;
+    int64_t base;
+    find(p, s_line, border, b, base);
+    const Sequence seq = sequence_of(p, b);
+    const int64_t item = (border - base) / seq.units, begin = base + item * seq.units, end = begin + seq.units;
+    if (begin == border || begin < border - each) return;
+    const int rows_max = p.shape.rows, head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * rows_max;
+    const int rows = seq.tokens * p.shape.group - row0 < rows_max ? seq.tokens * p.shape.group - row0 : rows_max;
+    const int64_t first = begin / each, last = (end - 1) / each;
+    auto part = [&](int64_t w) {
+        const int64_t from = w * each;
+        return part_of<D>(p, w, slot_of(from > begin ? from : begin, from));
+    };
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        float most = -__builtin_inff();
+        for (int64_t w = first; w <= last; ++w) most = fmaxf(most, part(w)[rows_max * D + r]);
+        f32x4 sum = (f32x4)0.f;
+        float all = 0.f;
+        for (int64_t w = first; w <= last; ++w) {
+            const float *from = part(w), f = weight_of(from[rows_max * D + r], most);
+            sum += *reinterpret_cast<const f32x4 *>(from + r * D + c) * f;
+            all += from[rows_max * (D + 1) + r] * f;
+        }
+        if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+struct Form {
+    int D, nq;
+    int64_t groups;  // work-groups
+    size_t bytes;    // of the workspace
+    bool one_unit;   // no item has more than one unit
+};
+
+// The form of a call, and the work-groups that the card holds at once.
+Form form_of(int64_t d, int64_t group, int64_t heads, int64_t B, int64_t capacity, int64_t most)
+{
+    Form f;
+    f.D = padded(d);
+    f.nq = most * group > 16 && f.D <= 128 ? 2 : 1;
+    const int64_t items = B * heads * ((most * group + 16 * f.nq - 1) / (16 * f.nq));
+    const int64_t units = (capacity + kUnit - 1) / kUnit;
+    f.one_unit = units <= 1;
+    const int64_t line = items > ((int64_t)1 << 40) / (units < 1 ? 1 : units) ? (int64_t)1 << 40 : items * (units < 1 ? 1 : units);
+    f.groups = 256 * (f.D == 256 ? 1 : f.nq == 2 ? 2 : 3);
+    if (f.groups > line) f.groups = line;
+    f.bytes = f.one_unit ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
+    return f;
+}
+
+template <typename T, int D, int NQ>
+int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
+{
+    constexpr int kSum = 16 * NQ * (D + 4) * 4;
+    constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
+    // (a constant of the kernel, set at every call: no state is kept)
+    if (kWaves * kWave > 65536 - 8192 &&
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_kernel<T, D, NQ>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, kWaves * kWave) != hipSuccess)
+        return PK_ERR_LAUNCH;
+    hipLaunchKernelGGL((attention_kernel<T, D, NQ>), dim3((unsigned)f.groups), dim3(kThreads), kWaves * kWave, s, a);
+    if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    if (joined && f.groups > 1) {
+        hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kThreads), 0, s, a, (int)f.groups);
+        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    }
+    return PK_OK;
+}
+
+template <typename T>
+int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
+{
+    if (f.D == 64) return f.nq == 1 ? launch<T, 64, 1>(a, f, joined, s) : launch<T, 64, 2>(a, f, joined, s);
+    if (f.D == 128) return f.nq == 1 ? launch<T, 128, 1>(a, f, joined, s) : launch<T, 128, 2>(a, f, joined, s);
+    return launch<T, 256, 1>(a, f, joined, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pk_attention_tree_workspace_bytes(int dtype, int64_t d, int64_t q_heads, int64_t heads, int64_t B, int64_t P,
+                                         int64_t page_size, int64_t most)
+{
+    using namespace pk::heads;
+    if (!pk::dtype_size(dtype) || d < 1 || d > 256 || heads < 1 || q_heads < heads || q_heads % heads || q_heads > kMostHeads ||
+        B < 1 || B > kMostSize || P < 1 || P > kMostSize || page_size < 1 || page_size > kMostSize || most < 1 ||
+        most > kMostTokens || P * page_size > kMostSize)
+        return 0;
+    return form_of(d, q_heads / heads, heads, B, P * page_size, most).bytes;
+}
+
+int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_cache *cache, const int32_t *page_table,
+                      int64_t B, int64_t P, int64_t ld_table, const int32_t *lengths, const int32_t *starts, int64_t most,
+                      const uint64_t *mask, float scale, float cap, const pk_heads *out, float *lse, int64_t ld_lse,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace pk;
+    using namespace pk::heads;
+    api_begin();
+    const int size = dtype_size(dtype);
+    if (!size) return api_invalid(1);
+    if (M < 0) return api_invalid(2);
+    if (d < 1) return api_invalid(3);
+    if (!q) return api_invalid(4);
+    if (!cache) return api_invalid(5);
+    if (B < 0) return api_invalid(7);
+    if (P < 0) return api_invalid(8);
+    if (ld_table < P) return api_invalid(9);
+    if (most < 1) return api_invalid(12);
+    if (!(cap >= 0.f) || cap > 3e38f) return api_invalid(15);
+    if (!out || out->heads != q->heads) return api_invalid(16);
+    if (lse && ld_lse < q->heads) return api_invalid(18);
+    if ((uintptr_t)workspace % 16) return api_invalid(19);
+    if (M > kMostSize || d > 256 || B > kMostSize || P > kMostSize || ld_table > kMostSize || most > kMostTokens ||
+        (lse && ld_lse > kMostSize))
+        return PK_ERR_NOT_SUPPORTED;
+    int st;
+    if ((st = check_heads(*q, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(4) : st;
+    if ((st = check_cache(*cache, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(5) : st;
+    if (cache->heads < 1 || q->heads % cache->heads) return api_invalid(5);
+    if ((st = check_heads(*out, M, size, true, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(16) : st;
+    if (P && cache->page_size > kMostSize / P) return PK_ERR_NOT_SUPPORTED;
+    if (M == 0 || B == 0 || q->heads == 0) return PK_OK;
+    if (P && (!page_table || (uintptr_t)page_table % 4)) return api_invalid(6);
+    if (!lengths || (uintptr_t)lengths % 4) return api_invalid(10);
+    if (!starts || (uintptr_t)starts % 4) return api_invalid(11);
+    if ((uintptr_t)mask % 8) return api_invalid(13);
+    if ((uintptr_t)lse % 4) return api_invalid(17);
+    const int64_t heads = cache->heads, group = q->heads / heads;
+    const Form f = form_of(d, group, heads, B, P * cache->page_size, most);
+    const bool joined = f.bytes && workspace && workspace_bytes >= f.bytes;
+    const Region in[7] = {of_heads(*q, M, d, size), of_cache(cache->key, cache->key_stride, *cache, d, size),
+                          of_cache(cache->value, cache->value_stride, *cache, d, size),
+                          matrix(page_table, P ? B : 0, ld_table * 4, P * 4), flat(lengths, 4 * B), flat(starts, 4 * B + 4),
+                          flat(mask, mask ? 8 * M : 0)};
+    const Region ro = of_heads(*out, M, d, size), rl = matrix(lse, lse ? M : 0, ld_lse * 4, q->heads * 4),
+                 rw = flat(workspace, joined ? (int64_t)f.bytes : 0);
+    for (int i = 0; i < 7; ++i) {
+        if (shared(ro, in[i]) && !(i == 0 && same_place(*q, *out, M))) return api_invalid(16);
+        if (shared(rl, in[i])) return api_invalid(17);
+        if (shared(rw, in[i])) return api_invalid(19);
+    }
+    if (shared(rl, ro)) return api_invalid(17);
+    if (shared(rw, ro) || shared(rw, rl)) return api_invalid(19);
+
+    Args a = {};
+    a.q = q->data;
+    a.out = out->data;
+    a.key = cache->key;
+    a.value = cache->value;
+    a.table = page_table;
+    a.lengths = lengths;
+    a.starts = starts;
+    a.mask = mask;
+    a.lse = lse;
+    a.parts = (float *)workspace;
+    a.q_token = q->token_stride;
+    a.q_head = q->head_stride;
+    a.out_token = out->token_stride;
+    a.out_head = out->head_stride;
+    a.lse_token = ld_lse;
+    a.table_row = ld_table;
+    a.key_page = cache->key_stride[0];
+    a.key_place = cache->key_stride[1];
+    a.key_head = cache->key_stride[2];
+    a.value_page = cache->value_stride[0];
+    a.value_place = cache->value_stride[1];
+    a.value_head = cache->value_stride[2];
+    a.pages = cache->pages;
+    a.shape = {M, P * cache->page_size, (int)heads, (int)group, (int)most, 16 * f.nq, joined ? kUnit : 0};
+    a.B = (int)B;
+    a.d = (int)d;
+    a.page_size = (int)cache->page_size;
+    a.page_shift = -1;
+    for (int i = 0; i < 31; ++i)
+        if ((int64_t)1 << i == cache->page_size) a.page_shift = i;
+    a.scale = cap != 0.f ? scale / cap : scale * kLog2e;
+    a.cap = cap * kLog2e;
+    hipStream_t s = (hipStream_t)stream;
+    st = dtype == PK_F32 ? launch<float>(a, f, joined, s) : dtype == PK_BF16 ? launch<bf16>(a, f, joined, s) : launch<f16>(a, f, joined, s);
+    if (st == PK_OK) api_ran("attention_tree");
+    return st;
+}
+
+}  // extern "C"

@@ -1,0 +1,799 @@
+// pk_heads.hip -- queries and keys between the products of an attention layer: the
+// norm of each head and the rotation by its token's position, with its gradients,
+// and the same on the way into a paged cache.
+//
+// A head's row x of d channels becomes, in fp32,
+//   z = x w n,  n = 1 / sqrt(mean x^2 + eps)     (x itself without a weight)
+//   (a, b) -> (a cos t - b sin t, b cos t + a sin t) amplitude   for its pairs.
+// A team of lanes holds a row, a lane two vectors of 16 bytes: of a pair's two
+// channels where pairs are halves apart, of neighbours elsewhere, so that no lane
+// needs another's channels and every element is read once and written once.  The
+// angles of a token are common to its heads: a work-group has all heads of a token
+// and makes them once, into LDS.
+#include "pk_heads_checks.hpp"
+#include "pk_heads_launch.hpp"
+#include "pk_i8.hpp"
+#include "pk_i8_checks.hpp"
+
+namespace {
+
+using pk::bf16;
+using pk::f16;
+using pk::Pack;
+using pk::rounded;
+
+// Where a side's heads lie: m * token + h * head, in elements.
+struct Place {
+    void *p;
+    int64_t token, head;
+};
+
+struct HeadsArgs {
+    Place q, k, v, q_out, k_out, v_out;  // gradient: q_out, k_out the inputs' gradients
+    Place q_in, k_in;                    // gradient: the forward call's inputs
+    const void *q_weight, *k_weight;
+    const int64_t *slots;  // cache: where k and v go
+    const int64_t *positions;
+    const double *frequencies;
+    float *partial;  // gradient of the weights: a row of 2 d for each work-group
+    int64_t first, M;
+    int64_t pages, key_page, value_page;  // cache: k_out.token and v_out.token are a position's strides
+    int page_size, Hq, Hk, rows;
+    int d, pairs, pair_chunks, team, team_shift, teams, tokens, rounds, interleaved;
+    float amplitude, eps;
+};
+
+// The channels of a lane's two vectors: a at oa (na of them), b at ob (nb).
+struct Chunk {
+    int oa, na, ob, nb;
+    bool pair;
+};
+
+template <int E>
+__device__ __forceinline__ Chunk chunk_of(int c, int d, int pairs, int pair_chunks, bool interleaved)
+{
+    Chunk k;
+    k.pair = c < pair_chunks;
+    int end = d, at = 2 * pairs + (c - pair_chunks) * 2 * E;
+    if (k.pair) {
+        end = 2 * pairs;
+        at = c * 2 * E;
+        if (!interleaved) {
+            k.oa = c * E;
+            k.ob = pairs + c * E;
+            k.na = k.nb = pairs - c * E < E ? pairs - c * E : E;
+            return k;
+        }
+    }
+    const int n = end - at;
+    k.oa = at;
+    k.ob = at + E;
+    k.na = n < 0 ? 0 : n < E ? n : E;
+    k.nb = n < E ? 0 : n < 2 * E ? n - E : E;
+    return k;
+}
+
+template <typename T>
+using Vec = typename Pack<T>::V;
+
+template <typename T>
+__device__ __forceinline__ Vec<T> get(const T *p, int n)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (n == E) return *reinterpret_cast<const typename Pack<T>::U *>(p);
+    Vec<T> v = (Vec<T>)(T)0.f;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (j < n) v[j] = p[j];
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void put(T *p, int n, const Vec<T> &v)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (n == E) {
+        *reinterpret_cast<typename Pack<T>::U *>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (j < n) p[j] = v[j];
+}
+
+// E weights from p on, as fp32
+template <typename W, int E>
+__device__ __forceinline__ void get_weights(const W *p, int n, float *w)
+{
+#pragma unroll
+    for (int j = 0; j < E; ++j) w[j] = 0.f;
+    if (n == E) {
+        const typename Pack<W, E>::V v = *reinterpret_cast<const typename Pack<W, E>::U *>(p);
+#pragma unroll
+        for (int j = 0; j < E; ++j) w[j] = (float)v[j];
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (j < n) w[j] = (float)p[j];
+}
+
+// The sum of v over the lanes of a team, in each of them.  Every lane of the wave
+// takes part.
+__device__ __forceinline__ float team_sum(float v, int team)
+{
+#define PK_DPP(ctrl) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, 0xf, 0xf, false))
+    if (team > 1) PK_DPP(0xb1);   // lane ^ 1
+    if (team > 2) PK_DPP(0x4e);   // lane ^ 2
+    if (team > 4) PK_DPP(0x141);  // mirrored in 8
+    if (team > 8) PK_DPP(0x140);  // mirrored in 16
+#undef PK_DPP
+    if (team > 16) v += __shfl_xor(v, 16);
+    if (team > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// cos and sin of position * frequency, times the amplitude.  The angle is formed in
+// turns and reduced in 64 bits: 2^-52 of its turns, 2e-10 of one at position 2^20.
+__device__ __forceinline__ float2 turn_of(int64_t position, double frequency, float amplitude)
+{
+    const double turns = (double)position * (frequency * 0.15915494309189535);
+    const float half_turns = 2.f * (float)(turns - rint(turns));
+    float s, c;
+    sincospif(half_turns, &s, &c);
+    return make_float2(c * amplitude, s * amplitude);
+}
+
+// The turns of `tokens` tokens from `first` on.
+__device__ __forceinline__ void make_turns(const HeadsArgs &p, float2 *turns, int64_t first)
+{
+    for (int i = threadIdx.x; i < p.tokens * p.pairs; i += blockDim.x) {
+        const int t = i / p.pairs;
+        const int64_t m = first + t;
+        turns[i] = m < p.M ? turn_of(p.positions[m], p.frequencies[i - t * p.pairs], p.amplitude) : make_float2(0.f, 0.f);
+    }
+}
+
+// The pairs of z (a's E values, then b's) turned; `back`: by the opposite angle.
+template <int E>
+__device__ __forceinline__ void rotate(float *z, const float2 *turns, int n, bool interleaved, float back)
+{
+    float2 t[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) t[j] = j < n ? turns[j] : make_float2(0.f, 0.f);
+    if (interleaved) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float a = z[2 * j], b = z[2 * j + 1], s = t[j].y * back;
+            z[2 * j] = fmaf(a, t[j].x, -(b * s));
+            z[2 * j + 1] = fmaf(b, t[j].x, a * s);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float a = z[j], b = z[E + j], s = t[j].y * back;
+            z[j] = fmaf(a, t[j].x, -(b * s));
+            z[E + j] = fmaf(b, t[j].x, a * s);
+        }
+    }
+}
+
+// z, a row over its team, times 1 / sqrt(mean z^2 + eps): the factor is up * root.
+// A sum of squares that leaves the 32 bits' range, or falls where eps does not cover
+// what it loses, is taken once more of z times a power of two.
+struct Factor {
+    float up, root;
+};
+
+template <int E>
+__device__ __forceinline__ Factor norm(float *z, int d, int team, float eps)
+{
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2 * E; ++j) ss = fmaf(z[j], z[j], ss);
+    ss = team_sum(ss, team);
+    Factor f = {1.f, 0.f};
+    const bool above = !(ss < 0x1p120f), below = ss < 0x1p-80f && eps < 0x1p-100f;
+    if (__any(above || below)) {  // the whole wave: the sum is across lanes
+        f.up = above ? 0x1p-70f : below ? 0x1p100f : 1.f;
+        ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2 * E; ++j) {
+            z[j] *= f.up;
+            ss = fmaf(z[j], z[j], ss);
+        }
+        ss = team_sum(ss, team);
+        eps = eps * f.up * f.up;  // one by one: 2^200 is no fp32 number
+    }
+    f.root = 1.f / sqrtf(ss / (float)d + eps);
+#pragma unroll
+    for (int j = 0; j < 2 * E; ++j) z[j] *= f.root;
+    return f;
+}
+
+// One token's heads are its queries', its keys', then its values'.
+template <typename T, typename W>
+__global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    extern __shared__ float2 s_turns[];
+    const int c = threadIdx.x & (p.team - 1), slot = threadIdx.x >> p.team_shift;
+    int t = 0, r = slot;
+    if (p.tokens > 1) {
+        t = slot / p.rows;
+        r = t < p.tokens ? slot - t * p.rows : p.rows;
+    }
+    const int64_t first = p.first + (int64_t)blockIdx.x * p.tokens, m = first + t;
+    const Chunk ck = chunk_of<E>(c, p.d, p.pairs, p.pair_chunks, p.interleaved);
+    const Chunk cv = chunk_of<E>(c, p.d, 0, 0, false);
+    const float2 *turns = s_turns + t * p.pairs + c * E;
+
+    // the token's place in the cache
+    int64_t page = 0, place = 0;
+    bool kept = true;
+    if (p.slots && m < p.M) {
+        const int64_t s = p.slots[m];
+        if ((uint64_t)s >> 32) {
+            page = (int64_t)((uint64_t)s / (unsigned)p.page_size);
+            place = s - page * p.page_size;
+        } else {
+            page = (unsigned)s / (unsigned)p.page_size;
+            place = (unsigned)s - (unsigned)page * (unsigned)p.page_size;
+        }
+        kept = s >= 0 && page < p.pages;
+    }
+
+    struct Row {
+        Chunk k;
+        Vec<T> a, b;
+        T *to;
+        const W *w;
+        bool on, plain;
+    };
+    auto fetch = [&](int row) {
+        Row x;
+        x.on = m < p.M && row < p.rows && (row < p.Hq || kept);
+        x.plain = row >= p.Hq + p.Hk;
+        x.k = x.plain ? cv : ck;
+        x.a = x.b = (Vec<T>)(T)0.f;
+        x.w = nullptr;
+        x.to = nullptr;
+        if (!x.on) return x;
+        const bool query = row < p.Hq;
+        const int h = query ? row : x.plain ? row - p.Hq - p.Hk : row - p.Hq;
+        const Place &from = query ? p.q : x.plain ? p.v : p.k;
+        const Place &to = query ? p.q_out : x.plain ? p.v_out : p.k_out;
+        const T *at = (const T *)from.p + m * from.token + h * from.head;
+        x.to = (T *)to.p + h * to.head + (query || !p.slots ? m * to.token
+                                                            : page * (x.plain ? p.value_page : p.key_page) + place * to.token);
+        x.a = get(at + x.k.oa, x.k.na);
+        x.b = get(at + x.k.ob, x.k.nb);
+        x.w = x.plain ? nullptr : (const W *)(query ? p.q_weight : p.k_weight);
+        return x;
+    };
+
+    Row x = fetch(r);
+    if (p.pairs) {
+        make_turns(p, s_turns, first);
+        __syncthreads();
+    }
+    for (int i = 0;;) {
+        if (p.q_weight || p.k_weight || p.pairs) {
+            float z[2 * E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                z[j] = (float)x.a[j];
+                z[E + j] = (float)x.b[j];
+            }
+            if (p.q_weight || p.k_weight) {
+                float y[2 * E];
+#pragma unroll
+                for (int j = 0; j < 2 * E; ++j) y[j] = z[j];
+                norm<E>(y, p.d, p.team, p.eps);  // every lane of the wave, whatever its row
+                if (x.w) {
+                    float w[2 * E];
+                    get_weights<W, E>(x.w + x.k.oa, x.k.na, w);
+                    get_weights<W, E>(x.w + x.k.ob, x.k.nb, w + E);
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) z[j] = y[j] * w[j];
+                }
+            }
+            if (!x.plain) {
+                if (x.k.pair) rotate<E>(z, turns, p.pairs - c * E, p.interleaved, 1.f);
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    x.a[j] = rounded<T>(z[j]);
+                    x.b[j] = rounded<T>(z[E + j]);
+                }
+            }
+        }
+        if (x.on) {
+            put(x.to + x.k.oa, x.k.na, x.a);
+            put(x.to + x.k.ob, x.k.nb, x.b);
+        }
+        if (++i >= p.rounds) break;
+        r += p.teams;
+        x = fetch(r);
+    }
+}
+
+// Gradients: with g the output's gradient turned back, u = x n,
+//   dx = n (g w - u mean(g w u)),  dw = sum g u.
+// A lane has the same channels of every row, so a work-group keeps its part of dw
+// in registers over all its tokens; its rows are added up by weights_kernel in the
+// order of the work-groups.
+template <typename T, typename W>
+__global__ void __launch_bounds__(pk::kMostHeadThreads) heads_grad_kernel(HeadsArgs p)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    extern __shared__ float2 s_turns[];
+    const int c = threadIdx.x & (p.team - 1), slot = threadIdx.x >> p.team_shift;
+    int t = 0, r0 = slot;
+    if (p.tokens > 1) {
+        t = slot / p.rows;
+        r0 = t < p.tokens ? slot - t * p.rows : p.rows;
+    }
+    const Chunk ck = chunk_of<E>(c, p.d, p.pairs, p.pair_chunks, p.interleaved);
+    float sum_q[2 * E], sum_k[2 * E];
+#pragma unroll
+    for (int j = 0; j < 2 * E; ++j) sum_q[j] = sum_k[j] = 0.f;
+
+    int half = 0;
+    for (int64_t first = (int64_t)blockIdx.x * p.tokens; first < p.M; first += (int64_t)gridDim.x * p.tokens, half ^= 1) {
+        const int64_t m = first + t;
+        float2 *turns = s_turns + half * p.tokens * p.pairs;
+        if (p.pairs) {
+            // the other half may still be read
+            make_turns(p, turns, first);
+            __syncthreads();
+        }
+        turns += t * p.pairs + c * E;
+        int r = r0;
+        for (int i = 0; i < p.rounds; ++i, r += p.teams) {
+            const bool on = m < p.M && r < p.rows, query = r < p.Hq;
+            const int h = query ? r : r - p.Hq;
+            const W *weight = (const W *)(query ? p.q_weight : p.k_weight);
+            Vec<T> a = (Vec<T>)(T)0.f, b = a, xa = a, xb = a;
+            if (on) {
+                const Place &from = query ? p.q : p.k, &in = query ? p.q_in : p.k_in;
+                const T *at = (const T *)from.p + m * from.token + h * from.head;
+                a = get(at + ck.oa, ck.na);
+                b = get(at + ck.ob, ck.nb);
+                if (weight) {
+                    const T *px = (const T *)in.p + m * in.token + h * in.head;
+                    xa = get(px + ck.oa, ck.na);
+                    xb = get(px + ck.ob, ck.nb);
+                }
+            }
+            float g[2 * E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                g[j] = (float)a[j];
+                g[E + j] = (float)b[j];
+            }
+            if (ck.pair) rotate<E>(g, turns, p.pairs - c * E, p.interleaved, -1.f);
+            if (p.q_weight || p.k_weight) {
+                float u[2 * E], w[2 * E], dot = 0.f;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    u[j] = (float)xa[j];
+                    u[E + j] = (float)xb[j];
+                }
+                const Factor f = norm<E>(u, p.d, p.team, p.eps);
+                if (on && weight) {
+                    get_weights<W, E>(weight + ck.oa, ck.na, w);
+                    get_weights<W, E>(weight + ck.ob, ck.nb, w + E);
+                    // rows that are not there, and sides without a weight, add nothing
+                    if (query) {
+#pragma unroll
+                        for (int j = 0; j < 2 * E; ++j) sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2 * E; ++j) sum_k[j] = fmaf(g[j], u[j], sum_k[j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) {
+                        w[j] *= g[j];
+                        dot = fmaf(w[j], u[j], dot);
+                    }
+                }
+                dot = team_sum(dot, p.team) / (float)p.d;
+                if (on && weight) {
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) g[j] = fmaf(-u[j], dot, w[j]) * f.root * f.up;
+                }
+            }
+            if (on) {
+                const Place &to = query ? p.q_out : p.k_out;
+                T *at = (T *)to.p + m * to.token + h * to.head;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    a[j] = rounded<T>(g[j]);
+                    b[j] = rounded<T>(g[E + j]);
+                }
+                put(at + ck.oa, ck.na, a);
+                put(at + ck.ob, ck.nb, b);
+            }
+        }
+    }
+    if (!p.q_weight && !p.k_weight) return;
+
+    // over the teams of a wave, then over the waves
+    for (int o = p.team; o < 64; o *= 2) {
+#pragma unroll
+        for (int j = 0; j < 2 * E; ++j) {
+            sum_q[j] += __shfl_xor(sum_q[j], o);
+            sum_k[j] += __shfl_xor(sum_k[j], o);
+        }
+    }
+    float *s_sum = (float *)s_turns;
+    __syncthreads();  // the turns have been read
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    if (threadIdx.x % 64 < p.team) {
+        float *q = s_sum + wave * 2 * p.d, *k = q + p.d;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if (j < ck.na) {
+                q[ck.oa + j] = sum_q[j];
+                k[ck.oa + j] = sum_k[j];
+            }
+            if (j < ck.nb) {
+                q[ck.ob + j] = sum_q[E + j];
+                k[ck.ob + j] = sum_k[E + j];
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.d; i += blockDim.x) {
+        float v = 0.f;
+        for (int w = 0; w < waves; ++w) v += s_sum[w * 2 * p.d + i];
+        p.partial[(int64_t)blockIdx.x * 2 * p.d + i] = v;
+    }
+}
+
+// The rows of `partial` added up, 64 columns a work-group, sixteen lanes a column.
+template <typename W>
+__global__ void __launch_bounds__(1024) weights_kernel(const float *partial, int groups, int d, W *q, W *k)
+{
+    __shared__ float s_v[16][64];
+    const int x = threadIdx.x % 64, y = threadIdx.x / 64, col = blockIdx.x * 64 + x;
+    float v = 0.f;
+    if (col < 2 * d) {
+#pragma unroll 8
+        for (int g = y; g < groups; g += 16) v += partial[(int64_t)g * 2 * d + col];
+    }
+    s_v[y][x] = v;
+    __syncthreads();
+    if (y || col >= 2 * d) return;
+    for (int i = 1; i < 16; ++i) v += s_v[i][x];
+    W *to = col < d ? q : k;
+    if (to) to[col < d ? col : col - d] = (W)v;
+}
+
+// ---------------------------------------------------------------- launches
+
+constexpr int64_t kMostGroups = 1 << 22;  // of a launch: 512 work-items each stay below 2^32
+constexpr int kGradGroups = 1024;         // four work-groups a CU
+
+int log2_of(int v)
+{
+    int s = 0;
+    while (1 << s < v) ++s;
+    return s;
+}
+
+// The tiling of `a` for its type's vectors.
+pk::HeadGroup lay_out(HeadsArgs &a, int rows, int size)
+{
+    const pk::HeadTiling t = pk::head_tiling(a.d, a.pairs, 16 / size);
+    const pk::HeadGroup g = pk::head_group(rows, t.team, a.pairs);
+    a.rows = rows;
+    a.pair_chunks = t.pair_chunks;
+    a.team = t.team;
+    a.team_shift = log2_of(t.team);
+    a.teams = g.teams;
+    a.tokens = g.tokens;
+    a.rounds = g.tokens > 1 ? 1 : (rows + g.teams - 1) / g.teams;
+    return g;
+}
+
+template <typename T, typename W>
+int launch_heads(HeadsArgs a, int rows, hipStream_t s)
+{
+    const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
+    const size_t lds = (size_t)a.tokens * a.pairs * sizeof(float2);
+    for (int64_t left = (a.M + a.tokens - 1) / a.tokens; left > 0; left -= kMostGroups) {
+        const int64_t now = left < kMostGroups ? left : kMostGroups;
+        hipLaunchKernelGGL((heads_kernel<T, W>), dim3((unsigned)now), dim3(g.threads), lds, s, a);
+        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+        a.first += now * a.tokens;
+    }
+    return PK_OK;
+}
+
+template <typename T, typename W>
+int launch_grad(HeadsArgs a, int rows, void *q_weight_grad, void *k_weight_grad, hipStream_t s)
+{
+    int64_t groups = 0;
+    if (rows && a.M) {
+        const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
+        groups = (a.M + a.tokens - 1) / a.tokens;
+        if (groups > kGradGroups) groups = kGradGroups;
+        size_t lds = (size_t)2 * a.tokens * a.pairs * sizeof(float2);
+        const size_t sums = (size_t)(g.threads / 64) * 2 * a.d * sizeof(float);
+        if (lds < sums) lds = sums;
+        hipLaunchKernelGGL((heads_grad_kernel<T, W>), dim3((unsigned)groups), dim3(g.threads), lds, s, a);
+        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    }
+    if (q_weight_grad || k_weight_grad) {
+        hipLaunchKernelGGL((weights_kernel<W>), dim3((2 * a.d + 63) / 64), dim3(1024), 0, s, a.partial, (int)groups, a.d,
+                           (W *)q_weight_grad, (W *)k_weight_grad);
+        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    }
+    return PK_OK;
+}
+
+// What every call checks of its rotation: 0, or the status.
+int check_rotation(const pk_rotation *rot, int64_t d, bool read)
+{
+    if (!rot) return PK_OK;
+    if (rot->pairs < 0 || 2 * rot->pairs > d) return PK_ERR_INVALID_VALUE;
+    if (rot->pairs && read &&
+        (!rot->positions || !rot->frequencies || (uintptr_t)rot->positions % 8 || (uintptr_t)rot->frequencies % 8))
+        return PK_ERR_INVALID_VALUE;
+    return PK_OK;
+}
+
+void set_rotation(HeadsArgs &a, const pk_rotation *rot)
+{
+    if (!rot || !rot->pairs) return;
+    a.positions = rot->positions;
+    a.frequencies = rot->frequencies;
+    a.pairs = (int)rot->pairs;
+    a.interleaved = rot->interleaved != 0;
+    a.amplitude = rot->amplitude;
+}
+
+Place place(const pk_heads *t)
+{
+    if (!t) return {nullptr, 0, 0};
+    return {t->data, t->token_stride, t->head_stride};
+}
+
+// Whether an output shares memory with the rotation's arrays or a weight.
+bool over_small(const pk::heads::Region &out, const pk_rotation *rot, int64_t M, const void *qw, const void *kw, int64_t wbytes)
+{
+    using namespace pk::heads;
+    if (rot && rot->pairs && (shared(out, flat(rot->positions, 8 * M)) || shared(out, flat(rot->frequencies, 8 * rot->pairs))))
+        return true;
+    return (qw && shared(out, flat(qw, wbytes))) || (kw && shared(out, flat(kw, wbytes)));
+}
+
+#define PK_HEADS_TYPES(FN, ...)                                                                        \
+    (dtype == PK_F32           ? FN<float, float>(__VA_ARGS__)                                         \
+     : weight_dtype == PK_F32  ? (dtype == PK_BF16 ? FN<bf16, float>(__VA_ARGS__) : FN<f16, float>(__VA_ARGS__)) \
+     : dtype == PK_BF16        ? FN<bf16, bf16>(__VA_ARGS__)                                           \
+                               : FN<f16, f16>(__VA_ARGS__))
+
+}  // namespace
+
+extern "C" {
+
+int pk_rope_qk(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_heads *k, const pk_rotation *rotation,
+               const void *q_weight, const void *k_weight, int weight_dtype, float eps, const pk_heads *q_out,
+               const pk_heads *k_out, void *stream)
+{
+    using namespace pk;
+    using namespace pk::heads;
+    api_begin();
+    const int size = dtype_size(dtype), wsize = dtype_size(weight_dtype);
+    if (!size) return api_invalid(1);
+    if (M < 0) return api_invalid(2);
+    if (d < 1) return api_invalid(3);
+    if (q_weight && !q) return api_invalid(7);
+    if (k_weight && !k) return api_invalid(8);
+    if ((q_weight || k_weight) && weight_dtype != PK_F32 && weight_dtype != dtype) return api_invalid(9);
+    if ((q_weight || k_weight) && !(eps >= 0.f)) return api_invalid(10);
+    if (!q_out != !q || (q && q_out->heads != q->heads)) return api_invalid(11);
+    if (!k_out != !k || (k && k_out->heads != k->heads)) return api_invalid(12);
+    if (M > kMostSize || d > 256) return PK_ERR_NOT_SUPPORTED;
+    int st;
+    if (check_rotation(rotation, d, M > 0)) return api_invalid(6);
+    if (q && (st = check_heads(*q, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(4) : st;
+    if (k && (st = check_heads(*k, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(5) : st;
+    if (q && (st = check_heads(*q_out, M, size, true, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(11) : st;
+    if (k && (st = check_heads(*k_out, M, size, true, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(12) : st;
+    if (q_weight && (uintptr_t)q_weight % (uintptr_t)wsize) return api_invalid(7);
+    if (k_weight && (uintptr_t)k_weight % (uintptr_t)wsize) return api_invalid(8);
+    const int64_t Hq = q ? q->heads : 0, Hk = k ? k->heads : 0;
+    if (M == 0 || Hq + Hk == 0) return PK_OK;
+    const Region none = flat(nullptr, 0), rq = q ? of_heads(*q, M, d, size) : none, rk = k ? of_heads(*k, M, d, size) : none;
+    const Region oq = q ? of_heads(*q_out, M, d, size) : none, ok = k ? of_heads(*k_out, M, d, size) : none;
+    if (shared(oq, rk) || (shared(oq, rq) && !same_place(*q, *q_out, M)) ||
+        over_small(oq, rotation, M, q_weight, k_weight, d * wsize))
+        return api_invalid(11);
+    if (shared(ok, rq) || shared(ok, oq) || (shared(ok, rk) && !same_place(*k, *k_out, M)) ||
+        over_small(ok, rotation, M, q_weight, k_weight, d * wsize))
+        return api_invalid(12);
+    HeadsArgs a = {};
+    a.q = place(q);
+    a.k = place(k);
+    a.q_out = place(q_out);
+    a.k_out = place(k_out);
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.M = M;
+    a.Hq = (int)Hq;
+    a.Hk = (int)Hk;
+    a.d = (int)d;
+    a.eps = eps;
+    set_rotation(a, rotation);
+    st = PK_HEADS_TYPES(launch_heads, a, (int)(Hq + Hk), (hipStream_t)stream);
+    if (st == PK_OK) api_ran("rope_qk");
+    return st;
+}
+
+size_t pk_rope_qk_backward_workspace_bytes(int64_t M, int64_t d)
+{
+    if (M < 1 || d < 1 || d > 256) return 0;
+    return (size_t)(M < kGradGroups ? M : kGradGroups) * 2 * (size_t)d * sizeof(float);
+}
+
+int pk_rope_qk_backward(int dtype, int64_t M, int64_t d, const pk_heads *dq, const pk_heads *dk, const pk_heads *q,
+                        const pk_heads *k, const pk_rotation *rotation, const void *q_weight, const void *k_weight,
+                        int weight_dtype, float eps, const pk_heads *q_grad, const pk_heads *k_grad,
+                        void *q_weight_grad, void *k_weight_grad, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace pk;
+    using namespace pk::heads;
+    api_begin();
+    const int size = dtype_size(dtype), wsize = dtype_size(weight_dtype);
+    const bool weights = q_weight || k_weight;
+    if (!size) return api_invalid(1);
+    if (M < 0) return api_invalid(2);
+    if (d < 1) return api_invalid(3);
+    if (q_weight && (!q || !dq || q->heads != dq->heads)) return api_invalid(6);
+    if (k_weight && (!k || !dk || k->heads != dk->heads)) return api_invalid(7);
+    if (weights && weight_dtype != PK_F32 && weight_dtype != dtype) return api_invalid(11);
+    if (weights && !(eps >= 0.f)) return api_invalid(12);
+    if (!q_grad != !dq || (dq && q_grad->heads != dq->heads)) return api_invalid(13);
+    if (!k_grad != !dk || (dk && k_grad->heads != dk->heads)) return api_invalid(14);
+    if (!q_weight_grad != !q_weight) return api_invalid(15);
+    if (!k_weight_grad != !k_weight) return api_invalid(16);
+    if (M > kMostSize || d > 256) return PK_ERR_NOT_SUPPORTED;
+    if (!q_weight) q = nullptr;  // not read
+    if (!k_weight) k = nullptr;
+    int st;
+    if (check_rotation(rotation, d, M > 0)) return api_invalid(8);
+    const pk_heads *in[6] = {dq, dk, q, k, q_grad, k_grad};
+    const int at[6] = {4, 5, 6, 7, 13, 14};
+    for (int i = 0; i < 6; ++i)
+        if (in[i] && (st = check_heads(*in[i], M, size, i >= 4, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(at[i]) : st;
+    if (weights) {
+        const void *vectors[4] = {q_weight, k_weight, q_weight_grad, k_weight_grad};
+        const int where[4] = {9, 10, 15, 16};
+        for (int i = 0; i < 4; ++i)
+            if (vectors[i] && (uintptr_t)vectors[i] % (uintptr_t)wsize) return api_invalid(where[i]);
+    }
+    Region r[6];
+    for (int i = 0; i < 6; ++i) r[i] = in[i] ? of_heads(*in[i], M, d, size) : flat(nullptr, 0);
+    for (int o = 4; o < 6; ++o) {
+        for (int i = 0; i < o; ++i) {
+            const bool own = i == o - 4 && in[i] && same_place(*in[i], *in[o], M);
+            if (shared(r[o], r[i]) && !own) return api_invalid(at[o]);
+        }
+        if (over_small(r[o], rotation, M, q_weight, k_weight, d * wsize)) return api_invalid(at[o]);
+    }
+    const int64_t wbytes = weights ? d * wsize : 0;
+    void *wg[2] = {q_weight_grad, k_weight_grad};
+    for (int o = 0; o < 2; ++o) {
+        if (!wg[o]) continue;
+        const Region w = flat(wg[o], wbytes);
+        for (int i = 0; i < 6; ++i)
+            if (shared(w, r[i])) return api_invalid(15 + o);
+        if (over_small(w, rotation, M, q_weight, k_weight, wbytes) || (o && wg[0] && shared(w, flat(wg[0], wbytes))))
+            return api_invalid(15 + o);
+    }
+    const int64_t Hq = dq ? dq->heads : 0, Hk = dk ? dk->heads : 0;
+    const bool work = M > 0 && Hq + Hk > 0;
+    if (weights) {
+        const size_t need = work ? pk_rope_qk_backward_workspace_bytes(M, d) : 0;
+        if (workspace_bytes < need || (need && !workspace)) return PK_ERR_WORKSPACE;
+        if ((uintptr_t)workspace % 16) return api_invalid(17);
+        const Region ws = flat(workspace, (int64_t)need);
+        for (int i = 0; i < 6; ++i)
+            if (shared(ws, r[i])) return api_invalid(17);
+        for (int o = 0; o < 2; ++o)
+            if (wg[o] && shared(ws, flat(wg[o], wbytes))) return api_invalid(17);
+        if (over_small(ws, rotation, M, q_weight, k_weight, wbytes)) return api_invalid(17);
+    }
+    if (!work && !weights) return PK_OK;
+    HeadsArgs a = {};
+    a.q = place(dq);
+    a.k = place(dk);
+    a.q_in = place(q);
+    a.k_in = place(k);
+    a.q_out = place(q_grad);
+    a.k_out = place(k_grad);
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.partial = (float *)workspace;
+    a.M = M;
+    a.Hq = (int)Hq;
+    a.Hk = (int)Hk;
+    a.d = (int)d;
+    a.eps = eps;
+    set_rotation(a, rotation);
+    st = PK_HEADS_TYPES(launch_grad, a, (int)(Hq + Hk), q_weight_grad, k_weight_grad, (hipStream_t)stream);
+    if (st == PK_OK) api_ran("rope_qk_backward");
+    return st;
+}
+
+int pk_cache_append(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_heads *k, const pk_heads *v,
+                    const pk_rotation *rotation, const void *q_weight, const void *k_weight, int weight_dtype, float eps,
+                    const pk_heads *q_out, const pk_cache *cache, const int64_t *slots, void *stream)
+{
+    using namespace pk;
+    using namespace pk::heads;
+    api_begin();
+    const int size = dtype_size(dtype), wsize = dtype_size(weight_dtype);
+    if (!size) return api_invalid(1);
+    if (M < 0) return api_invalid(2);
+    if (d < 1) return api_invalid(3);
+    if (!k) return api_invalid(5);
+    if (!v || v->heads != k->heads) return api_invalid(6);
+    if (q_weight && !q) return api_invalid(8);
+    if ((q_weight || k_weight) && weight_dtype != PK_F32 && weight_dtype != dtype) return api_invalid(10);
+    if ((q_weight || k_weight) && !(eps >= 0.f)) return api_invalid(11);
+    if (!q_out != !q || (q && q_out->heads != q->heads)) return api_invalid(12);
+    if (!cache || cache->heads != k->heads) return api_invalid(13);
+    if (M > kMostSize || d > 256) return PK_ERR_NOT_SUPPORTED;
+    int st;
+    if (check_rotation(rotation, d, M > 0)) return api_invalid(7);
+    if (q && (st = check_heads(*q, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(4) : st;
+    if ((st = check_heads(*k, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(5) : st;
+    if ((st = check_heads(*v, M, size, false, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(6) : st;
+    if (q && (st = check_heads(*q_out, M, size, true, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(12) : st;
+    if ((st = check_cache(*cache, size, true, d))) return st == PK_ERR_INVALID_VALUE ? api_invalid(13) : st;
+    if (q_weight && (uintptr_t)q_weight % (uintptr_t)wsize) return api_invalid(8);
+    if (k_weight && (uintptr_t)k_weight % (uintptr_t)wsize) return api_invalid(9);
+    const int64_t Hq = q ? q->heads : 0, Hk = k->heads;
+    if (M == 0 || Hq + Hk == 0) return PK_OK;
+    if (!slots || (uintptr_t)slots % 8) return api_invalid(14);
+    const Region none = flat(nullptr, 0), rq = q ? of_heads(*q, M, d, size) : none, rk = of_heads(*k, M, d, size),
+                 rv = of_heads(*v, M, d, size), rs = flat(slots, 8 * M);
+    const Region oq = q ? of_heads(*q_out, M, d, size) : none, kc = of_cache(cache->key, cache->key_stride, *cache, d, size),
+                 vc = of_cache(cache->value, cache->value_stride, *cache, d, size);
+    if (shared(oq, rk) || shared(oq, rv) || shared(oq, rs) || (shared(oq, rq) && !same_place(*q, *q_out, M)) ||
+        over_small(oq, rotation, M, q_weight, k_weight, d * wsize))
+        return api_invalid(12);
+    for (const Region &c : {kc, vc})
+        if (shared(c, rq) || shared(c, rk) || shared(c, rv) || shared(c, rs) || shared(c, oq) ||
+            over_small(c, rotation, M, q_weight, k_weight, d * wsize))
+            return api_invalid(13);
+    HeadsArgs a = {};
+    a.q = place(q);
+    a.k = place(k);
+    a.v = place(v);
+    a.q_out = place(q_out);
+    a.k_out = {cache->key, cache->key_stride[1], cache->key_stride[2]};
+    a.v_out = {cache->value, cache->value_stride[1], cache->value_stride[2]};
+    a.slots = slots;
+    a.pages = cache->pages;
+    a.page_size = (int)cache->page_size;
+    a.key_page = cache->key_stride[0];
+    a.value_page = cache->value_stride[0];
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.M = M;
+    a.Hq = (int)Hq;
+    a.Hk = (int)Hk;
+    a.d = (int)d;
+    a.eps = eps;
+    set_rotation(a, rotation);
+    st = PK_HEADS_TYPES(launch_heads, a, (int)(Hq + 2 * Hk), (hipStream_t)stream);
+    if (st == PK_OK) api_ran("cache_append");
+    return st;
+}
+
+}  // extern "C"
