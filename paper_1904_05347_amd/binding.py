@@ -170,7 +170,9 @@ EXT_PATH = os.path.join(HERE, "_pk_torch.so")
 _NATIVE_ENTRIES = ("pk_sgemm_ws", "pk_sgemm_workspace_bytes_for", "pk_conv2d_fwd", "pk_conv2d_workspace_bytes_for",
                    "pk_conv2d_out_dims", "pk_conv2d_same_pads", "pk_conv2d_winograd_tile_fwd",
                    "pk_conv2d_winograd_tile_workspace_bytes", "pk_quantize_i8", "pk_rmsnorm_i8", "pk_gated_i8",
-                   "pk_dequantize_i8", "pk_gemm_i8_ws", "pk_gemm_i8_workspace_bytes_for")
+                   "pk_dequantize_i8", "pk_gemm_i8_ws", "pk_gemm_i8_workspace_bytes_for", "pk_rope_qk",
+                   "pk_rope_qk_backward", "pk_rope_qk_backward_workspace_bytes", "pk_cache_append", "pk_attention_tree",
+                   "pk_attention_tree_workspace_bytes")
 _native = None
 
 
@@ -183,6 +185,7 @@ class _PythonOnly:
 
     conv2d_fwd = conv2d_winograd = gemm
     quantize_i8 = rmsnorm_i8 = gated_i8 = dequantize_i8 = gemm_i8 = gemm
+    rope_qk = rope_qk_backward = cache_append = attention_tree = gemm
 
 
 def _load_native():
@@ -850,7 +853,9 @@ def rope_qk(q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6
     channels from 2 * pairs on stay as they are.  ``q_weight`` and ``k_weight`` (the
     heads' type or float32) are the norms' weights, None for no norm; ``amplitude``
     multiplies what is rotated.  ``q_out`` may be ``q`` and ``k_out`` ``k``."""
-    import torch  # noqa: F401
+    r = (_native or _load_native()).rope_qk(q, k, positions, frequencies, q_weight, k_weight, eps, layout, amplitude, q_out, k_out)
+    if r is not None:
+        return r
     hq = _check_heads(q, "q")
     dt = _dtype_code(q.dtype, "q")
     M, _, d = q.shape
@@ -877,6 +882,10 @@ def rope_qk_backward(dq, dk, q, k, positions, frequencies, q_weight=None, k_weig
     (see pk_rope_qk_backward).  q or k may be None where its side has no weight;
     the weights' gradients are None there.  ``q_grad`` may be ``dq`` and ``k_grad``
     ``dk``."""
+    r = (_native or _load_native()).rope_qk_backward(dq, dk, q, k, positions, frequencies, q_weight, k_weight, eps, layout, amplitude,
+                                                     q_grad, k_grad)
+    if r is not None:
+        return r
     import torch
     hdq = _check_heads(dq, "dq")
     dt = _dtype_code(dq.dtype, "dq")
@@ -918,6 +927,10 @@ def cache_append(k, v, key_cache, value_cache, slots, positions=None, frequencie
     strides (a permuted view, the halves of one tensor); ``slots`` (int64) has a page
     times the positions of a page plus the position in it for each token, those that
     are negative or beyond the cache are left out, and the others must be distinct."""
+    r = (_native or _load_native()).cache_append(k, v, key_cache, value_cache, slots, positions, frequencies, k_weight, q, q_weight,
+                                                 eps, layout, amplitude, q_out)
+    if r is not None:
+        return r[0]
     import torch
     hk = _check_heads(k, "k")
     dt = _dtype_code(k.dtype, "k")
@@ -956,6 +969,10 @@ def attention_tree(q, key_cache, value_cache, page_table, lengths, starts, most,
     of tokens that are in no sequence.  workspace (a float32 device tensor) lets long
     sequences be divided over the card; when None, one of the size that the library
     asks for is allocated."""
+    r = (_native or _load_native()).attention_tree(q, key_cache, value_cache, page_table, lengths, starts, most, mask, scale, cap,
+                                                   out, lse, workspace)
+    if r is not None:
+        return r
     import torch
     hq = _check_heads(q, "q")
     dt = _dtype_code(q.dtype, "q")

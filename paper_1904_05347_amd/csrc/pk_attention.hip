@@ -140,11 +140,12 @@ __device__ __forceinline__ float tanh_of(float x)
 
 constexpr int kThreads = kWaves * 64;
 
+template <int THREADS>
 struct Line {
-    int64_t ends[kThreads];  // units up to the end of each work-item's sequences
-    int64_t base;            // of the sequence found
+    int64_t ends[THREADS];  // units up to the end of each work-item's sequences
+    int64_t base;           // of the sequence found
     int b;
-    int64_t waves[kThreads / 64];
+    int64_t waves[THREADS / 64];
 };
 
 __device__ __forceinline__ Sequence sequence_of(const Args &p, int b)
@@ -153,9 +154,10 @@ __device__ __forceinline__ Sequence sequence_of(const Args &p, int b)
 }
 
 // Units of the whole call.  Each work-item adds up its own run of sequences.
-__device__ __forceinline__ int64_t measure(const Args &p, Line &s)
+template <int THREADS>
+__device__ __forceinline__ int64_t measure(const Args &p, Line<THREADS> &s)
 {
-    const int t = threadIdx.x, run = (p.B + kThreads - 1) / kThreads;
+    const int t = threadIdx.x, run = (p.B + THREADS - 1) / THREADS;
     int64_t sum = 0;
     for (int b = t * run; b < (t + 1) * run && b < p.B; ++b) sum += sequence_of(p, b).cost(p.shape.heads);
     for (int o = 1; o < 64; o *= 2) {
@@ -165,7 +167,7 @@ __device__ __forceinline__ int64_t measure(const Args &p, Line &s)
     if (t % 64 == 63) s.waves[t / 64] = sum;
     __syncthreads();
     int64_t before = 0, total = 0;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < t / 64) before += s.waves[w];
         total += s.waves[w];
     }
@@ -175,9 +177,10 @@ __device__ __forceinline__ int64_t measure(const Args &p, Line &s)
 }
 
 // The sequence that has unit u < total, and the units before it.
-__device__ __forceinline__ void find(const Args &p, Line &s, int64_t u, int &b, int64_t &base)
+template <int THREADS>
+__device__ __forceinline__ void find(const Args &p, Line<THREADS> &s, int64_t u, int &b, int64_t &base)
 {
-    const int t = threadIdx.x, run = (p.B + kThreads - 1) / kThreads;
+    const int t = threadIdx.x, run = (p.B + THREADS - 1) / THREADS;
     const int64_t before = t ? s.ends[t - 1] : 0;
     if (u >= before && u < s.ends[t]) {
         int64_t at = before;
@@ -257,8 +260,8 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(Args p)
     constexpr int C = D / 32, N = D / 16, ROWS = 16 * NQ;
     constexpr int kSum = ROWS * (D + 4) * 4;  // a wave's sums
     constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
-    extern __shared__ __align__(16) char s_raw[];  // kWaves * kWave: too much to be static for the widest heads
-    __shared__ Line s_line;
+    __shared__ __align__(16) char s_raw[kWaves * kWave];
+    __shared__ Line<kThreads> s_line;
     __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
     T *s_v = reinterpret_cast<T *>(s_raw + wave * kWave);
@@ -495,13 +498,372 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(Args p)
     }
 }
 
+// ------------------------------------------------------------------ the attention, copied to LDS
+
+// A wave's 32 rows of K or V in LDS as copies leave them: 1 KiB an instruction, 16
+// bytes a lane, so that a row's chunks of 16 bytes lie side by side.  Chunk c of row r
+// is at place c ^ turn(r): sixteen rows' chunks of one column lie in all banks.
+template <typename T, int D>
+struct Copied {
+    static constexpr int kChunks = D * (int)sizeof(T) / 16;  // of a row
+    static constexpr int kRow = kChunks * 16;
+    static constexpr int kBytes = kTile * kRow;
+    static constexpr int kRows = 64 / kChunks;      // of a copy
+    static constexpr int kCopies = kTile / kRows;   // of a tile
+    static constexpr int kTurns = kRows >= 16 ? 1 : 16 / kRows < kCopies ? 16 / kRows : kCopies;  // copies until turn() repeats
+
+    static __device__ __forceinline__ int turn(int r) { return kChunks >= 16 ? r & 15 : r >> 1 & 7; }
+
+    // channels 8 i on of row r, for the product's operand
+    static __device__ __forceinline__ typename Eight<T>::V row(const char *s, int r, int i)
+    {
+        if constexpr (sizeof(T) == 2) {
+            return *reinterpret_cast<const typename Eight<T>::V *>(s + r * kRow + (i ^ turn(r)) * 16);
+        } else {
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(s + r * kRow + (2 * i ^ turn(r)) * 16);
+            const f32x4 hi = *reinterpret_cast<const f32x4 *>(s + r * kRow + ((2 * i + 1) ^ turn(r)) * 16);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+
+    // channel 16 n + lane % 16 of positions 4 (lane / 16) + 0..3 and those + 16
+    static __device__ __forceinline__ typename Eight<T>::V column(const char *s, int n, int lane)
+    {
+        typename Eight<T>::V v;
+        if constexpr (sizeof(T) == 2) {
+            typedef short S4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) S4 *P;
+            const int r = lane / 4;
+            const char *p = s + r * kRow + ((2 * n + lane / 2 % 2) ^ turn(r)) * 16 + lane % 2 * 8;
+            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
+            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * kRow));
+            const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            v = __builtin_bit_cast(typename Eight<T>::V, both);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = lane / 16 * 4 + j;
+                const char *p = s + r * kRow + ((4 * n + lane / 4 % 4) ^ turn(r)) * 16 + lane % 4 * 4;
+                v[j] = *reinterpret_cast<const float *>(p);
+                v[4 + j] = *reinterpret_cast<const float *>(p + 16 * kRow);
+            }
+        }
+        return v;
+    }
+
+    // element (r, channel)
+    static __device__ __forceinline__ float at(const char *s, int r, int channel)
+    {
+        const int byte = channel * (int)sizeof(T);
+        return (float)*reinterpret_cast<const T *>(s + r * kRow + (byte / 16 ^ turn(r)) * 16 + byte % 16);
+    }
+};
+
+// Each lane's 16 bytes at base + off to the wave's 1 KiB from `to` on.  Written out,
+// because the compiler would wait for every such copy before the next read of LDS; the
+// wave waits for a tile's when it begins it.  m0, where `to` is passed, is read one wait
+// state after it is set, scalar operands five after a vector instruction that may
+// have made them.
+__device__ __forceinline__ void copy16(char *to, const char *base, unsigned off)
+{
+    const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(at), "v"(off), "s"(base) : "memory");
+}
+
+// The same attention where K's and V's rows are whole chunks of 16 bytes and a copy's
+// rows lie in one page.  A wave's tiles go from memory straight to its own part of
+// LDS, one on its way while the one before is worked on; nothing waits for another
+// wave until their sums are joined.
+template <typename T, int D, int NQ, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
+{
+    typedef typename Eight<T>::V V8;
+    typedef Copied<T, D> S;
+    constexpr int C = D / 32, N = D / 16, ROWS = 16 * NQ, THREADS = WAVES * 64, STEP = WAVES * kTile;
+    constexpr int kStage = 2 * S::kBytes, kWave = 2 * kStage;  // K and V, twice
+    static_assert(ROWS * (D + 4) * 4 <= kWave, "a wave's sums fit its stages");
+    __shared__ __align__(16) char s_raw[WAVES * kWave];
+    __shared__ Line<THREADS> s_line;
+    __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
+    char *const s_own = s_raw + wave * kWave;
+
+    const int64_t total = measure(p, s_line);
+    const int64_t each = share(total, gridDim.x), active = (total + each - 1) / each;
+    if ((int64_t)blockIdx.x >= active) return;
+    const int64_t rank = rank_of(blockIdx.x, active), share_begin = rank * each;
+    const int64_t share_end = share_begin + each < total ? share_begin + each : total;
+    int b;
+    int64_t base;
+    find(p, s_line, share_begin, b, base);
+    Sequence seq = sequence_of(p, b);
+
+    // what a lane copies: a row of each copy, and its chunk of it
+    const int chunks = p.d * (int)sizeof(T) / 16;
+    unsigned key_off[S::kTurns], value_off[S::kTurns];
+    bool copies[S::kTurns];
+#pragma unroll
+    for (int t = 0; t < S::kTurns; ++t) {
+        const int r = lane / S::kChunks, c = lane % S::kChunks ^ S::turn(t * S::kRows + r);
+        key_off[t] = (unsigned)(r * (int)p.key_place * (int)sizeof(T) + c * 16);
+        value_off[t] = (unsigned)(r * (int)p.value_place * (int)sizeof(T) + c * 16);
+        copies[t] = c < chunks;
+    }
+    // chunks that no copy writes are multiplied by zeros
+    if (p.d != D)
+        for (int i = threadIdx.x; i < WAVES * kWave / 16; i += THREADS) reinterpret_cast<f32x4 *>(s_raw)[i] = (f32x4)0.f;
+    bool zeroed = p.d != D;
+
+    for (int64_t u = share_begin; u < share_end;) {
+        while (u >= base + seq.cost(p.shape.heads)) {
+            base += seq.cost(p.shape.heads);
+            seq = sequence_of(p, ++b);
+        }
+        const int64_t item = (u - base) / seq.units, item_begin = base + item * seq.units, part_begin = u;
+        const int64_t part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
+        const int head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * ROWS;
+        const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
+        const int begin = (int)((part_begin - item_begin) * p.shape.unit);
+        const int end = p.shape.unit && (part_end - item_begin) * p.shape.unit < seq.keys
+                            ? (int)((part_end - item_begin) * p.shape.unit) : (int)seq.keys;
+        const int length = (int)seq.length;
+        const char *key = (const char *)((const T *)p.key + head * p.key_head);
+        const char *value = (const char *)((const T *)p.value + head * p.value_head);
+        const int32_t *table = p.table + b * p.table_row;
+
+        // lane r and r + 32 have row r of a tile: whether it holds something, and where it lies
+        auto page_at = [&](int j) {
+            int page = -1;
+            if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
+            return (unsigned)page < (uint64_t)p.pages ? page : -1;
+        };
+        auto copy = [&](int at, int page, char *to) {
+            const int j = at + lane % 32;
+            const int place = p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
+            const int64_t k = (page * p.key_page + place * p.key_place) * (int)sizeof(T);
+            const int64_t v = (page * p.value_page + place * p.value_place) * (int)sizeof(T);
+            auto from = [&](const char *first, int64_t off, int r) {
+                const unsigned lo = __builtin_amdgcn_readlane((int)off, r), hi = __builtin_amdgcn_readlane((int)(off >> 32), r);
+                return first + (int64_t)((uint64_t)hi << 32 | lo);
+            };
+            const unsigned there = (unsigned)__ballot(page >= 0);
+            // all of K, then all of V
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                if (there >> (i * S::kRows) & 1) {
+                    const char *at = from(key, k, i * S::kRows);
+                    if (copies[i % S::kTurns]) copy16(to + i * 1024, at, key_off[i % S::kTurns]);
+                }
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                if (there >> (i * S::kRows) & 1) {
+                    const char *at = from(value, v, i * S::kRows);
+                    if (copies[i % S::kTurns]) copy16(to + S::kBytes + i * 1024, at, value_off[i % S::kTurns]);
+                }
+        };
+        int at = begin + wave * kTile, stage = 0;
+        int page = page_at(at + lane % 32);
+        if (zeroed) {
+            __syncthreads();  // the zeros are in place
+            zeroed = false;
+        }
+        if (at < end) copy(at, page, s_own);
+        int next = page_at(at + STEP + lane % 32);
+
+        // the rows, and which of the sequence's tokens each sees
+        V8 q[NQ][C];
+        uint64_t word[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int r = n * 16 + col;
+            word[n] = 0;
+            const T *from = (const T *)p.q;
+            if (r < rows) {
+                const RowAt row = row_at(p, seq, head, row0 + r);
+                from += row.m * p.q_token + row.h * p.q_head;
+                word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) q[n][c] = get8(from + c * 32 + g * 8, r < rows ? p.d - c * 32 - g * 8 : 0);
+        }
+        f32x4 o[NQ][N];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            m[n] = -__builtin_inff();
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
+        }
+
+        for (; at < end; at += STEP, stage ^= 1) {
+            char *const s_k = s_own + stage * kStage, *const s_v = s_k + S::kBytes;
+            const unsigned there = (unsigned)__ballot(page >= 0);
+            // this tile is here, and the other stage has been read
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (at + STEP < end) copy(at + STEP, next, s_own + (stage ^ 1) * kStage);
+            page = next;
+            next = page_at(at + 2 * STEP + lane % 32);
+
+            if (there != ~0u) {
+                // V's rows that hold nothing: zeros, whatever was copied with them
+                for (int i = lane; i < S::kBytes / 16; i += 64)
+                    if (!(there >> (i / S::kChunks) & 1)) reinterpret_cast<f32x4 *>(s_v)[i] = (f32x4)0.f;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+            const bool drafted = at + kTile > length;
+            bool odd = false;
+            if (drafted) {
+                // a token's NaN or infinity: some rows may not see it
+                for (int i = lane; i < S::kBytes / 16; i += 64) {
+                    typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+                    const V v = reinterpret_cast<const V *>(s_v)[i];
+#pragma unroll
+                    for (int j = 0; j < 16 / (int)sizeof(T); ++j) odd |= !(fabsf((float)v[j]) < __builtin_inff());
+                }
+                odd = __any(odd);
+            }
+
+            f32x4 x[NQ][2];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = (f32x4)0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const V8 k = S::row(s_k, h * 16 + col, c * 4 + g);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) x[n][h] = product(k, q[n][c], x[n][h]);
+                }
+
+            V8 weight[NQ];
+            unsigned seen[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                seen[n] = there;
+                if (drafted) {
+                    const int off = length - at;  // the tile's first token
+                    seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
+                }
+                float most = -__builtin_inff(), s[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[e] = x[n][e / 4][e % 4] * p.scale;
+                    if (p.cap != 0.f) s[e] = tanh_of(s[e]) * p.cap;
+                }
+                if (drafted || there != ~0u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) s[e] = -__builtin_inff();
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, s[e]);
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                // the sums' origin moves only where a weight would pass 2^8: they stay in range,
+                // and nearly no tile has them multiplied
+                if (__any(most > m[n] + 8.f)) {
+                    most = fmaxf(most, m[n]);
+                    const float shrink = __builtin_amdgcn_exp2f(m[n] - (most == -__builtin_inff() ? 0.f : most));
+                    m[n] = most;
+                    l[n] *= shrink;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) o[n][i] *= shrink;
+                }
+                const float origin = m[n] == -__builtin_inff() ? 0.f : m[n];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[e] = __builtin_amdgcn_exp2f(s[e] - origin);
+                    l[n] += s[e];
+                    weight[n][e] = (T)s[e];
+                }
+            }
+            if (!odd) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const V8 v = S::column(s_v, i, lane);
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][i] = product(v, weight[n], o[n][i]);
+                }
+            } else {
+                // a NaN or an infinity reaches the rows that see it and no other: position by position
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    for (int from = 0; from < 4; ++from) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int j = e / 4 * 16 + from * 4 + e % 4;
+                            const float w = __shfl((float)weight[n][e], from * 16 + col);
+                            const bool sees = seen[n] >> j & 1;
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    const float v = S::at(s_v, j, i * 16 + g * 4 + c);
+                                    o[n][i][c] += sees ? w * v : 0.f;
+                                }
+                        }
+                    }
+            }
+        }
+
+        // the waves' sums together
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        float *s_o = reinterpret_cast<float *>(s_own);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+            if (g == 0) {
+                s_m[wave][n * 16 + col] = m[n];
+                s_l[wave][n * 16 + col] = l[n];
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = o[n][i];
+        }
+        __syncthreads();
+        const bool whole = part_begin == item_begin && part_end == item_begin + seq.units;
+        float *part = whole ? nullptr : part_of<D>(p, rank, slot_of(part_begin, share_begin));
+        for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4;
+            float most = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) most = fmaxf(most, s_m[w][r]);
+            f32x4 sum = (f32x4)0.f;
+            float all = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = weight_of(s_m[w][r], most);
+                sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kWave + (r * (D + 4) + c) * 4) * f;
+                all += s_l[w][r] * f;
+            }
+            if (whole) {
+                if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
+            } else {
+                *reinterpret_cast<f32x4 *>(part + r * D + c) = sum;
+                if (c == 0) {
+                    part[ROWS * D + r] = most;
+                    part[ROWS * (D + 1) + r] = all;
+                }
+            }
+        }
+        __syncthreads();
+        if (p.d != D && part_end < share_end) {
+            for (int i = threadIdx.x; i < WAVES * kWave / 16; i += THREADS) reinterpret_cast<f32x4 *>(s_raw)[i] = (f32x4)0.f;
+            zeroed = true;
+        }
+        u = part_end;
+    }
+}
+
 // Joins the parts of items that more than one work-group had, in the order of the
 // line.  A work-group for each border between shares; the first border in an item
 // does it.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(Args p, int groups)
 {
-    __shared__ Line s_line;
+    __shared__ Line<kThreads> s_line;
     const int64_t total = measure(p, s_line);
     const int64_t each = share(total, groups), border = ((int64_t)blockIdx.x + 1) * each;
     if (border >= total) return;
@@ -539,52 +901,71 @@ int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct Form {
     int D, nq;
+    int unit;        // positions that a work-group's waves have in work
     int64_t groups;  // work-groups
     size_t bytes;    // of the workspace
-    bool one_unit;   // no item has more than one unit
 };
 
-// The form of a call, and the work-groups that the card holds at once.
-Form form_of(int64_t d, int64_t group, int64_t heads, int64_t B, int64_t capacity, int64_t most)
+// Waves of stream_kernel: what a CU's LDS holds of their stages.
+constexpr int stream_waves(int row_bytes) { return row_bytes >= 1024 ? 1 : row_bytes >= 512 ? 2 : 4; }
+
+// The form of a call: the work-groups that the card holds at once.
+Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64_t capacity, int64_t most, bool copied)
 {
     Form f;
     f.D = padded(d);
+    const int waves = copied ? stream_waves(f.D * size) : kWaves;
     f.nq = most * group > 16 && f.D <= 128 ? 2 : 1;
+    f.unit = waves * kTile;
     const int64_t items = B * heads * ((most * group + 16 * f.nq - 1) / (16 * f.nq));
-    const int64_t units = (capacity + kUnit - 1) / kUnit;
-    f.one_unit = units <= 1;
-    const int64_t line = items > ((int64_t)1 << 40) / (units < 1 ? 1 : units) ? (int64_t)1 << 40 : items * (units < 1 ? 1 : units);
-    f.groups = 256 * (f.D == 256 ? 1 : f.nq == 2 ? 2 : 3);
+    const int64_t units = capacity <= f.unit ? 1 : (capacity + f.unit - 1) / f.unit;
+    const int64_t line = items > ((int64_t)1 << 40) / units ? (int64_t)1 << 40 : items * units;
+    if (copied)
+        f.groups = 256 * (f.D * size <= 128 ? 2 : 1);
+    else
+        f.groups = 256 * (f.D == 256 ? 1 : f.nq == 2 ? 2 : 3);
     if (f.groups > line) f.groups = line;
-    f.bytes = f.one_unit ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
+    f.bytes = units == 1 ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
     return f;
 }
 
-template <typename T, int D, int NQ>
-int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
+template <typename T, int D>
+int join(const Args &a, const Form &f, bool joined, hipStream_t s)
 {
-    constexpr int kSum = 16 * NQ * (D + 4) * 4;
-    constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
-    // (a constant of the kernel, set at every call: no state is kept)
-    if (kWaves * kWave > 65536 - 8192 &&
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attention_kernel<T, D, NQ>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, kWaves * kWave) != hipSuccess)
-        return PK_ERR_LAUNCH;
-    hipLaunchKernelGGL((attention_kernel<T, D, NQ>), dim3((unsigned)f.groups), dim3(kThreads), kWaves * kWave, s, a);
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
-    if (joined && f.groups > 1) {
-        hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kThreads), 0, s, a, (int)f.groups);
-        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+    if (!joined || f.groups == 1) return PK_OK;
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kThreads), 0, s, a, (int)f.groups);
+    return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
+}
+
+template <typename T, int D, int NQ>
+int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s)
+{
+    if (copied) {
+        constexpr int WAVES = stream_waves(D * (int)sizeof(T));
+        hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((attention_kernel<T, D, NQ>), dim3((unsigned)f.groups), dim3(kThreads), 0, s, a);
     }
-    return PK_OK;
+    return join<T, D>(a, f, joined, s);
 }
 
 template <typename T>
-int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
+int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s)
 {
-    if (f.D == 64) return f.nq == 1 ? launch<T, 64, 1>(a, f, joined, s) : launch<T, 64, 2>(a, f, joined, s);
-    if (f.D == 128) return f.nq == 1 ? launch<T, 128, 1>(a, f, joined, s) : launch<T, 128, 2>(a, f, joined, s);
-    return launch<T, 256, 1>(a, f, joined, s);
+    if (f.D == 64) return f.nq == 1 ? launch<T, 64, 1>(a, f, copied, joined, s) : launch<T, 64, 2>(a, f, copied, joined, s);
+    if (f.D == 128) return f.nq == 1 ? launch<T, 128, 1>(a, f, copied, joined, s) : launch<T, 128, 2>(a, f, copied, joined, s);
+    return launch<T, 256, 1>(a, f, copied, joined, s);
+}
+
+// Whether K and V can be copied in whole chunks: 16-byte rows at 16-byte places, the
+// rows of a copy (up to 8) in one page and within 32-bit offsets of each other.
+bool can_copy(const pk_cache &c, int64_t d, int size)
+{
+    if (d * size % 16 || (uintptr_t)c.key % 16 || (uintptr_t)c.value % 16 || c.page_size % 8) return false;
+    for (int i = 0; i < 3; ++i)
+        if (c.key_stride[i] * size % 16 || c.value_stride[i] * size % 16) return false;
+    return c.key_stride[1] < 1 << 24 && c.value_stride[1] < 1 << 24;
 }
 
 }  // namespace
@@ -599,7 +980,10 @@ size_t pk_attention_tree_workspace_bytes(int dtype, int64_t d, int64_t q_heads, 
         B < 1 || B > kMostSize || P < 1 || P > kMostSize || page_size < 1 || page_size > kMostSize || most < 1 ||
         most > kMostTokens || P * page_size > kMostSize)
         return 0;
-    return form_of(d, q_heads / heads, heads, B, P * page_size, most).bytes;
+    // either form
+    const Form a = form_of(pk::dtype_size(dtype), d, q_heads / heads, heads, B, P * page_size, most, false);
+    const Form b = form_of(pk::dtype_size(dtype), d, q_heads / heads, heads, B, P * page_size, most, true);
+    return a.bytes > b.bytes ? a.bytes : b.bytes;
 }
 
 int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_cache *cache, const int32_t *page_table,
@@ -640,7 +1024,8 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     if ((uintptr_t)mask % 8) return api_invalid(13);
     if ((uintptr_t)lse % 4) return api_invalid(17);
     const int64_t heads = cache->heads, group = q->heads / heads;
-    const Form f = form_of(d, group, heads, B, P * cache->page_size, most);
+    const bool copied = can_copy(*cache, d, size);
+    const Form f = form_of(size, d, group, heads, B, P * cache->page_size, most, copied);
     const bool joined = f.bytes && workspace && workspace_bytes >= f.bytes;
     const Region in[7] = {of_heads(*q, M, d, size), of_cache(cache->key, cache->key_stride, *cache, d, size),
                           of_cache(cache->value, cache->value_stride, *cache, d, size),
@@ -680,7 +1065,7 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.value_place = cache->value_stride[1];
     a.value_head = cache->value_stride[2];
     a.pages = cache->pages;
-    a.shape = {M, P * cache->page_size, (int)heads, (int)group, (int)most, 16 * f.nq, joined ? kUnit : 0};
+    a.shape = {M, P * cache->page_size, (int)heads, (int)group, (int)most, 16 * f.nq, joined ? f.unit : 0};
     a.B = (int)B;
     a.d = (int)d;
     a.page_size = (int)cache->page_size;
@@ -690,8 +1075,8 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.scale = cap != 0.f ? scale / cap : scale * kLog2e;
     a.cap = cap * kLog2e;
     hipStream_t s = (hipStream_t)stream;
-    st = dtype == PK_F32 ? launch<float>(a, f, joined, s) : dtype == PK_BF16 ? launch<bf16>(a, f, joined, s) : launch<f16>(a, f, joined, s);
-    if (st == PK_OK) api_ran("attention_tree");
+    st = dtype == PK_F32 ? launch<float>(a, f, copied, joined, s) : dtype == PK_BF16 ? launch<bf16>(a, f, copied, joined, s) : launch<f16>(a, f, copied, joined, s);
+    if (st == PK_OK) api_ran(copied ? "attention_tree_copied" : "attention_tree_read");
     return st;
 }
 

@@ -1,6 +1,6 @@
 // pk_torch.cpp -- the tensor calls of binding.py (gemm, conv2d_fwd,
-// conv2d_winograd and the 8-bit operators) marshalled natively: torch tensors in, one C-ABI call on the
-// current stream, the output tensor out.
+// conv2d_winograd, the 8-bit and the attention operators) marshalled natively: torch tensors in, one
+// C-ABI call on the current stream, the output tensor out.
 //
 // Every pointer is read before the interpreter lock is released: data_ptr()
 // throws for a tensor without a storage, and an exception must not leave the
@@ -35,7 +35,9 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "../../include/pk.h"
 
@@ -56,6 +58,12 @@ decltype(&pk_gated_i8) f_gated_i8;
 decltype(&pk_dequantize_i8) f_dequantize_i8;
 decltype(&pk_gemm_i8_ws) f_gemm_i8;
 decltype(&pk_gemm_i8_workspace_bytes_for) f_gemm_i8_workspace_bytes;
+decltype(&pk_rope_qk) f_rope_qk;
+decltype(&pk_rope_qk_backward) f_rope_qk_backward;
+decltype(&pk_rope_qk_backward_workspace_bytes) f_rope_qk_backward_workspace_bytes;
+decltype(&pk_cache_append) f_cache_append;
+decltype(&pk_attention_tree) f_attention_tree;
+decltype(&pk_attention_tree_workspace_bytes) f_attention_tree_workspace_bytes;
 PyObject *f_check;  // binding._check(status, entry point): raises
 
 // The answer to a status other than PK_OK.
@@ -592,13 +600,324 @@ PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------- attention operators
+
+// A plain tensor of tokens x heads x channels, its channels contiguous.
+const at::Tensor *heads(PyObject *o, pk_heads *h)
+{
+    const at::Tensor *t = on_gpu(o);
+    if (!t || t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1)) return nullptr;
+    *h = {t->data_ptr(), t->size(1), t->stride(0), t->stride(1)};
+    return t;
+}
+
+// The same, of `like`'s type, device, tokens and channels.
+const at::Tensor *heads_like(PyObject *o, const at::Tensor &like, pk_heads *h)
+{
+    const at::Tensor *t = heads(o, h);
+    return t && t->scalar_type() == like.scalar_type() && t->device() == like.device() && t->size(0) == like.size(0) &&
+                   t->size(2) == like.size(2)
+               ? t : nullptr;
+}
+
+// An output of `like`'s shape: the caller's, or a new one.
+bool heads_out(PyObject *o, const at::Tensor &like, at::Tensor *t, pk_heads *h)
+{
+    if (o != Py_None) {
+        const at::Tensor *given = heads_like(o, like, h);
+        if (!given || given->size(1) != like.size(1)) return false;
+        *t = *given;
+        return true;
+    }
+    const int64_t H = like.size(1), d = like.size(2), row = std::max<int64_t>(H * d, 1), step = std::max<int64_t>(d, 1);
+    *t = fresh({like.size(0), H, d}, {row, step, 1}, like.scalar_type(), like);
+    *h = {t->data_ptr(), H, row, step};
+    return true;
+}
+
+bool pages_of(PyObject *key, PyObject *value, const at::Tensor &like, pk_cache *c)
+{
+    const at::Tensor *k = on_gpu(key), *v = on_gpu(value);
+    if (!k || !v || k->dim() != 4 || v->dim() != 4 || k->sizes() != v->sizes() || k->size(3) != like.size(2)) return false;
+    if (k->scalar_type() != like.scalar_type() || v->scalar_type() != like.scalar_type() || k->device() != like.device() ||
+        v->device() != like.device() || (k->size(3) > 1 && (k->stride(3) != 1 || v->stride(3) != 1)))
+        return false;
+    *c = {k->data_ptr(), v->data_ptr(), k->size(0), k->size(1), k->size(2),
+          {k->stride(0), k->stride(1), k->stride(2)}, {v->stride(0), v->stride(1), v->stride(2)}};
+    return true;
+}
+
+// Both None (*rot is NULL then), or positions and frequencies of these tokens.
+bool rotation(PyObject *positions, PyObject *frequencies, PyObject *layout, PyObject *amplitude, const at::Tensor &like,
+              pk_rotation *r, const pk_rotation **rot)
+{
+    *rot = nullptr;
+    if (!PyUnicode_CheckExact(layout)) return false;
+    r->interleaved = PyUnicode_CompareWithASCIIString(layout, "interleaved") == 0;
+    if (!r->interleaved && PyUnicode_CompareWithASCIIString(layout, "half") != 0) return false;
+    if (!as_float(amplitude, &r->amplitude)) return false;
+    if (positions == Py_None && frequencies == Py_None) return true;
+    const at::Tensor *f = on_gpu(frequencies), *p = vec(positions, like.size(0), at::kLong, like);
+    if (!f || !p || f->dim() != 1 || !vec(frequencies, f->size(0), at::kDouble, like) || 2 * f->size(0) > like.size(2)) return false;
+    r->positions = (const int64_t *)p->data_ptr();
+    r->frequencies = (const double *)f->data_ptr();
+    r->pairs = f->size(0);
+    *rot = r;
+    return true;
+}
+
+// The norms' weights, of one type: the heads' or fp32.
+struct Weights {
+    const at::Tensor *t[2];
+    const void *p[2];
+    int code;
+};
+
+bool weights(PyObject *q, PyObject *k, const at::Tensor &like, Weights *w)
+{
+    *w = {{nullptr, nullptr}, {nullptr, nullptr}, PK_F32};
+    PyObject *given[2] = {q, k};
+    for (int i = 0; i < 2; ++i) {
+        if (given[i] == Py_None) continue;
+        const at::Tensor *t = on_gpu(given[i]);
+        if (!t || (t->scalar_type() != like.scalar_type() && t->scalar_type() != at::kFloat)) return false;
+        if (!vec(given[i], like.size(2), t->scalar_type(), like)) return false;
+        const int code = dtype_code(t->scalar_type());
+        if ((w->t[0] || w->t[1]) && code != w->code) return false;
+        w->code = code;
+        w->t[i] = t;
+        w->p[i] = t->data_ptr();
+    }
+    return true;
+}
+
+// `given`, or the new tensor in its place; None where there is neither.
+PyObject *given_or_none(PyObject *given, at::Tensor &&t)
+{
+    if (given == Py_None && !t.defined()) Py_RETURN_NONE;
+    return given_or(given, std::move(t));
+}
+
+PyObject *tuple_of(std::initializer_list<PyObject *> parts)
+{
+    PyObject *t = PyTuple_New((Py_ssize_t)parts.size());
+    Py_ssize_t i = 0;
+    bool whole = t != nullptr;
+    for (PyObject *p : parts) {
+        if (!p) whole = false;
+        if (t)
+            PyTuple_SET_ITEM(t, i++, p);  // NULL is no value of a finished tuple: it is dropped below
+        else
+            Py_XDECREF(p);
+    }
+    if (!whole) Py_CLEAR(t);
+    return t;
+}
+
+// rope_qk(q, k, positions, frequencies, q_weight, k_weight, eps, layout, amplitude, q_out, k_out)
+PyObject *py_rope_qk(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    pk_heads hq, hk, oq, ok;
+    pk_rotation r;
+    const pk_rotation *rot;
+    Weights w;
+    float eps;
+    at::Tensor out_q, out_k;
+    if (nargs != 11 || !as_float(args[6], &eps) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *q = heads(args[0], &hq), *k = nullptr;
+    if (!q) Py_RETURN_NONE;
+    const int dt = dtype_code(q->scalar_type());
+    if (dt < 0 || !rotation(args[2], args[3], args[7], args[8], *q, &r, &rot) || !weights(args[4], args[5], *q, &w)) Py_RETURN_NONE;
+    if (args[1] != Py_None) {
+        k = heads_like(args[1], *q, &hk);
+        if (!k || !heads_out(args[10], *k, &out_k, &ok)) Py_RETURN_NONE;
+    } else if (args[5] != Py_None || args[10] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    if (!heads_out(args[9], *q, &out_q, &oq)) Py_RETURN_NONE;
+    const int64_t M = q->size(0), d = q->size(2);
+    const pk_heads *ph = k ? &hk : nullptr, *po = k ? &ok : nullptr;
+    const void *qw = w.p[0], *kw = w.p[1];
+    const int wt = w.code;
+    void *stream = stream_of(*q);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_rope_qk(dt, M, d, &hq, ph, rot, qw, kw, wt, eps, &oq, po, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_rope_qk");
+    return tuple_of({given_or(args[9], std::move(out_q)), given_or_none(args[10], std::move(out_k))});
+    END_HANDLE_TH_ERRORS
+}
+
+// rope_qk_backward(dq, dk, q, k, positions, frequencies, q_weight, k_weight, eps, layout, amplitude, q_grad, k_grad)
+PyObject *py_rope_qk_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    pk_heads hdq, hdk, hq, hk, gq, gk;
+    pk_rotation r;
+    const pk_rotation *rot;
+    Weights w;
+    float eps;
+    at::Tensor out_q, out_k, wgrad[2], own;
+    if (nargs != 13 || !as_float(args[8], &eps) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *dq = heads(args[0], &hdq), *dk = nullptr;
+    if (!dq) Py_RETURN_NONE;
+    const int dt = dtype_code(dq->scalar_type());
+    if (dt < 0 || !rotation(args[4], args[5], args[9], args[10], *dq, &r, &rot) || !weights(args[6], args[7], *dq, &w)) Py_RETURN_NONE;
+    if (args[1] != Py_None) {
+        dk = heads_like(args[1], *dq, &hdk);
+        if (!dk || !heads_out(args[12], *dk, &out_k, &gk)) Py_RETURN_NONE;
+    } else if (args[7] != Py_None || args[12] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    if (!heads_out(args[11], *dq, &out_q, &gq)) Py_RETURN_NONE;
+    // the inputs, where a weight needs them
+    const pk_heads *pq = nullptr, *pk = nullptr;
+    if (w.t[0]) {
+        const at::Tensor *q = heads_like(args[2], *dq, &hq);
+        if (!q || q->size(1) != dq->size(1)) Py_RETURN_NONE;
+        pq = &hq;
+    }
+    if (w.t[1]) {
+        const at::Tensor *k = heads_like(args[3], *dk, &hk);
+        if (!k || k->size(1) != dk->size(1)) Py_RETURN_NONE;
+        pk = &hk;
+    }
+    const int64_t M = dq->size(0), d = dq->size(2);
+    void *wg[2] = {nullptr, nullptr}, *ws = nullptr;
+    for (int i = 0; i < 2; ++i) {
+        if (!w.t[i]) continue;
+        wgrad[i] = fresh({d}, {1}, w.t[i]->scalar_type(), *dq);
+        wg[i] = wgrad[i].data_ptr();
+    }
+    size_t bytes = w.t[0] || w.t[1] ? f_rope_qk_backward_workspace_bytes(M, d) : 0;
+    if (bytes) {
+        own = fresh({(int64_t)(bytes / 4)}, {1}, at::kFloat, *dq);
+        ws = own.data_ptr();
+    }
+    const pk_heads *pdk = dk ? &hdk : nullptr, *pgk = dk ? &gk : nullptr;
+    const void *qw = w.p[0], *kw = w.p[1];
+    const int wt = w.code;
+    void *gqw = wg[0], *gkw = wg[1], *stream = stream_of(*dq);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_rope_qk_backward(dt, M, d, &hdq, pdk, pq, pk, rot, qw, kw, wt, eps, &gq, pgk, gqw, gkw, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_rope_qk_backward");
+    return tuple_of({given_or(args[11], std::move(out_q)), given_or_none(args[12], std::move(out_k)),
+                     given_or_none(Py_None, std::move(wgrad[0])), given_or_none(Py_None, std::move(wgrad[1]))});
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_append(k, v, key_cache, value_cache, slots, positions, frequencies, k_weight, q, q_weight, eps, layout, amplitude, q_out):
+// (q_out,), which tells a call without queries from one that was not made
+PyObject *py_cache_append(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    pk_heads hq, hk, hv, oq;
+    pk_cache cache;
+    pk_rotation r;
+    const pk_rotation *rot;
+    Weights w;
+    float eps;
+    at::Tensor out_q;
+    if (nargs != 14 || !as_float(args[10], &eps) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *k = heads(args[0], &hk), *q = nullptr;
+    if (!k) Py_RETURN_NONE;
+    const int dt = dtype_code(k->scalar_type());
+    const at::Tensor *v = heads_like(args[1], *k, &hv);
+    if (dt < 0 || !v || v->size(1) != k->size(1) || !pages_of(args[2], args[3], *k, &cache) || cache.heads != k->size(1)) Py_RETURN_NONE;
+    const at::Tensor *slots = vec(args[4], k->size(0), at::kLong, *k);
+    if (!slots || !rotation(args[5], args[6], args[11], args[12], *k, &r, &rot) || !weights(args[9], args[7], *k, &w)) Py_RETURN_NONE;
+    if (args[8] != Py_None) {
+        q = heads_like(args[8], *k, &hq);
+        if (!q || !heads_out(args[13], *q, &out_q, &oq)) Py_RETURN_NONE;
+    } else if (args[9] != Py_None || args[13] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    const int64_t M = k->size(0), d = k->size(2), *at = (const int64_t *)slots->data_ptr();
+    const pk_heads *ph = q ? &hq : nullptr, *po = q ? &oq : nullptr;
+    const void *qw = w.p[0], *kw = w.p[1];
+    const int wt = w.code;
+    void *stream = stream_of(*k);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_cache_append(dt, M, d, ph, &hk, &hv, rot, qw, kw, wt, eps, po, &cache, at, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_cache_append");
+    return tuple_of({given_or_none(args[13], std::move(out_q))});
+    END_HANDLE_TH_ERRORS
+}
+
+// attention_tree(q, key_cache, value_cache, page_table, lengths, starts, most, mask, scale, cap, out, lse, workspace)
+PyObject *py_attention_tree(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    pk_heads hq, ho;
+    pk_cache cache;
+    int64_t most, ld_table, ld_lse = 0;
+    float scale, cap;
+    at::Tensor out, sums, own;
+    if (nargs != 13 || !as_int(args[6], &most) || !as_float(args[9], &cap) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor *q = heads(args[0], &hq);
+    if (!q) Py_RETURN_NONE;
+    const int dt = dtype_code(q->scalar_type());
+    if (dt < 0 || !pages_of(args[1], args[2], *q, &cache)) Py_RETURN_NONE;
+    const int64_t M = q->size(0), Hq = q->size(1), d = q->size(2);
+    if (args[8] == Py_None)
+        scale = (float)std::pow((double)std::max<int64_t>(d, 1), -0.5);
+    else if (!as_float(args[8], &scale))
+        Py_RETURN_NONE;
+    const at::Tensor *table = on_gpu(args[3]);
+    if (!table || table->scalar_type() != at::kInt || table->device() != q->device() || (ld_table = ld_2d(*table)) < 0) Py_RETURN_NONE;
+    const int64_t B = table->size(0), P = table->size(1);
+    const at::Tensor *lengths = vec(args[4], B, at::kInt, *q), *starts = vec(args[5], B + 1, at::kInt, *q), *mask = nullptr;
+    if (!lengths || !starts || (args[7] != Py_None && !(mask = vec(args[7], M, at::kLong, *q)))) Py_RETURN_NONE;
+    if (!heads_out(args[10], *q, &out, &ho)) Py_RETURN_NONE;
+    const bool none = args[11] == Py_None || args[11] == Py_False, made = args[11] == Py_True;
+    if (made) {
+        sums = fresh_matrix(M, Hq, at::kFloat, *q);
+        ld_lse = std::max<int64_t>(Hq, 1);
+    } else if (!none) {
+        const at::Tensor *t = on_gpu(args[11]);
+        if (!t || t->scalar_type() != at::kFloat || (ld_lse = ld_2d(*t)) < 0 || !same_shape(*t, M, Hq, *q)) Py_RETURN_NONE;
+        sums = *t;
+    }
+    void *ws = nullptr;
+    size_t bytes = 0;
+    if (args[12] != Py_None) {
+        const at::Tensor *t = plain(args[12]);
+        if (!t || !t->is_contiguous() || t->device() != q->device()) Py_RETURN_NONE;
+        ws = t->data_ptr();
+        bytes = (size_t)t->numel() * 4;
+    } else if ((bytes = f_attention_tree_workspace_bytes(dt, d, Hq, cache.heads, B, P, cache.page_size, most)) != 0) {
+        own = fresh({(int64_t)(bytes / 4)}, {1}, at::kFloat, *q);
+        ws = own.data_ptr();
+    }
+    const int32_t *pt = (const int32_t *)table->data_ptr(), *pl = (const int32_t *)lengths->data_ptr(),
+                  *ps = (const int32_t *)starts->data_ptr();
+    const uint64_t *pm = mask ? (const uint64_t *)mask->data_ptr() : nullptr;
+    float *lse = none ? nullptr : (float *)sums.data_ptr();
+    void *stream = stream_of(*q);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_attention_tree(dt, M, d, &hq, &cache, pt, B, P, ld_table, pl, ps, most, pm, scale, cap, &ho, lse, ld_lse, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PK_OK) return refused(st, "pk_attention_tree");
+    PyObject *o = given_or(args[10], std::move(out));
+    if (none || !o) return o;
+    return tuple_of({o, given_or(made ? Py_None : args[11], std::move(sums))});
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses, check): the entry points above, in their order, and the
 // function that raises for a status.
 PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    constexpr int kEntries = 14;
+    constexpr int kEntries = 20;
     if (nargs != kEntries + 1) {
-        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of fourteen entry points and a function");
+        PyErr_SetString(PyExc_TypeError, "bind takes the addresses of twenty entry points and a function");
         return nullptr;
     }
     void *p[kEntries];
@@ -623,6 +942,12 @@ PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     f_dequantize_i8 = (decltype(f_dequantize_i8))p[11];
     f_gemm_i8 = (decltype(f_gemm_i8))p[12];
     f_gemm_i8_workspace_bytes = (decltype(f_gemm_i8_workspace_bytes))p[13];
+    f_rope_qk = (decltype(f_rope_qk))p[14];
+    f_rope_qk_backward = (decltype(f_rope_qk_backward))p[15];
+    f_rope_qk_backward_workspace_bytes = (decltype(f_rope_qk_backward_workspace_bytes))p[16];
+    f_cache_append = (decltype(f_cache_append))p[17];
+    f_attention_tree = (decltype(f_attention_tree))p[18];
+    f_attention_tree_workspace_bytes = (decltype(f_attention_tree_workspace_bytes))p[19];
     Py_INCREF(args[kEntries]);
     Py_XSETREF(f_check, args[kEntries]);
     Py_RETURN_NONE;
@@ -638,6 +963,10 @@ PyMethodDef kMethods[] = {
     {"gated_i8", (PyCFunction)(void (*)(void))py_gated_i8, METH_FASTCALL, nullptr},
     {"dequantize_i8", (PyCFunction)(void (*)(void))py_dequantize_i8, METH_FASTCALL, nullptr},
     {"gemm_i8", (PyCFunction)(void (*)(void))py_gemm_i8, METH_FASTCALL, nullptr},
+    {"rope_qk", (PyCFunction)(void (*)(void))py_rope_qk, METH_FASTCALL, nullptr},
+    {"rope_qk_backward", (PyCFunction)(void (*)(void))py_rope_qk_backward, METH_FASTCALL, nullptr},
+    {"cache_append", (PyCFunction)(void (*)(void))py_cache_append, METH_FASTCALL, nullptr},
+    {"attention_tree", (PyCFunction)(void (*)(void))py_attention_tree, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
