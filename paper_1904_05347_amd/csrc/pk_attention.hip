@@ -140,76 +140,115 @@ __device__ __forceinline__ float tanh_of(float x)
 
 constexpr int kThreads = kWaves * 64;
 
-template <int THREADS>
-struct Line {
-    int64_t ends[THREADS];  // units up to the end of each work-item's sequences
-    int64_t base;           // of the sequence found
-    int b;
-    int64_t waves[THREADS / 64];
-};
-
 __device__ __forceinline__ Sequence sequence_of(const Args &p, int b)
 {
     return sequence(p.shape, p.starts[b], p.starts[b + 1], p.lengths[b]);
 }
 
-// Units of the whole call.  Each work-item adds up its own run of sequences.
-template <int THREADS>
-__device__ __forceinline__ int64_t measure(const Args &p, Line<THREADS> &s)
+__device__ __forceinline__ unsigned scan(unsigned v)
 {
-    const int t = threadIdx.x, run = (p.B + THREADS - 1) / THREADS;
-    int64_t sum = 0;
-    for (int b = t * run; b < (t + 1) * run && b < p.B; ++b) sum += sequence_of(p, b).cost(p.shape.heads);
+    const int lane = threadIdx.x % 64;
+#pragma unroll
     for (int o = 1; o < 64; o *= 2) {
-        const int64_t v = __shfl_up(sum, o);
-        if (t % 64 >= o) sum += v;
+        const unsigned w = __shfl_up(v, o);
+        if (lane >= o) v += w;
     }
-    if (t % 64 == 63) s.waves[t / 64] = sum;
-    __syncthreads();
-    int64_t before = 0, total = 0;
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < t / 64) before += s.waves[w];
-        total += s.waves[w];
-    }
-    s.ends[t] = before + sum;
-    __syncthreads();
-    return total;
+    return v;
 }
 
-// The sequence that has unit u < total, and the units before it.
+// All sequences.  Up to 64 of them are a lane's each, and every wave knows them
+// without waiting for another (a call of one token: two barriers and the reading of
+// its sequence's indices less); of more, each work-item adds up its own run.
 template <int THREADS>
-__device__ __forceinline__ void find(const Args &p, Line<THREADS> &s, int64_t u, int &b, int64_t &base)
-{
-    const int t = threadIdx.x, run = (p.B + THREADS - 1) / THREADS;
-    const int64_t before = t ? s.ends[t - 1] : 0;
-    if (u >= before && u < s.ends[t]) {
-        int64_t at = before;
-        int i = t * run;
-        for (;; ++i) {
-            const int64_t c = sequence_of(p, i).cost(p.shape.heads);
-            if (u < at + c) break;
-            at += c;
+struct Line {
+    struct Shared {
+        unsigned ends[THREADS], waves[THREADS / 64], base;
+        int b;
+    };
+    const Args &p;
+    Shared &s;
+    const bool few;
+    Sequence mine;
+    unsigned end;  // of this lane's sequence
+    unsigned total;
+
+    __device__ __forceinline__ Line(const Args &args, Shared &shared) : p(args), s(shared), few(args.B <= 64)
+    {
+        const int t = threadIdx.x, lane = t % 64;
+        if (few) {
+            mine = sequence(p.shape, 0, 0, 0);
+            if (lane < p.B) mine = sequence_of(p, lane);
+            end = scan(mine.cost(p.shape.heads));
+            total = __builtin_amdgcn_readlane(end, 63);
+            return;
         }
-        s.b = i;
-        s.base = at;
+        const int run = (p.B + THREADS - 1) / THREADS;
+        unsigned sum = 0;
+        for (int b = t * run; b < (t + 1) * run && b < p.B; ++b) sum += sequence_of(p, b).cost(p.shape.heads);
+        end = scan(sum);
+        if (lane == 63) s.waves[t / 64] = end;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < t / 64) end += s.waves[w];
+            total += s.waves[w];
+        }
+        s.ends[t] = end;
+        __syncthreads();
     }
-    __syncthreads();
-    b = __builtin_amdgcn_readfirstlane(s.b);
-    base = s.base;
-}
+    // sequence b's indices
+    __device__ __forceinline__ Sequence get(int b) const
+    {
+        if (!few) return sequence_of(p, b);
+        Sequence q;
+        q.first = __builtin_amdgcn_readlane(mine.first, b);
+        q.tokens = __builtin_amdgcn_readlane(mine.tokens, b);
+        q.length = __builtin_amdgcn_readlane(mine.length, b);
+        q.keys = __builtin_amdgcn_readlane(mine.keys, b);
+        q.groups = __builtin_amdgcn_readlane(mine.groups, b);
+        q.units = __builtin_amdgcn_readlane(mine.units, b);
+        return q;
+    }
+    // the sequence that has unit u < total, and the units before it
+    __device__ __forceinline__ void find(unsigned u, int &b, unsigned &base) const
+    {
+        const int t = threadIdx.x;
+        if (few) {
+            b = __builtin_ctzll(__ballot(u < end));
+            base = b ? __builtin_amdgcn_readlane(end, b - 1) : 0;
+            return;
+        }
+        const unsigned before = t ? s.ends[t - 1] : 0;
+        if (u >= before && u < end) {
+            unsigned at = before;
+            int i = t * ((p.B + THREADS - 1) / THREADS);
+            for (;; ++i) {
+                const unsigned c = sequence_of(p, i).cost(p.shape.heads);
+                if (u < at + c) break;
+                at += c;
+            }
+            s.b = i;
+            s.base = at;
+        }
+        __syncthreads();
+        b = __builtin_amdgcn_readfirstlane(s.b);
+        base = __builtin_amdgcn_readfirstlane(s.base);
+    }
+};
 
 // The work-group's number on the line: neighbours on it share an XCD's L2.
-__device__ __forceinline__ int64_t rank_of(int64_t block, int64_t active)
+__device__ __forceinline__ unsigned rank_of(unsigned block, unsigned active)
 {
-    const int64_t x = block % 8, extra = active % 8;
+    const unsigned x = block % 8, extra = active % 8;
     return x * (active / 8) + (x < extra ? x : extra) + block / 8;
 }
 
 // A part's place in the workspace: `rows` x D sums, then maxima and sums of exponentials.
 template <int D>
-__device__ __forceinline__ float *part_of(const Args &p, int64_t group, int slot)
+__device__ __forceinline__ float *part_of(const Args &p, unsigned group, int slot)
 {
-    return p.parts + (group * 2 + slot) * ((int64_t)p.shape.rows * (D + 2));
+    return p.parts + (((uint64_t)group * 2 + slot) * (D + 2) << p.shape.rows_shift);
 }
 
 // Row r of an item's group: its token and query head.
@@ -261,34 +300,33 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(Args p)
     constexpr int kSum = ROWS * (D + 4) * 4;  // a wave's sums
     constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
     __shared__ __align__(16) char s_raw[kWaves * kWave];
-    __shared__ Line<kThreads> s_line;
+    __shared__ Line<kThreads>::Shared s_line;
     __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
     T *s_v = reinterpret_cast<T *>(s_raw + wave * kWave);
 
-    const int64_t total = measure(p, s_line);
-    const int64_t each = share(total, gridDim.x), active = (total + each - 1) / each;
-    if ((int64_t)blockIdx.x >= active) return;
-    const int64_t rank = rank_of(blockIdx.x, active), share_begin = rank * each;
-    const int64_t share_end = share_begin + each < total ? share_begin + each : total;
+    const Line<kThreads> line(p, s_line);
+    const unsigned total = line.total, each = share(total, gridDim.x), active = (total + each - 1) / each;
+    if (blockIdx.x >= active) return;
+    const unsigned rank = rank_of(blockIdx.x, active), share_begin = rank * each;
+    const unsigned share_end = share_begin + each < total ? share_begin + each : total;
     int b;
-    int64_t base;
-    find(p, s_line, share_begin, b, base);
-    Sequence seq = sequence_of(p, b);
+    unsigned base;
+    line.find(share_begin, b, base);
+    Sequence seq = line.get(b);
 
-    for (int64_t u = share_begin; u < share_end;) {
+    for (unsigned u = share_begin; u < share_end;) {
         while (u >= base + seq.cost(p.shape.heads)) {
             base += seq.cost(p.shape.heads);
-            seq = sequence_of(p, ++b);
+            seq = line.get(++b);
         }
-        const int64_t item = (u - base) / seq.units, item_begin = base + item * seq.units, part_begin = u;
-        const int64_t part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
-        const int head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * ROWS;
+        const unsigned item = (u - base) / (unsigned)seq.units, item_begin = base + item * seq.units, part_begin = u;
+        const unsigned part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
+        const int head = (int)(item / (unsigned)seq.groups), row0 = (int)(item % (unsigned)seq.groups) * ROWS;
         const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
-        const int begin = (int)((part_begin - item_begin) * p.shape.unit);
-        const int end = p.shape.unit && (part_end - item_begin) * p.shape.unit < seq.keys
-                            ? (int)((part_end - item_begin) * p.shape.unit) : (int)seq.keys;
-        const int length = (int)seq.length;
+        const int begin = p.shape.unit_shift < 0 ? 0 : (int)(part_begin - item_begin) << p.shape.unit_shift;
+        const int end = part_end == item_begin + seq.units ? seq.keys : (int)(part_end - item_begin) << p.shape.unit_shift;
+        const int length = seq.length;
         const T *key = (const T *)p.key + head * p.key_head, *value = (const T *)p.value + head * p.value_head;
         const int32_t *table = p.table + b * p.table_row;
 
@@ -583,20 +621,20 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     constexpr int kStage = 2 * S::kBytes, kWave = 2 * kStage;  // K and V, twice
     static_assert(ROWS * (D + 4) * 4 <= kWave, "a wave's sums fit its stages");
     __shared__ __align__(16) char s_raw[WAVES * kWave];
-    __shared__ Line<THREADS> s_line;
+    __shared__ typename Line<THREADS>::Shared s_line;
     __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     char *const s_own = s_raw + wave * kWave;
 
-    const int64_t total = measure(p, s_line);
-    const int64_t each = share(total, gridDim.x), active = (total + each - 1) / each;
-    if ((int64_t)blockIdx.x >= active) return;
-    const int64_t rank = rank_of(blockIdx.x, active), share_begin = rank * each;
-    const int64_t share_end = share_begin + each < total ? share_begin + each : total;
+    const Line<THREADS> line(p, s_line);
+    const unsigned total = line.total, each = share(total, gridDim.x), active = (total + each - 1) / each;
+    if (blockIdx.x >= active) return;
+    const unsigned rank = rank_of(blockIdx.x, active), share_begin = rank * each;
+    const unsigned share_end = share_begin + each < total ? share_begin + each : total;
     int b;
-    int64_t base;
-    find(p, s_line, share_begin, b, base);
-    Sequence seq = sequence_of(p, b);
+    unsigned base;
+    line.find(share_begin, b, base);
+    Sequence seq = line.get(b);
 
     // what a lane copies: a row of each copy, and its chunk of it
     const int chunks = p.d * (int)sizeof(T) / 16;
@@ -614,19 +652,18 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
         for (int i = threadIdx.x; i < WAVES * kWave / 16; i += THREADS) reinterpret_cast<f32x4 *>(s_raw)[i] = (f32x4)0.f;
     bool zeroed = p.d != D;
 
-    for (int64_t u = share_begin; u < share_end;) {
+    for (unsigned u = share_begin; u < share_end;) {
         while (u >= base + seq.cost(p.shape.heads)) {
             base += seq.cost(p.shape.heads);
-            seq = sequence_of(p, ++b);
+            seq = line.get(++b);
         }
-        const int64_t item = (u - base) / seq.units, item_begin = base + item * seq.units, part_begin = u;
-        const int64_t part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
-        const int head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * ROWS;
+        const unsigned item = (u - base) / (unsigned)seq.units, item_begin = base + item * seq.units, part_begin = u;
+        const unsigned part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
+        const int head = (int)(item / (unsigned)seq.groups), row0 = (int)(item % (unsigned)seq.groups) * ROWS;
         const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
-        const int begin = (int)((part_begin - item_begin) * p.shape.unit);
-        const int end = p.shape.unit && (part_end - item_begin) * p.shape.unit < seq.keys
-                            ? (int)((part_end - item_begin) * p.shape.unit) : (int)seq.keys;
-        const int length = (int)seq.length;
+        const int begin = p.shape.unit_shift < 0 ? 0 : (int)(part_begin - item_begin) << p.shape.unit_shift;
+        const int end = part_end == item_begin + seq.units ? seq.keys : (int)(part_end - item_begin) << p.shape.unit_shift;
+        const int length = seq.length;
         const char *key = (const char *)((const T *)p.key + head * p.key_head);
         const char *value = (const char *)((const T *)p.value + head * p.value_head);
         const int32_t *table = p.table + b * p.table_row;
@@ -857,41 +894,75 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     }
 }
 
-// Joins the parts of items that more than one work-group had, in the order of the
-// line.  A work-group for each border between shares; the first border in an item
-// does it.
+constexpr int kJoinThreads = 1024;
+
+// Joins the parts of items that more than one work-group had.  A work-group for each
+// border between shares; the first border in an item does it.  Its lanes take four
+// channels of a row each, and where there are fewer of them than lanes, the parts in
+// turn: many parts (a long sequence alone) would else be read one after the other.
+// Sums are made in an order that the call's sizes alone decide.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) join_kernel(Args p, int groups)
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned groups)
 {
-    __shared__ Line<kThreads> s_line;
-    const int64_t total = measure(p, s_line);
-    const int64_t each = share(total, groups), border = ((int64_t)blockIdx.x + 1) * each;
+    __shared__ typename Line<kJoinThreads>::Shared s_line;
+    __shared__ float s_sum[kJoinThreads][7];  // a maximum, a sum of exponentials, four of values; odd, for the banks
+    const Line<kJoinThreads> line(p, s_line);
+    const unsigned total = line.total, each = share(total, groups), border = (blockIdx.x + 1) * each;
     if (border >= total) return;
     int b;
-    int64_t base;
-    find(p, s_line, border, b, base);
-    const Sequence seq = sequence_of(p, b);
-    const int64_t item = (border - base) / seq.units, begin = base + item * seq.units, end = begin + seq.units;
-    if (begin == border || begin < border - each) return;
-    const int rows_max = p.shape.rows, head = (int)(item / seq.groups), row0 = (int)(item % seq.groups) * rows_max;
-    const int rows = seq.tokens * p.shape.group - row0 < rows_max ? seq.tokens * p.shape.group - row0 : rows_max;
-    const int64_t first = begin / each, last = (end - 1) / each;
-    auto part = [&](int64_t w) {
-        const int64_t from = w * each;
-        return part_of<D>(p, w, slot_of(from > begin ? from : begin, from));
+    unsigned base;
+    line.find(border, b, base);
+    const Sequence seq = line.get(b);
+    const unsigned item = (border - base) / (unsigned)seq.units, begin = base + item * seq.units, end = begin + seq.units;
+    if (begin == border || begin + each < border) return;
+    const int most_rows = 1 << p.shape.rows_shift, head = (int)(item / (unsigned)seq.groups);
+    const int row0 = (int)(item % (unsigned)seq.groups) * most_rows;
+    const int rows = seq.tokens * p.shape.group - row0 < most_rows ? seq.tokens * p.shape.group - row0 : most_rows;
+    const unsigned first = blockIdx.x, parts = (end - 1) / each - first + 1;
+    auto part = [&](unsigned i) {
+        const unsigned from = (first + i) * each;
+        return part_of<D>(p, first + i, slot_of(i ? from : begin, from));
     };
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+    // lanes to a part's sums: a power of two
+    int lanes = D / 4;
+    while (lanes < rows * (D / 4) && lanes < kJoinThreads) lanes *= 2;
+    const int turns = kJoinThreads / lanes, turn = threadIdx.x / lanes;
+    for (int i = threadIdx.x % lanes; i - (int)(threadIdx.x % lanes) < rows * (D / 4); i += lanes) {
         const int r = i / (D / 4), c = i % (D / 4) * 4;
-        float most = -__builtin_inff();
-        for (int64_t w = first; w <= last; ++w) most = fmaxf(most, part(w)[rows_max * D + r]);
+        const bool on = r < rows;
+        float most = -__builtin_inff(), all = 0.f;
         f32x4 sum = (f32x4)0.f;
-        float all = 0.f;
-        for (int64_t w = first; w <= last; ++w) {
-            const float *from = part(w), f = weight_of(from[rows_max * D + r], most);
-            sum += *reinterpret_cast<const f32x4 *>(from + r * D + c) * f;
-            all += from[rows_max * (D + 1) + r] * f;
+        if (on) {
+#pragma unroll 8
+            for (unsigned w = turn; w < parts; w += turns) most = fmaxf(most, part(w)[D * most_rows + r]);
+#pragma unroll 8
+            for (unsigned w = turn; w < parts; w += turns) {
+                const float *from = part(w), f = weight_of(from[D * most_rows + r], most);
+                sum += *reinterpret_cast<const f32x4 *>(from + r * D + c) * f;
+                all += from[(D + 1) * most_rows + r] * f;
+            }
         }
-        if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
+        // the turns' sums, two by two
+        float *mine = s_sum[threadIdx.x];
+        for (int o = turns / 2; o > 0; o /= 2) {
+            __syncthreads();
+            if (turn >= o && turn < 2 * o) {
+                mine[0] = most;
+                mine[1] = all;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mine[2 + j] = sum[j];
+            }
+            __syncthreads();
+            if (turn < o) {
+                const float *other = s_sum[threadIdx.x + o * lanes];
+                const float top = fmaxf(most, other[0]), f = weight_of(most, top), h = weight_of(other[0], top);
+                all = all * f + other[1] * h;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f + other[2 + j] * h;
+                most = top;
+            }
+        }
+        if (turn == 0 && on && c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
     }
 }
 
@@ -904,6 +975,7 @@ struct Form {
     int unit;        // positions that a work-group's waves have in work
     int64_t groups;  // work-groups
     size_t bytes;    // of the workspace
+    int64_t items;
 };
 
 // Waves of stream_kernel: what a CU's LDS holds of their stages.
@@ -919,13 +991,15 @@ Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64
     f.unit = waves * kTile;
     const int64_t items = B * heads * ((most * group + 16 * f.nq - 1) / (16 * f.nq));
     const int64_t units = capacity <= f.unit ? 1 : (capacity + f.unit - 1) / f.unit;
-    const int64_t line = items > ((int64_t)1 << 40) / units ? (int64_t)1 << 40 : items * units;
+    const bool divided = items <= kMostLine / units;  // else an item is a unit
+    const int64_t line = divided ? items * units : items;
+    f.items = items;
     if (copied)
         f.groups = 256 * (f.D * size <= 128 ? 2 : 1);
     else
         f.groups = 256 * (f.D == 256 ? 1 : f.nq == 2 ? 2 : 3);
     if (f.groups > line) f.groups = line;
-    f.bytes = units == 1 ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
+    f.bytes = units == 1 || !divided ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
     return f;
 }
 
@@ -934,7 +1008,7 @@ int join(const Args &a, const Form &f, bool joined, hipStream_t s)
 {
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
     if (!joined || f.groups == 1) return PK_OK;
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kThreads), 0, s, a, (int)f.groups);
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kJoinThreads), 0, s, a, (unsigned)f.groups);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 
@@ -1026,6 +1100,7 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     const int64_t heads = cache->heads, group = q->heads / heads;
     const bool copied = can_copy(*cache, d, size);
     const Form f = form_of(size, d, group, heads, B, P * cache->page_size, most, copied);
+    if (f.items > kMostLine) return PK_ERR_NOT_SUPPORTED;
     const bool joined = f.bytes && workspace && workspace_bytes >= f.bytes;
     const Region in[7] = {of_heads(*q, M, d, size), of_cache(cache->key, cache->key_stride, *cache, d, size),
                           of_cache(cache->value, cache->value_stride, *cache, d, size),
@@ -1065,7 +1140,9 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.value_place = cache->value_stride[1];
     a.value_head = cache->value_stride[2];
     a.pages = cache->pages;
-    a.shape = {M, P * cache->page_size, (int)heads, (int)group, (int)most, 16 * f.nq, joined ? f.unit : 0};
+    a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.nq == 2 ? 5 : 4, -1};
+    if (joined)
+        for (a.shape.unit_shift = 0; 1 << a.shape.unit_shift < f.unit;) ++a.shape.unit_shift;
     a.B = (int)B;
     a.d = (int)d;
     a.page_size = (int)cache->page_size;

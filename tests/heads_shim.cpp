@@ -33,8 +33,11 @@ void shim_tiling(int d, int pairs, int E, int64_t rows, int *out)
 void shim_sequence(int64_t M, int64_t capacity, int group, int most, int rows, int unit, int64_t start, int64_t end,
                    int64_t length, int64_t *out)
 {
-    const pk::attention::Shape s = {M, capacity, 1, group, most, rows, unit};
-    const pk::attention::Sequence q = pk::attention::sequence(s, start, end, length);
+    int rows_shift = 0, unit_shift = unit ? 0 : -1;
+    while (1 << rows_shift < rows) ++rows_shift;
+    while (unit && 1 << unit_shift < unit) ++unit_shift;
+    const pk::attention::Shape s = {(int)M, (int)capacity, 1, group, most, rows_shift, unit_shift};
+    const pk::attention::Sequence q = pk::attention::sequence(s, (int)start, (int)end, (int)length);
     out[0] = q.first;
     out[1] = q.length;
     out[2] = q.keys;
@@ -43,6 +46,6 @@ void shim_sequence(int64_t M, int64_t capacity, int group, int most, int rows, i
     out[5] = q.units;
 }
 
-int64_t shim_share(int64_t total, int64_t groups) { return pk::attention::share(total, groups); }
-int shim_slot(int64_t part, int64_t share) { return pk::attention::slot_of(part, share); }
+int64_t shim_share(int64_t total, int64_t groups) { return pk::attention::share((unsigned)total, (unsigned)groups); }
+int shim_slot(int64_t part, int64_t share) { return pk::attention::slot_of((unsigned)part, (unsigned)share); }
 }
