@@ -3,11 +3,10 @@
 //   o_i = sum_j p_ij v_j,  p_i the softmax over the j that row i sees of
 //   x_ij = c tanh(scale (q_i . k_j) / c)   (scale (q_i . k_j) without a cap c).
 //
-// One pass over the cache: each wave takes 32 positions at a time and keeps, for
-// each of its rows, the largest x so far, the sum of exponentials and the sum of
-// values weighted by them.  All rows that read one head of the cache (its tokens
-// times the query heads that share it) are columns of one product, so that K and V
-// are read once for them.
+// One pass over the cache, 32 positions at a time: for each row the largest x so far,
+// the sum of exponentials and the sum of values weighted by them.  All rows that
+// read one head of the cache (its tokens times the query heads that share it) are
+// columns of one product, so that K and V are read once for up to 128 of them.
 //
 // Lanes.  x^T = K q^T and o^T = V^T p^T on the 16 x 16 matrix instruction, whose
 // operands hold 8 neighbours along the sum a lane: K's and q's rows are read as
@@ -30,9 +29,7 @@ using pk::rounded;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;       // of a work-group
-constexpr int kTile = 32;       // positions that a wave has in work
-constexpr int kUnit = kWaves * kTile;
+constexpr int kTile = 32;  // positions of one step
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 struct Args {
@@ -47,7 +44,9 @@ struct Args {
     int64_t pages;
     Shape shape;
     int B, d, page_size, page_shift;  // page_shift: of a power of two, else -1
-    float scale, cap;  // scores are formed in powers of two: scale * log2(e), or scale / cap and cap * log2(e)
+    // scores are formed in powers of two: scale * log2(e), or scale / cap and cap * log2(e).
+    // scale is positive: q is multiplied by its sign (by 0, and scale is 1, for a scale of 0)
+    float scale, cap, sign;
 };
 
 template <typename T>
@@ -88,38 +87,6 @@ __device__ __forceinline__ f32x4 product(Eight<float>::V a, Eight<float>::V b, f
     return c;
 }
 
-// A wave's 32 rows of V in LDS.  Rows are padded so that the lanes of one read of a
-// column tile start at different banks: 8 apart in 16 bits, 4 in 32.
-template <typename T, int D>
-struct Staged {
-    static constexpr int kPad = sizeof(T) == 2 ? 16 : 4;
-    static constexpr int kRow = D + kPad;
-    static constexpr int kBytes = kTile * kRow * (int)sizeof(T);
-
-    // channels 16 n + lane % 16 of positions 4 (lane / 16) + 0..3 and those + 16
-    static __device__ __forceinline__ typename Eight<T>::V column(const T *s, int n, int lane)
-    {
-        typename Eight<T>::V v;
-        if constexpr (sizeof(T) == 2) {
-            typedef short S4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) S4 *P;
-            const T *p = s + (lane / 4) * kRow + n * 16 + (lane % 4) * 4;
-            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
-            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * kRow));
-            const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            v = __builtin_bit_cast(typename Eight<T>::V, both);
-        } else {
-            const T *p = s + (lane / 16) * 4 * kRow + n * 16 + lane % 16;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = p[j * kRow];
-                v[4 + j] = p[(16 + j) * kRow];
-            }
-        }
-        return v;
-    }
-};
-
 // tanh, to 2 units in the last place.  The exponential's form would lose digits
 // below 0.6: there x (1 + x^2 P(x^2)), P a least-squares fit whose error is 2^-30 of
 // the result.
@@ -137,8 +104,6 @@ __device__ __forceinline__ float tanh_of(float x)
 }
 
 // ------------------------------------------------------------------ the line of units
-
-constexpr int kThreads = kWaves * 64;
 
 __device__ __forceinline__ Sequence sequence_of(const Args &p, int b)
 {
@@ -289,282 +254,47 @@ __device__ __forceinline__ float weight_of(float m, float most)
     return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - most);
 }
 
-// ------------------------------------------------------------------ the attention
+// ------------------------------------------------------------------ K and V in LDS
 
-// NQ groups of 16 rows; the waves divide the positions.
-template <typename T, int D, int NQ>
-__global__ void __launch_bounds__(kThreads) attention_kernel(Args p)
+// The lane's number as the compiler cannot know it ahead: addresses made of it are made
+// where they are used.  Left alone, they are made once before all loops and held in
+// registers that the sums need.
+__device__ __forceinline__ int lane_here()
 {
-    typedef typename Eight<T>::V V8;
-    constexpr int C = D / 32, N = D / 16, ROWS = 16 * NQ;
-    constexpr int kSum = ROWS * (D + 4) * 4;  // a wave's sums
-    constexpr int kWave = Staged<T, D>::kBytes > kSum ? Staged<T, D>::kBytes : kSum;
-    __shared__ __align__(16) char s_raw[kWaves * kWave];
-    __shared__ Line<kThreads>::Shared s_line;
-    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
-    T *s_v = reinterpret_cast<T *>(s_raw + wave * kWave);
-
-    const Line<kThreads> line(p, s_line);
-    const unsigned total = line.total, each = share(total, gridDim.x), active = (total + each - 1) / each;
-    if (blockIdx.x >= active) return;
-    const unsigned rank = rank_of(blockIdx.x, active), share_begin = rank * each;
-    const unsigned share_end = share_begin + each < total ? share_begin + each : total;
-    int b;
-    unsigned base;
-    line.find(share_begin, b, base);
-    Sequence seq = line.get(b);
-
-    for (unsigned u = share_begin; u < share_end;) {
-        while (u >= base + seq.cost(p.shape.heads)) {
-            base += seq.cost(p.shape.heads);
-            seq = line.get(++b);
-        }
-        const unsigned item = (u - base) / (unsigned)seq.units, item_begin = base + item * seq.units, part_begin = u;
-        const unsigned part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
-        const int head = (int)(item / (unsigned)seq.groups), row0 = (int)(item % (unsigned)seq.groups) * ROWS;
-        const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
-        const int begin = p.shape.unit_shift < 0 ? 0 : (int)(part_begin - item_begin) << p.shape.unit_shift;
-        const int end = part_end == item_begin + seq.units ? seq.keys : (int)(part_end - item_begin) << p.shape.unit_shift;
-        const int length = seq.length;
-        const T *key = (const T *)p.key + head * p.key_head, *value = (const T *)p.value + head * p.value_head;
-        const int32_t *table = p.table + b * p.table_row;
-
-        // the rows, and which of the sequence's tokens each sees
-        V8 q[NQ][C];
-        uint64_t word[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int r = n * 16 + col;
-            word[n] = 0;
-            const T *at = (const T *)p.q;
-            if (r < rows) {
-                const RowAt row = row_at(p, seq, head, row0 + r);
-                at += row.m * p.q_token + row.h * p.q_head;
-                word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c) q[n][c] = get8(at + c * 32 + g * 8, r < rows ? p.d - c * 32 - g * 8 : 0);
-        }
-
-        f32x4 o[NQ][N];
-        float m[NQ], l[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            m[n] = -__builtin_inff();
-            l[n] = 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
-        }
-
-        // where positions at + col and at + 16 + col lie: their pages' numbers
-        auto page_at = [&](int j) {
-            int page = -1;
-            if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
-            return (unsigned)page < (uint64_t)p.pages ? page : -1;
-        };
-        auto place_in = [&](int j) {
-            return p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
-        };
-        V8 kk[2][C], vv[2][C];
-        auto fetch = [&](int at, const int *page) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int place = place_in(at + h * 16 + col);
-                const T *pk = key, *pv = value;
-                if (page[h] >= 0) {
-                    pk += page[h] * p.key_page + place * p.key_place;
-                    pv += page[h] * p.value_page + place * p.value_place;
-                }
-#pragma unroll
-                for (int c = 0; c < C; ++c) kk[h][c] = get8(pk + c * 32 + g * 8, page[h] >= 0 ? p.d - c * 32 - g * 8 : 0);
-#pragma unroll
-                for (int c = 0; c < C; ++c) vv[h][c] = get8(pv + c * 32 + g * 8, page[h] >= 0 ? p.d - c * 32 - g * 8 : 0);
-            }
-        };
-        int at = begin + wave * kTile;
-        int page[2] = {page_at(at + col), page_at(at + 16 + col)};
-        if (at < end) fetch(at, page);
-        int next[2] = {page_at(at + kUnit + col), page_at(at + kUnit + 16 + col)};
-
-        for (; at < end; at += kUnit) {
-            // positions that hold something
-            const unsigned there = (unsigned)(__ballot(page[0] >= 0) & 0xffff) | (unsigned)(__ballot(page[1] >= 0) & 0xffff) << 16;
-            f32x4 x[NQ][2];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    x[n][h] = (f32x4)0.f;
-#pragma unroll
-                    for (int c = 0; c < C; ++c) x[n][h] = product(kk[h][c], q[n][c], x[n][h]);
-                }
-            // V to LDS; a token's NaN or infinity is told from here on
-            bool odd = false;
-            const bool drafted = at + kTile > length;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    *reinterpret_cast<V8 *>(s_v + (h * 16 + col) * Staged<T, D>::kRow + c * 32 + g * 8) = vv[h][c];
-                    if (drafted) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) odd |= !(fabsf((float)vv[h][c][j]) < __builtin_inff());
-                    }
-                }
-            odd = __any(odd);
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            // the next tile on its way
-            page[0] = next[0];
-            page[1] = next[1];
-            if (at + kUnit < end) fetch(at + kUnit, page);
-            next[0] = page_at(at + 2 * kUnit + col);
-            next[1] = page_at(at + 2 * kUnit + 16 + col);
-
-            V8 weight[NQ];
-            unsigned seen[NQ];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                seen[n] = there;
-                if (drafted) {
-                    const int off = length - at;  // the tile's first token
-                    seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
-                }
-                float most = -__builtin_inff(), s[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[e] = x[n][e / 4][e % 4] * p.scale;
-                    if (p.cap != 0.f) s[e] = tanh_of(s[e]) * p.cap;
-                }
-                if (seen[n] != ~0u) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) s[e] = -__builtin_inff();
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, s[e]);
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                most = fmaxf(most, m[n]);
-                const float origin = most == -__builtin_inff() ? 0.f : most;
-                const float shrink = __builtin_amdgcn_exp2f(m[n] - origin);
-                m[n] = most;
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[e] = __builtin_amdgcn_exp2f(s[e] - origin);
-                    sum += s[e];
-                    weight[n][e] = (T)s[e];
-                }
-                l[n] = fmaf(l[n], shrink, sum);
-#pragma unroll
-                for (int i = 0; i < N; ++i) o[n][i] *= shrink;
-            }
-            if (!odd) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const V8 v = Staged<T, D>::column(s_v, i, lane);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][i] = product(v, weight[n], o[n][i]);
-                }
-            } else {
-                // a NaN or an infinity reaches the rows that see it and no other: position by position
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    for (int from = 0; from < 4; ++from) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int j = e / 4 * 16 + from * 4 + e % 4;
-                            const float w = __shfl((float)weight[n][e], from * 16 + col);
-#pragma unroll 1
-                            for (int c = 0; c < N * 4; ++c) {
-                                const float v = (float)s_v[j * Staged<T, D>::kRow + (c / 4) * 16 + g * 4 + c % 4];
-                                const float add = seen[n] >> j & 1 ? w * v : 0.f;
-#pragma unroll
-                                for (int i = 0; i < N * 4; ++i)
-                                    if (i == c) o[n][i / 4][i % 4] += add;
-                            }
-                        }
-                    }
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-
-        // the waves' sums together
-        float *s_o = reinterpret_cast<float *>(s_raw + wave * kWave);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            l[n] += __shfl_xor(l[n], 16);
-            l[n] += __shfl_xor(l[n], 32);
-            if (g == 0) {
-                s_m[wave][n * 16 + col] = m[n];
-                s_l[wave][n * 16 + col] = l[n];
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = o[n][i];
-        }
-        __syncthreads();
-        const bool whole = part_begin == item_begin && part_end == item_begin + seq.units;
-        float *part = whole ? nullptr : part_of<D>(p, rank, slot_of(part_begin, share_begin));
-        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), c = i % (D / 4) * 4;
-            float most = s_m[0][r];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s_m[w][r]);
-            f32x4 sum = (f32x4)0.f;
-            float all = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = weight_of(s_m[w][r], most);
-                sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kWave + (r * (D + 4) + c) * 4) * f;
-                all += s_l[w][r] * f;
-            }
-            if (whole) {
-                if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
-            } else {
-                *reinterpret_cast<f32x4 *>(part + r * D + c) = sum;
-                if (c == 0) {
-                    part[ROWS * D + r] = most;
-                    part[ROWS * (D + 1) + r] = all;
-                }
-            }
-        }
-        __syncthreads();
-        u = part_end;
-    }
+    int lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));
+    return lane;
 }
 
-// ------------------------------------------------------------------ the attention, copied to LDS
-
-// A wave's 32 rows of K or V in LDS as copies leave them: 1 KiB an instruction, 16
-// bytes a lane, so that a row's chunks of 16 bytes lie side by side.  Chunk c of row r
-// is at place c ^ turn(r): sixteen rows' chunks of one column lie in all banks.
+// Rows of K or V in LDS as copies leave them: 1 KiB an instruction, 16 bytes a lane, so
+// that a row's chunks of 16 bytes lie side by side.  Chunk c of row r is at place
+// c ^ turn(r): sixteen rows' chunks of one column lie in all banks.
 template <typename T, int D>
-struct Copied {
-    static constexpr int kChunks = D * (int)sizeof(T) / 16;  // of a row
+struct Lds {
+    static constexpr int kElements = 16 / (int)sizeof(T);
+    static constexpr int kChunks = D / kElements;  // of a row
     static constexpr int kRow = kChunks * 16;
-    static constexpr int kBytes = kTile * kRow;
-    static constexpr int kRows = 64 / kChunks;      // of a copy
-    static constexpr int kCopies = kTile / kRows;   // of a tile
-    static constexpr int kTurns = kRows >= 16 ? 1 : 16 / kRows < kCopies ? 16 / kRows : kCopies;  // copies until turn() repeats
+    static constexpr int kRows = 64 / kChunks;  // of a copy
 
     static __device__ __forceinline__ int turn(int r) { return kChunks >= 16 ? r & 15 : r >> 1 & 7; }
 
-    // channels 8 i on of row r, for the product's operand
-    static __device__ __forceinline__ typename Eight<T>::V row(const char *s, int r, int i)
+    // channels 8 i on of row r, for the product's operand; chunks from `chunks` on are zero
+    template <bool PART>
+    static __device__ __forceinline__ typename Eight<T>::V row(const char *s, int r, int i, int chunks)
     {
+        typedef typename Eight<T>::V V;
         if constexpr (sizeof(T) == 2) {
-            return *reinterpret_cast<const typename Eight<T>::V *>(s + r * kRow + (i ^ turn(r)) * 16);
+            const V v = *reinterpret_cast<const V *>(s + r * kRow + (i ^ turn(r)) * 16);
+            return PART && i >= chunks ? (V)(T)0.f : v;
         } else {
             const f32x4 lo = *reinterpret_cast<const f32x4 *>(s + r * kRow + (2 * i ^ turn(r)) * 16);
             const f32x4 hi = *reinterpret_cast<const f32x4 *>(s + r * kRow + ((2 * i + 1) ^ turn(r)) * 16);
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_shufflevector(PART && 2 * i >= chunks ? (f32x4)0.f : lo, PART && 2 * i + 1 >= chunks ? (f32x4)0.f : hi,
+                                           0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
 
-    // channel 16 n + lane % 16 of positions 4 (lane / 16) + 0..3 and those + 16
+    // channel 16 n + lane % 16 of rows 4 (lane / 16) + 0..3 and those + 16
     static __device__ __forceinline__ typename Eight<T>::V column(const char *s, int n, int lane)
     {
         typename Eight<T>::V v;
@@ -589,7 +319,6 @@ struct Copied {
         return v;
     }
 
-    // element (r, channel)
     static __device__ __forceinline__ float at(const char *s, int r, int channel)
     {
         const int byte = channel * (int)sizeof(T);
@@ -599,250 +328,460 @@ struct Copied {
 
 // Each lane's 16 bytes at base + off to the wave's 1 KiB from `to` on.  Written out,
 // because the compiler would wait for every such copy before the next read of LDS; the
-// wave waits for a tile's when it begins it.  m0, where `to` is passed, is read one wait
-// state after it is set, scalar operands five after a vector instruction that may
-// have made them.
+// kernels wait for a tile's when they begin it.  m0, where `to` is passed, is read one
+// wait state after it is set, scalar operands five after a vector instruction that
+// may have made them.
 __device__ __forceinline__ void copy16(char *to, const char *base, unsigned off)
 {
     const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
     asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(at), "v"(off), "s"(base) : "memory");
 }
 
-// The same attention where K's and V's rows are whole chunks of 16 bytes and a copy's
-// rows lie in one page.  A wave's tiles go from memory straight to its own part of
-// LDS, one on its way while the one before is worked on; nothing waits for another
-// wave until their sums are joined.
-template <typename T, int D, int NQ, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
-{
-    typedef typename Eight<T>::V V8;
-    typedef Copied<T, D> S;
-    constexpr int C = D / 32, N = D / 16, ROWS = 16 * NQ, THREADS = WAVES * 64, STEP = WAVES * kTile;
-    constexpr int kStage = 2 * S::kBytes, kWave = 2 * kStage;  // K and V, twice
-    static_assert(ROWS * (D + 4) * 4 <= kWave, "a wave's sums fit its stages");
-    __shared__ __align__(16) char s_raw[WAVES * kWave];
-    __shared__ typename Line<THREADS>::Shared s_line;
-    __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
-    char *const s_own = s_raw + wave * kWave;
+// What one wave brings of an item's K and V into LDS: ROWS rows of a tile, from row
+// `first` of it on (a multiple of 8).
+//   COPIED   straight from memory: rows are whole chunks at multiples of 16 bytes, and a
+//            copy's rows (up to 8) lie in one page;
+//   else     through registers, chunk by chunk: any head size, alignment and page.
+template <typename T, int D, int ROWS, bool COPIED>
+struct Mover {
+    typedef Lds<T, D> L;
+    typedef typename Pack<T>::V V;
+    static constexpr int kCopies = ROWS / L::kRows;
+    static constexpr int kTurns = L::kRows >= 16 ? 1 : 16 / L::kRows < kCopies ? 16 / L::kRows : kCopies;  // until turn() repeats
+    static_assert(kCopies * L::kRows == ROWS, "whole copies");
+    const Args &p;
+    const char *key, *value;  // the head's
+    const int32_t *table;
+    int first, chunks;
+    unsigned key_off[COPIED ? kTurns : 1], value_off[COPIED ? kTurns : 1];
+    unsigned copies;  // bit t: this lane has a chunk in copies of turn t
+    V in_k[COPIED ? 1 : kCopies], in_v[COPIED ? 1 : kCopies];
 
-    const Line<THREADS> line(p, s_line);
-    const unsigned total = line.total, each = share(total, gridDim.x), active = (total + each - 1) / each;
-    if (blockIdx.x >= active) return;
-    const unsigned rank = rank_of(blockIdx.x, active), share_begin = rank * each;
-    const unsigned share_end = share_begin + each < total ? share_begin + each : total;
-    int b;
-    unsigned base;
-    line.find(share_begin, b, base);
-    Sequence seq = line.get(b);
-
-    // what a lane copies: a row of each copy, and its chunk of it
-    const int chunks = p.d * (int)sizeof(T) / 16;
-    unsigned key_off[S::kTurns], value_off[S::kTurns];
-    bool copies[S::kTurns];
+    __device__ __forceinline__ Mover(const Args &args, int first_row) : p(args), first(first_row), copies(0)
+    {
+        const int lane = threadIdx.x % 64;
+        chunks = (p.d + L::kElements - 1) / L::kElements;
+        if constexpr (COPIED) {
 #pragma unroll
-    for (int t = 0; t < S::kTurns; ++t) {
-        const int r = lane / S::kChunks, c = lane % S::kChunks ^ S::turn(t * S::kRows + r);
-        key_off[t] = (unsigned)(r * (int)p.key_place * (int)sizeof(T) + c * 16);
-        value_off[t] = (unsigned)(r * (int)p.value_place * (int)sizeof(T) + c * 16);
-        copies[t] = c < chunks;
-    }
-    // chunks that no copy writes are multiplied by zeros
-    if (p.d != D)
-        for (int i = threadIdx.x; i < WAVES * kWave / 16; i += THREADS) reinterpret_cast<f32x4 *>(s_raw)[i] = (f32x4)0.f;
-    bool zeroed = p.d != D;
-
-    for (unsigned u = share_begin; u < share_end;) {
-        while (u >= base + seq.cost(p.shape.heads)) {
-            base += seq.cost(p.shape.heads);
-            seq = line.get(++b);
-        }
-        const unsigned item = (u - base) / (unsigned)seq.units, item_begin = base + item * seq.units, part_begin = u;
-        const unsigned part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
-        const int head = (int)(item / (unsigned)seq.groups), row0 = (int)(item % (unsigned)seq.groups) * ROWS;
-        const int rows = seq.tokens * p.shape.group - row0 < ROWS ? seq.tokens * p.shape.group - row0 : ROWS;
-        const int begin = p.shape.unit_shift < 0 ? 0 : (int)(part_begin - item_begin) << p.shape.unit_shift;
-        const int end = part_end == item_begin + seq.units ? seq.keys : (int)(part_end - item_begin) << p.shape.unit_shift;
-        const int length = seq.length;
-        const char *key = (const char *)((const T *)p.key + head * p.key_head);
-        const char *value = (const char *)((const T *)p.value + head * p.value_head);
-        const int32_t *table = p.table + b * p.table_row;
-
-        // lane r and r + 32 have row r of a tile: whether it holds something, and where it lies
-        auto page_at = [&](int j) {
-            int page = -1;
-            if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
-            return (unsigned)page < (uint64_t)p.pages ? page : -1;
-        };
-        auto copy = [&](int at, int page, char *to) {
-            const int j = at + lane % 32;
-            const int place = p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
-            const int64_t k = (page * p.key_page + place * p.key_place) * (int)sizeof(T);
-            const int64_t v = (page * p.value_page + place * p.value_place) * (int)sizeof(T);
-            auto from = [&](const char *first, int64_t off, int r) {
-                const unsigned lo = __builtin_amdgcn_readlane((int)off, r), hi = __builtin_amdgcn_readlane((int)(off >> 32), r);
-                return first + (int64_t)((uint64_t)hi << 32 | lo);
-            };
-            const unsigned there = (unsigned)__ballot(page >= 0);
-            // all of K, then all of V
-#pragma unroll
-            for (int i = 0; i < S::kCopies; ++i)
-                if (there >> (i * S::kRows) & 1) {
-                    const char *at = from(key, k, i * S::kRows);
-                    if (copies[i % S::kTurns]) copy16(to + i * 1024, at, key_off[i % S::kTurns]);
-                }
-#pragma unroll
-            for (int i = 0; i < S::kCopies; ++i)
-                if (there >> (i * S::kRows) & 1) {
-                    const char *at = from(value, v, i * S::kRows);
-                    if (copies[i % S::kTurns]) copy16(to + S::kBytes + i * 1024, at, value_off[i % S::kTurns]);
-                }
-        };
-        int at = begin + wave * kTile, stage = 0;
-        int page = page_at(at + lane % 32);
-        if (zeroed) {
-            __syncthreads();  // the zeros are in place
-            zeroed = false;
-        }
-        if (at < end) copy(at, page, s_own);
-        int next = page_at(at + STEP + lane % 32);
-
-        // the rows, and which of the sequence's tokens each sees
-        V8 q[NQ][C];
-        uint64_t word[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int r = n * 16 + col;
-            word[n] = 0;
-            const T *from = (const T *)p.q;
-            if (r < rows) {
-                const RowAt row = row_at(p, seq, head, row0 + r);
-                from += row.m * p.q_token + row.h * p.q_head;
-                word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
+            for (int t = 0; t < kTurns; ++t) {
+                const int r = lane / L::kChunks, c = lane % L::kChunks ^ L::turn(first + t * L::kRows + r);
+                key_off[t] = (unsigned)(r * (int)p.key_place * (int)sizeof(T) + c * 16);
+                value_off[t] = (unsigned)(r * (int)p.value_place * (int)sizeof(T) + c * 16);
+                copies |= (c < chunks ? 1u : 0u) << t;
             }
-#pragma unroll
-            for (int c = 0; c < C; ++c) q[n][c] = get8(from + c * 32 + g * 8, r < rows ? p.d - c * 32 - g * 8 : 0);
         }
-        f32x4 o[NQ][N];
-        float m[NQ], l[NQ];
+    }
+    __device__ __forceinline__ void head(int b, int h)
+    {
+        key = (const char *)((const T *)p.key + h * p.key_head);
+        value = (const char *)((const T *)p.value + h * p.value_head);
+        table = p.table + b * p.table_row;
+    }
+    // the page that position j < end lies in, or -1
+    __device__ __forceinline__ int page_at(int j, int end) const
+    {
+        int page = -1;
+        if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
+        return (unsigned)page < (uint64_t)p.pages ? page : -1;
+    }
+    // The rows of the tile at position `at`, whose pages are `page` (row lane % 32 of what
+    // this wave moves, or lane % 64 of 64), on their way to s_k and s_v, both at the tile's row 0.
+    __device__ __forceinline__ void begin(int at, int page, char *s_k, char *s_v)
+    {
+        const int lane = threadIdx.x % 64, j = at + first + lane % ROWS;
+        const int place = p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
+        const int64_t k = (page * p.key_page + place * p.key_place) * (int)sizeof(T);
+        const int64_t v = (page * p.value_page + place * p.value_place) * (int)sizeof(T);
+        if constexpr (COPIED) {
+            auto from = [&](const char *start, int64_t off, int r) {
+                const unsigned lo = __builtin_amdgcn_readlane((int)off, r), hi = __builtin_amdgcn_readlane((int)(off >> 32), r);
+                return start + (int64_t)((uint64_t)hi << 32 | lo);
+            };
+            // all of K, then all of V; rows without a page, and chunks beyond the head's, are left out
+            auto copy = [&]<bool ALL>(unsigned there) {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i)
+                    if (ALL || there >> (i * L::kRows) & 1) {
+                        const char *start = from(key, k, i * L::kRows);
+                        if (ALL || copies >> (i % kTurns) & 1) copy16(s_k + (first + i * L::kRows) * L::kRow, start, key_off[i % kTurns]);
+                    }
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i)
+                    if (ALL || there >> (i * L::kRows) & 1) {
+                        const char *start = from(value, v, i * L::kRows);
+                        if (ALL || copies >> (i % kTurns) & 1) copy16(s_v + (first + i * L::kRows) * L::kRow, start, value_off[i % kTurns]);
+                    }
+            };
+            if (p.d == D && __all(page >= 0))
+                copy.template operator()<true>(0);
+            else
+                copy.template operator()<false>((unsigned)__ballot(page >= 0));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int r = i * L::kRows + lane / L::kChunks, c = lane % L::kChunks;
+                const int64_t ok = (int64_t)((uint64_t)(unsigned)__shfl((int)(k >> 32), r) << 32 | (unsigned)__shfl((int)k, r));
+                const int64_t ov = (int64_t)((uint64_t)(unsigned)__shfl((int)(v >> 32), r) << 32 | (unsigned)__shfl((int)v, r));
+                const int n = __shfl(page, r) >= 0 ? p.d - c * L::kElements : 0;
+                in_k[i] = part((const T *)(key + ok) + c * L::kElements, n);
+                in_v[i] = part((const T *)(value + ov) + c * L::kElements, n);
+            }
+        }
+    }
+    // n elements from `from` on, zeros after them
+    static __device__ __forceinline__ V part(const T *from, int n)
+    {
+        V v = (V)(T)0.f;
+        if (n >= L::kElements) return *reinterpret_cast<const typename Pack<T>::U *>(from);
+#pragma unroll
+        for (int j = 0; j < L::kElements; ++j)
+            if (j < n) v[j] = from[j];
+        return v;
+    }
+    // What begin() began is in LDS (of this wave); `there`: the rows that hold something.  V's
+    // others become zeros: their weights are, but what was copied with them may be NaN.
+    __device__ __forceinline__ void end(uint64_t there, char *s_k, char *s_v) const
+    {
+        const int lane = threadIdx.x % 64;
+        if constexpr (COPIED) {
+            constexpr uint64_t all = ROWS == 64 ? ~0ull : (1ull << ROWS % 64) - 1;
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if ((there & all) != all) {
+                f32x4 *to = reinterpret_cast<f32x4 *>(s_v + first * L::kRow);
+#pragma unroll 1
+                for (int i = lane_here(); i < ROWS * L::kChunks; i += 64)
+                    if (!(there >> (i / L::kChunks) & 1)) to[i] = (f32x4)0.f;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int r = first + i * L::kRows + lane / L::kChunks, c = lane % L::kChunks ^ L::turn(r);
+                *reinterpret_cast<V *>(s_k + r * L::kRow + c * 16) = in_k[i];
+                *reinterpret_cast<V *>(s_v + r * L::kRow + c * 16) = in_v[i];
+            }
+        }
+    }
+    // whether its rows of V have a NaN or an infinity
+    __device__ __forceinline__ bool odd(const char *s_v) const
+    {
+        bool odd = false;
+#pragma unroll 1
+        for (int i = lane_here(); i < ROWS * L::kChunks; i += 64) {
+            const int r = first + i / L::kChunks, c = i % L::kChunks ^ L::turn(r);
+            const V v = *reinterpret_cast<const V *>(s_v + r * L::kRow + i % L::kChunks * 16);
+#pragma unroll
+            for (int j = 0; j < L::kElements; ++j) odd |= c < chunks && !(fabsf((float)v[j]) < __builtin_inff());
+        }
+        return __any(odd);
+    }
+};
+
+// A wave's stores to LDS are seen by its loads after this
+__device__ __forceinline__ void own_lds()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// ------------------------------------------------------------------ the attention
+
+// The larger of v in lanes 16 and 32 apart, in all of them.
+__device__ __forceinline__ float across(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+
+// 16 NQ rows of an item, a wave's: lane l has row l % 16 of each sixteen.
+template <typename T, int D, int NQ>
+struct Rows {
+    typedef typename Eight<T>::V V8;
+    typedef Lds<T, D> L;
+    static constexpr int C = D / 32, N = D / 16;
+    static constexpr int kGroup = sizeof(T) == 2 ? 8 : 4;  // operands read from LDS at once: 32 registers
+    V8 q[NQ][C];
+    uint64_t word[NQ];  // the sequence's tokens that a row sees
+    f32x4 o[NQ][N];     // sums of values: channels 16 i + 4 (l / 16) + 0..3
+    float l[NQ];        // sums of exponentials: of this lane's positions
+    float m[NQ];        // their origin, in the products' units
+
+    // Rows from row0 on; those from `rows` on are the last one again, and are not stored.
+    // WHOLE: rows are whole chunks of 16 bytes.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const Args &p, const Sequence &seq, int head, int row0, int rows, int chunks)
+    {
+        const int lane = threadIdx.x % 64, col = lane % 16, g = lane / 16;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
+            const int r = row0 + n * 16 + col;
+            const RowAt row = row_at(p, seq, head, r < rows ? r : rows - 1);
+            const T *from = (const T *)p.q + row.m * p.q_token + row.h * p.q_head;
+            word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if constexpr (!WHOLE) {
+                    q[n][c] = get8(from + c * 32 + g * 8, p.d - c * 32 - g * 8);
+                } else {
+                    constexpr int E = L::kElements;
+                    typename Pack<T>::V part[8 / E];
+#pragma unroll
+                    for (int h = 0; h < 8 / E; ++h) {
+                        const int i = (c * 4 + g) * (8 / E) + h;
+                        part[h] = *reinterpret_cast<const typename Pack<T>::U *>(from + (i < chunks ? i : 0) * E);
+                        if (p.d != D && i >= chunks) part[h] = (typename Pack<T>::V)(T)0.f;
+                    }
+                    if constexpr (E == 8)
+                        q[n][c] = part[0];
+                    else
+                        q[n][c] = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            }
             m[n] = -__builtin_inff();
             l[n] = 0.f;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
         }
-
-        for (; at < end; at += STEP, stage ^= 1) {
-            char *const s_k = s_own + stage * kStage, *const s_v = s_k + S::kBytes;
-            const unsigned there = (unsigned)__ballot(page >= 0);
-            // this tile is here, and the other stage has been read
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            if (at + STEP < end) copy(at + STEP, next, s_own + (stage ^ 1) * kStage);
-            page = next;
-            next = page_at(at + 2 * STEP + lane % 32);
-
-            if (there != ~0u) {
-                // V's rows that hold nothing: zeros, whatever was copied with them
-                for (int i = lane; i < S::kBytes / 16; i += 64)
-                    if (!(there >> (i / S::kChunks) & 1)) reinterpret_cast<f32x4 *>(s_v)[i] = (f32x4)0.f;
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-            const bool drafted = at + kTile > length;
-            bool odd = false;
-            if (drafted) {
-                // a token's NaN or infinity: some rows may not see it
-                for (int i = lane; i < S::kBytes / 16; i += 64) {
-                    typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
-                    const V v = reinterpret_cast<const V *>(s_v)[i];
+        if (p.sign == 1.f) return;
 #pragma unroll
-                    for (int j = 0; j < 16 / (int)sizeof(T); ++j) odd |= !(fabsf((float)v[j]) < __builtin_inff());
-                }
-                odd = __any(odd);
-            }
-
-            f32x4 x[NQ][2];
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = (f32x4)0.f;
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const V8 k = S::row(s_k, h * 16 + col, c * 4 + g);
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) x[n][h] = product(k, q[n][c], x[n][h]);
-                }
+                for (int j = 0; j < 8; ++j) q[n][c][j] = (T)((float)q[n][c][j] * p.sign);
+    }
 
-            V8 weight[NQ];
-            unsigned seen[NQ];
+    // One tile, at position `at`; `there`: its positions that hold something; `odd`: values
+    // among them that are no numbers, some of which a row may not see; `scratch`: 2 KiB of LDS.
+    __device__ __forceinline__ void step(const Args &p, const char *s_k, const char *s_v, int at, int length, unsigned there,
+                                         bool odd, int chunks, float *scratch)
+    {
+        const int lane = lane_here(), col = lane % 16, g = lane / 16;
+        f32x4 x[NQ][2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = (f32x4)0.f;
+        // (reads in groups before their products: one by one each product would wait for its own)
+        auto scores = [&]<bool PART>() {
+            constexpr int G = C < kGroup / 2 ? C : kGroup / 2;
+#pragma unroll
+            for (int from = 0; from < C; from += G) {
+                V8 k[G][2];
+#pragma unroll
+                for (int c = 0; c < G; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) k[c][h] = L::template row<PART>(s_k, h * 16 + col, (from + c) * 4 + g, chunks);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < G; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) x[n][h] = product(k[c][h], q[n][from + c], x[n][h]);
+            }
+        };
+        if (p.d == D)
+            scores.template operator()<false>();
+        else
+            scores.template operator()<true>();
+
+        // the first columns of V on their way while the weights are made
+        constexpr int G = N < kGroup ? N : kGroup;
+        V8 v[G];
+        if (!odd) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) v[i] = L::column(s_v, i, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+
+        const bool drafted = at + kTile > length;
+        V8 weight[NQ];
+        unsigned seen[NQ];
+        float scale = p.scale;
+        if (p.cap != 0.f) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[n][e / 4][e % 4] = tanh_of(x[n][e / 4][e % 4] * scale) * p.cap;
+                    if (e % 2) __builtin_amdgcn_sched_barrier(0);
+                }
+            scale = 1.f;
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            seen[n] = there;
+            if (drafted) {
+                const int off = length - at;  // the tile's first token
+                seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
+            }
+        }
+        if (drafted || there != ~0u) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) x[n][e / 4][e % 4] = -__builtin_inff();
+        }
+        float most[NQ];
+        bool move = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            most[n] = fmaxf(fmaxf(x[n][0][0], x[n][0][1]), x[n][0][2]);
+            most[n] = fmaxf(fmaxf(most[n], x[n][0][3]), x[n][1][0]);
+            most[n] = fmaxf(fmaxf(most[n], x[n][1][1]), x[n][1][2]);
+            most[n] = across(fmaxf(most[n], x[n][1][3]));
+            // (both -infinity: nothing seen yet)
+            move |= (most[n] - m[n]) * scale > 8.f;
+        }
+        // the sums' origins move only where a weight would pass 2^8: they stay in range, and
+        // nearly no tile has them multiplied
+        if (__any(move)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                seen[n] = there;
-                if (drafted) {
-                    const int off = length - at;  // the tile's first token
-                    seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
-                }
-                float most = -__builtin_inff(), s[8];
+                const float top = fmaxf(most[n], m[n]);
+                const float shrink = m[n] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m[n] - top) * scale);
+                m[n] = top;
+                l[n] *= shrink;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[e] = x[n][e / 4][e % 4] * p.scale;
-                    if (p.cap != 0.f) s[e] = tanh_of(s[e]) * p.cap;
-                }
-                if (drafted || there != ~0u) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) s[e] = -__builtin_inff();
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, s[e]);
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                // the sums' origin moves only where a weight would pass 2^8: they stay in range,
-                // and nearly no tile has them multiplied
-                if (__any(most > m[n] + 8.f)) {
-                    most = fmaxf(most, m[n]);
-                    const float shrink = __builtin_amdgcn_exp2f(m[n] - (most == -__builtin_inff() ? 0.f : most));
-                    m[n] = most;
-                    l[n] *= shrink;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) o[n][i] *= shrink;
-                }
-                const float origin = m[n] == -__builtin_inff() ? 0.f : m[n];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[e] = __builtin_amdgcn_exp2f(s[e] - origin);
-                    l[n] += s[e];
-                    weight[n][e] = (T)s[e];
-                }
+                for (int i = 0; i < N; ++i) o[n][i] *= shrink;
             }
-            if (!odd) {
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const float origin = m[n] == -__builtin_inff() ? 0.f : -m[n] * scale;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e / 4][e % 4], scale, origin));
+                l[n] += w;
+                weight[n][e] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
+            }
+        }
+        if (!odd) {
+#pragma unroll
+            for (int from = 0; from < N; from += G) {
+                if (from) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) v[i] = L::column(s_v, from + i, lane);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n], o[n][from + i]);
+            }
+            return;
+        }
+        // a NaN or an infinity reaches the rows that see it and no other: position by position
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            own_lds();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scratch[(e / 4 * 16 + g * 4 + e % 4) * 16 + col] = (float)weight[n][e];
+            own_lds();
+#pragma unroll 1
+            for (int j = 0; j < kTile; ++j) {
+                const float w = scratch[j * 16 + col];
+                const bool sees = seen[n] >> j & 1;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const V8 v = S::column(s_v, i, lane);
+                    const int here = lane_here() / 16 * 4;
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][i] = product(v, weight[n], o[n][i]);
-                }
-            } else {
-                // a NaN or an infinity reaches the rows that see it and no other: position by position
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    for (int from = 0; from < 4; ++from) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int j = e / 4 * 16 + from * 4 + e % 4;
-                            const float w = __shfl((float)weight[n][e], from * 16 + col);
-                            const bool sees = seen[n] >> j & 1;
-#pragma unroll
-                            for (int i = 0; i < N; ++i)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const float v = S::at(s_v, j, i * 16 + g * 4 + c);
-                                    o[n][i][c] += sees ? w * v : 0.f;
-                                }
-                        }
+                    for (int c = 0; c < 4; ++c) {
+                        const float v = L::at(s_v, j, i * 16 + here + c);
+                        o[n][i][c] += sees ? w * v : 0.f;
                     }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+        }
+    }
+};
+
+// What a work-group has of the line, part by part.
+struct Walk {
+    unsigned rank, share_begin, share_end;
+    int b;
+    unsigned base;  // units before sequence b
+    Sequence seq;
+    // the part at hand
+    unsigned item_begin, part_begin, part_end;
+    int head, row0, rows;  // of the item: its first row among its head's, and how many it has
+    int begin, end;        // positions
+    bool whole;
+
+    // from unit u on
+    template <int THREADS>
+    __device__ __forceinline__ void at(const Args &p, const Line<THREADS> &line, unsigned u)
+    {
+        while (u >= base + seq.cost(p.shape.heads)) {
+            base += seq.cost(p.shape.heads);
+            seq = line.get(++b);
+        }
+        const unsigned item = (u - base) / (unsigned)seq.units;
+        item_begin = base + item * seq.units;
+        part_begin = u;
+        part_end = item_begin + seq.units < share_end ? item_begin + seq.units : share_end;
+        const int most = 1 << p.shape.rows_shift;
+        head = (int)(item / (unsigned)seq.groups);
+        row0 = (int)(item % (unsigned)seq.groups) * most;
+        rows = seq.tokens * p.shape.group - row0 < most ? seq.tokens * p.shape.group - row0 : most;
+        begin = p.shape.unit_shift < 0 ? 0 : (int)(part_begin - item_begin) << p.shape.unit_shift;
+        end = part_end == item_begin + seq.units ? seq.keys : (int)(part_end - item_begin) << p.shape.unit_shift;
+        whole = part_begin == item_begin && part_end == item_begin + seq.units;
+    }
+};
+
+#define PK_WALK(THREADS)                                                                                       \
+    const Line<THREADS> line(p, s_line);                                                                       \
+    const unsigned total = line.total, each = share(total, gridDim.x), active = (total + each - 1) / each;     \
+    if (blockIdx.x >= active) return;                                                                          \
+    Walk walk;                                                                                                 \
+    walk.rank = rank_of(blockIdx.x, active);                                                                   \
+    walk.share_begin = walk.rank * each;                                                                       \
+    walk.share_end = walk.share_begin + each < total ? walk.share_begin + each : total;                        \
+    line.find(walk.share_begin, walk.b, walk.base);                                                            \
+    walk.seq = line.get(walk.b)
+
+// Few rows: the waves divide the positions.  Each has its own tiles, one on its way
+// while the one before is worked on, and nothing waits for another wave until their
+// sums are joined.
+template <typename T, int D, int NQ, int WAVES, bool COPIED>
+__global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
+{
+    typedef Lds<T, D> L;
+    constexpr int N = D / 16, ROWS = 16 * NQ, THREADS = WAVES * 64, STEP = WAVES * kTile;
+    constexpr int kHalf = kTile * L::kRow, kStages = COPIED ? 2 : 1, kWave = kStages * 2 * kHalf;
+    constexpr int kSum = ROWS * (D + 4) * 4, kOwn = kWave > kSum ? kWave : kSum;
+    __shared__ __align__(16) char s_raw[WAVES * kOwn];
+    __shared__ typename Line<THREADS>::Shared s_line;
+    __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_scratch[WAVES][kTile * 16];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
+    char *const s_own = s_raw + wave * kOwn;
+    PK_WALK(THREADS);
+    Mover<T, D, kTile, COPIED> mover(p, 0);
+    Rows<T, D, NQ> rows;
+
+    for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
+        walk.at(p, line, u);
+        mover.head(walk.b, walk.head);
+        const int end = walk.end, length = walk.seq.length;
+        // the first turn only brings the first tile: what brings a tile is here once
+        int at = walk.begin + (wave - WAVES) * kTile, stage = 0;
+        int page = -1, next = mover.page_at(at + STEP + lane % kTile, end);
+        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, walk.row0 + walk.rows, mover.chunks);
+        for (bool first = true; at < end; at += STEP, first = false) {
+            char *const s_k = s_own + stage * 2 * kHalf;
+            const unsigned there = (unsigned)__ballot(page >= 0);
+            if (!first) mover.end(there, s_k, s_k + kHalf);
+            if (COPIED) stage ^= 1;
+            char *const s_next = s_own + stage * 2 * kHalf;
+            if (at + STEP < end) mover.begin(at + STEP, next, s_next, s_next + kHalf);
+            page = next;
+            next = mover.page_at(at + 2 * STEP + lane % kTile, end);
+            if (first) continue;
+            own_lds();
+            const bool odd = at + kTile > length && mover.odd(s_k + kHalf);
+            rows.step(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
         }
 
         // the waves' sums together
@@ -850,19 +789,18 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
         float *s_o = reinterpret_cast<float *>(s_own);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            l[n] += __shfl_xor(l[n], 16);
-            l[n] += __shfl_xor(l[n], 32);
+            float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
+            l += __shfl_xor(l, 32);
             if (g == 0) {
-                s_m[wave][n * 16 + col] = m[n];
-                s_l[wave][n * 16 + col] = l[n];
+                s_m[wave][n * 16 + col] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+                s_l[wave][n * 16 + col] = l;
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = o[n][i];
+            for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = rows.o[n][i];
         }
         __syncthreads();
-        const bool whole = part_begin == item_begin && part_end == item_begin + seq.units;
-        float *part = whole ? nullptr : part_of<D>(p, rank, slot_of(part_begin, share_begin));
-        for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+        float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
+        for (int i = threadIdx.x; i < walk.rows * (D / 4); i += THREADS) {
             const int r = i / (D / 4), c = i % (D / 4) * 4;
             float most = s_m[0][r];
 #pragma unroll
@@ -872,11 +810,11 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float f = weight_of(s_m[w][r], most);
-                sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kWave + (r * (D + 4) + c) * 4) * f;
+                sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kOwn + (r * (D + 4) + c) * 4) * f;
                 all += s_l[w][r] * f;
             }
-            if (whole) {
-                if (c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
+            if (walk.whole) {
+                if (c < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, c, sum, all, most);
             } else {
                 *reinterpret_cast<f32x4 *>(part + r * D + c) = sum;
                 if (c == 0) {
@@ -886,11 +824,90 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             }
         }
         __syncthreads();
-        if (p.d != D && part_end < share_end) {
-            for (int i = threadIdx.x; i < WAVES * kWave / 16; i += THREADS) reinterpret_cast<f32x4 *>(s_raw)[i] = (f32x4)0.f;
-            zeroed = true;
+    }
+}
+
+// Many rows: a wave has 16 NQ of them, and the work-group's waves share its tiles of K
+// and V, of which each brings a fourth.  One barrier a tile: the one on its way goes
+// where the one before the last was read.
+template <typename T, int D>
+constexpr int wide_tile() { return D * (int)sizeof(T) <= 256 ? 64 : 32; }
+
+template <typename T, int D, int NQ, bool COPIED>
+__global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel(Args p)
+{
+    typedef Lds<T, D> L;
+    constexpr int N = D / 16, ROWS = 64 * NQ, TILE = wide_tile<T, D>(), OWN = TILE / 4, kHalf = TILE * L::kRow;
+    __shared__ __align__(16) char s_raw[4 * kHalf];
+    __shared__ typename Line<256>::Shared s_line;
+    __shared__ float s_scratch[4][kTile * 16];
+    __shared__ int s_odd[2][4];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
+    PK_WALK(256);
+    Mover<T, D, OWN, COPIED> mover(p, wave * OWN);
+    Rows<T, D, NQ> rows;
+
+    for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
+        walk.at(p, line, u);
+        mover.head(walk.b, walk.head);
+        const int end = walk.end, length = walk.seq.length, row0 = wave * 16 * NQ;
+        int at = walk.begin - TILE, stage = 0;
+        int page = -1, next = mover.page_at(at + TILE + lane % TILE, end);
+        const bool mine = row0 < walk.rows;
+        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + (mine ? row0 : 0), walk.row0 + walk.rows, mover.chunks);
+        for (bool first = true; at < end; at += TILE, first = false) {
+            char *const s_k = s_raw + stage * 2 * kHalf, *const s_v = s_k + kHalf;
+            const uint64_t there = __ballot(page >= 0);
+            const bool drafted = at + TILE > length;
+            if (!first) {
+                mover.end(there >> wave * OWN, s_k, s_v);
+                if (drafted) {
+                    own_lds();
+                    const bool odd = mover.odd(s_v);
+                    if (lane == 0) s_odd[stage][wave] = odd;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+            const int now = stage;
+            stage ^= 1;
+            char *const s_next = s_raw + stage * 2 * kHalf;
+            if (at + TILE < end) mover.begin(at + TILE, __shfl(next, wave * OWN + lane % OWN), s_next, s_next + kHalf);
+            page = next;
+            next = mover.page_at(at + 2 * TILE + lane % TILE, end);
+            if (first || !mine) continue;
+            bool odd = false;
+            if (drafted) odd = s_odd[now][0] | s_odd[now][1] | s_odd[now][2] | s_odd[now][3];
+#pragma unroll 1
+            for (int h = 0; h < TILE; h += kTile) {
+                const unsigned here = (unsigned)(there >> h);
+                if (here) rows.step(p, s_k + h * L::kRow, s_v + h * L::kRow, at + h, length, here, odd, mover.chunks, s_scratch[wave]);
+            }
         }
-        u = part_end;
+
+        float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int r = row0 + n * 16 + col;
+            float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
+            l += __shfl_xor(l, 32);
+            const float m = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+            if (r >= walk.rows) continue;
+            if (walk.whole) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i * 16 + g * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, i * 16 + g * 4, rows.o[n][i], l, m);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(part + r * D + i * 16 + g * 4) = rows.o[n][i];
+                if (g == 0) {
+                    part[ROWS * D + r] = m;
+                    part[ROWS * (D + 1) + r] = l;
+                }
+            }
+        }
+        __syncthreads();  // the last tile has been read
     }
 }
 
@@ -923,7 +940,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned gro
         const unsigned from = (first + i) * each;
         return part_of<D>(p, first + i, slot_of(i ? from : begin, from));
     };
-    // lanes to a part's sums: a power of two
+    // lanes to a part's sums: a power of two (with turns, one round: all elements have a lane)
     int lanes = D / 4;
     while (lanes < rows * (D / 4) && lanes < kJoinThreads) lanes *= 2;
     const int turns = kJoinThreads / lanes, turn = threadIdx.x / lanes;
@@ -932,35 +949,43 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned gro
         const bool on = r < rows;
         float most = -__builtin_inff(), all = 0.f;
         f32x4 sum = (f32x4)0.f;
+        auto add = [&](float m, float l, f32x4 o) {
+            const float top = fmaxf(most, m), f = weight_of(most, top), h = weight_of(m, top);
+            all = all * f + l * h;
+            sum = sum * f + o * h;
+            most = top;
+        };
         if (on) {
-#pragma unroll 8
-            for (unsigned w = turn; w < parts; w += turns) most = fmaxf(most, part(w)[D * most_rows + r]);
-#pragma unroll 8
-            for (unsigned w = turn; w < parts; w += turns) {
-                const float *from = part(w), f = weight_of(from[D * most_rows + r], most);
-                sum += *reinterpret_cast<const f32x4 *>(from + r * D + c) * f;
-                all += from[(D + 1) * most_rows + r] * f;
+            constexpr int AT_ONCE = 4;
+            for (unsigned w = turn; w < parts; w += turns * AT_ONCE) {
+                float m[AT_ONCE], l[AT_ONCE];
+                f32x4 o[AT_ONCE];
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    // beyond the last part: its own place again, with no weight
+                    const unsigned at = w + i * turns;
+                    const float *from = part(at < parts ? at : w);
+                    m[i] = from[D * most_rows + r];
+                    l[i] = from[(D + 1) * most_rows + r];
+                    o[i] = *reinterpret_cast<const f32x4 *>(from + r * D + c);
+                }
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
+                    if (w + i * turns < parts) add(m[i], l[i], o[i]);
             }
         }
-        // the turns' sums, two by two
-        float *mine = s_sum[threadIdx.x];
-        for (int o = turns / 2; o > 0; o /= 2) {
-            __syncthreads();
-            if (turn >= o && turn < 2 * o) {
-                mine[0] = most;
-                mine[1] = all;
+        if (turns > 1) {
+            float *mine = s_sum[threadIdx.x];
+            mine[0] = most;
+            mine[1] = all;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mine[2 + j] = sum[j];
-            }
+            for (int j = 0; j < 4; ++j) mine[2 + j] = sum[j];
             __syncthreads();
-            if (turn < o) {
-                const float *other = s_sum[threadIdx.x + o * lanes];
-                const float top = fmaxf(most, other[0]), f = weight_of(most, top), h = weight_of(other[0], top);
-                all = all * f + other[1] * h;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f + other[2 + j] * h;
-                most = top;
-            }
+            if (turn == 0)
+                for (int t = 1; t < turns; ++t) {
+                    const float *other = s_sum[threadIdx.x + t * lanes];
+                    add(other[0], other[1], f32x4{other[2], other[3], other[4], other[5]});
+                }
         }
         if (turn == 0 && on && c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
     }
@@ -972,64 +997,66 @@ int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct Form {
     int D, nq;
-    int unit;        // positions that a work-group's waves have in work
-    int64_t groups;  // work-groups
-    size_t bytes;    // of the workspace
+    bool wide;
+    int rows_shift, unit_shift;  // of an item; of a unit: what a work-group's waves have in work
+    int64_t groups;              // work-groups: what the card's LDS holds at once
     int64_t items;
+    size_t bytes;  // of the workspace
 };
 
 // Waves of stream_kernel: what a CU's LDS holds of their stages.
 constexpr int stream_waves(int row_bytes) { return row_bytes >= 1024 ? 1 : row_bytes >= 512 ? 2 : 4; }
 
-// The form of a call: the work-groups that the card holds at once.
-Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64_t capacity, int64_t most, bool copied)
+// The form of a call.  Up to 32 rows (16 of the widest heads) a wave has all of them, and
+// the waves divide the positions; more are divided over the waves.
+Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64_t capacity, int64_t most)
 {
     Form f;
     f.D = padded(d);
-    const int waves = copied ? stream_waves(f.D * size) : kWaves;
-    f.nq = most * group > 16 && f.D <= 128 ? 2 : 1;
-    f.unit = waves * kTile;
-    const int64_t items = B * heads * ((most * group + 16 * f.nq - 1) / (16 * f.nq));
-    const int64_t units = capacity <= f.unit ? 1 : (capacity + f.unit - 1) / f.unit;
-    const bool divided = items <= kMostLine / units;  // else an item is a unit
-    const int64_t line = divided ? items * units : items;
-    f.items = items;
-    if (copied)
-        f.groups = 256 * (f.D * size <= 128 ? 2 : 1);
-    else
-        f.groups = 256 * (f.D == 256 ? 1 : f.nq == 2 ? 2 : 3);
+    const int64_t rows = most * group;
+    const int row_bytes = f.D * size;
+    f.wide = rows > (f.D == 256 ? 16 : 32);
+    f.nq = f.D < 256 && rows > (f.wide ? 64 : 16) ? 2 : 1;
+    f.rows_shift = (f.wide ? 6 : 4) + (f.nq == 2);
+    const int unit = f.wide ? 128 : stream_waves(row_bytes) * kTile;
+    f.unit_shift = unit == 128 ? 7 : unit == 64 ? 6 : 5;
+    f.items = B * heads * ((rows + (1 << f.rows_shift) - 1) >> f.rows_shift);
+    const int64_t units = capacity <= unit ? 1 : (capacity + unit - 1) / unit;
+    const bool divided = f.items <= kMostLine / units;  // else an item is a unit
+    const int64_t line = divided ? f.items * units : f.items;
+    f.groups = 256 * (f.wide ? (row_bytes <= 512 ? 2 : 1) : row_bytes <= 128 ? 2 : 1);
     if (f.groups > line) f.groups = line;
-    f.bytes = units == 1 || !divided ? 0 : (size_t)f.groups * 2 * 16 * f.nq * (f.D + 2) * sizeof(float);
+    f.bytes = units == 1 || !divided ? 0 : ((size_t)f.groups * 2 * (f.D + 2) << f.rows_shift) * sizeof(float);
     return f;
 }
 
-template <typename T, int D>
-int join(const Args &a, const Form &f, bool joined, hipStream_t s)
+template <typename T, int D, int NQ, bool COPIED>
+int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
 {
+    if (f.wide) {
+        hipLaunchKernelGGL((wide_kernel<T, D, NQ, COPIED>), dim3((unsigned)f.groups), dim3(256), 0, s, a);
+    } else {
+        constexpr int WAVES = stream_waves(D * (int)sizeof(T));
+        hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES, COPIED>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
+    }
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
     if (!joined || f.groups == 1) return PK_OK;
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kJoinThreads), 0, s, a, (unsigned)f.groups);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 
-template <typename T, int D, int NQ>
-int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s)
+template <typename T, bool COPIED>
+int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
 {
-    if (copied) {
-        constexpr int WAVES = stream_waves(D * (int)sizeof(T));
-        hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
-    } else {
-        hipLaunchKernelGGL((attention_kernel<T, D, NQ>), dim3((unsigned)f.groups), dim3(kThreads), 0, s, a);
-    }
-    return join<T, D>(a, f, joined, s);
+    if (f.D == 64) return f.nq == 1 ? launch<T, 64, 1, COPIED>(a, f, joined, s) : launch<T, 64, 2, COPIED>(a, f, joined, s);
+    if (f.D == 128) return f.nq == 1 ? launch<T, 128, 1, COPIED>(a, f, joined, s) : launch<T, 128, 2, COPIED>(a, f, joined, s);
+    return launch<T, 256, 1, COPIED>(a, f, joined, s);
 }
 
 template <typename T>
 int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s)
 {
-    if (f.D == 64) return f.nq == 1 ? launch<T, 64, 1>(a, f, copied, joined, s) : launch<T, 64, 2>(a, f, copied, joined, s);
-    if (f.D == 128) return f.nq == 1 ? launch<T, 128, 1>(a, f, copied, joined, s) : launch<T, 128, 2>(a, f, copied, joined, s);
-    return launch<T, 256, 1>(a, f, copied, joined, s);
+    return copied ? launch<T, true>(a, f, joined, s) : launch<T, false>(a, f, joined, s);
 }
 
 // Whether K and V can be copied in whole chunks: 16-byte rows at 16-byte places, the
@@ -1054,10 +1081,7 @@ size_t pk_attention_tree_workspace_bytes(int dtype, int64_t d, int64_t q_heads, 
         B < 1 || B > kMostSize || P < 1 || P > kMostSize || page_size < 1 || page_size > kMostSize || most < 1 ||
         most > kMostTokens || P * page_size > kMostSize)
         return 0;
-    // either form
-    const Form a = form_of(pk::dtype_size(dtype), d, q_heads / heads, heads, B, P * page_size, most, false);
-    const Form b = form_of(pk::dtype_size(dtype), d, q_heads / heads, heads, B, P * page_size, most, true);
-    return a.bytes > b.bytes ? a.bytes : b.bytes;
+    return form_of(pk::dtype_size(dtype), d, q_heads / heads, heads, B, P * page_size, most).bytes;
 }
 
 int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_cache *cache, const int32_t *page_table,
@@ -1099,7 +1123,7 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     if ((uintptr_t)lse % 4) return api_invalid(17);
     const int64_t heads = cache->heads, group = q->heads / heads;
     const bool copied = can_copy(*cache, d, size);
-    const Form f = form_of(size, d, group, heads, B, P * cache->page_size, most, copied);
+    const Form f = form_of(size, d, group, heads, B, P * cache->page_size, most);
     if (f.items > kMostLine) return PK_ERR_NOT_SUPPORTED;
     const bool joined = f.bytes && workspace && workspace_bytes >= f.bytes;
     const Region in[7] = {of_heads(*q, M, d, size), of_cache(cache->key, cache->key_stride, *cache, d, size),
@@ -1140,20 +1164,20 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.value_place = cache->value_stride[1];
     a.value_head = cache->value_stride[2];
     a.pages = cache->pages;
-    a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.nq == 2 ? 5 : 4, -1};
-    if (joined)
-        for (a.shape.unit_shift = 0; 1 << a.shape.unit_shift < f.unit;) ++a.shape.unit_shift;
+    a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.rows_shift, joined ? f.unit_shift : -1};
     a.B = (int)B;
     a.d = (int)d;
     a.page_size = (int)cache->page_size;
     a.page_shift = -1;
     for (int i = 0; i < 31; ++i)
         if ((int64_t)1 << i == cache->page_size) a.page_shift = i;
-    a.scale = cap != 0.f ? scale / cap : scale * kLog2e;
+    a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+    a.scale = scale < 0.f ? -scale : scale == 0.f ? 1.f : scale;
+    a.scale = cap != 0.f ? a.scale / cap : a.scale * kLog2e;
     a.cap = cap * kLog2e;
     hipStream_t s = (hipStream_t)stream;
     st = dtype == PK_F32 ? launch<float>(a, f, copied, joined, s) : dtype == PK_BF16 ? launch<bf16>(a, f, copied, joined, s) : launch<f16>(a, f, copied, joined, s);
-    if (st == PK_OK) api_ran(copied ? "attention_tree_copied" : "attention_tree_read");
+    if (st == PK_OK) api_ran(f.wide ? (copied ? "attention_tree_wide" : "attention_tree_wide_read") : copied ? "attention_tree" : "attention_tree_read");
     return st;
 }
 

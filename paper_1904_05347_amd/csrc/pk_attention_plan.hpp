@@ -59,8 +59,10 @@ PK_PLAN Sequence sequence(const Shape &s, int start, int end, int length)
     q.length = length < 0 ? 0 : length > s.capacity ? s.capacity : length;
     q.keys = q.length + (int)t < s.capacity ? q.length + (int)t : s.capacity;
     q.groups = ((int)t * s.group + (1 << s.rows_shift) - 1) >> s.rows_shift;
-    // an item without positions still writes its rows
-    q.units = s.unit_shift < 0 || !q.keys ? 1 : (q.keys + (1 << s.unit_shift) - 1) >> s.unit_shift;
+    // An item without positions still writes its rows.  The last unit takes up to half a
+    // one more: a few tokens after a context of a round length are no unit of their own.
+    q.units = s.unit_shift < 0 ? 1 : (q.keys + (1 << s.unit_shift) / 2 - 1) >> s.unit_shift;
+    if (q.units < 1) q.units = 1;
     return q;
 }
 

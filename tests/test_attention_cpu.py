@@ -285,7 +285,7 @@ def test_indices_are_held_to_what_is_there(shim):
                                ctypes.c_int64(length), o)
             first, n, keys, tokens, groups, units = o
             assert 0 <= tokens <= most and (tokens == 0 or 0 <= first and first + tokens <= M)
-            assert 0 <= n <= keys <= capacity and groups * 16 >= tokens * 3 and units >= 1 and units * 128 >= keys
+            assert 0 <= n <= keys <= capacity and groups * 16 >= tokens * 3 and units >= 1 and units * 128 + 64 >= keys and (units == 1 or (units - 1) * 128 + 64 < keys)
 
 
 # ------------------------------------------------------------------ the plain forms themselves
