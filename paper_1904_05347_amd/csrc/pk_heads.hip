@@ -101,21 +101,16 @@ __device__ __forceinline__ void put(T *p, int n, const Vec<T> &v)
         if (j < n) p[j] = v[j];
 }
 
-// E weights from p on, as fp32
+// E weights from p on
 template <typename W, int E>
-__device__ __forceinline__ void get_weights(const W *p, int n, float *w)
+__device__ __forceinline__ typename Pack<W, E>::V get_weights(const W *p, int n)
 {
-#pragma unroll
-    for (int j = 0; j < E; ++j) w[j] = 0.f;
-    if (n == E) {
-        const typename Pack<W, E>::V v = *reinterpret_cast<const typename Pack<W, E>::U *>(p);
-#pragma unroll
-        for (int j = 0; j < E; ++j) w[j] = (float)v[j];
-        return;
-    }
+    if (n == E) return *reinterpret_cast<const typename Pack<W, E>::U *>(p);
+    typename Pack<W, E>::V v = (typename Pack<W, E>::V)(W)0.f;
 #pragma unroll
     for (int j = 0; j < E; ++j)
-        if (j < n) w[j] = (float)p[j];
+        if (j < n) v[j] = p[j];
+    return v;
 }
 
 // The sum of v over the lanes of a team, in each of them.  Every lane of the wave
@@ -154,39 +149,44 @@ __device__ __forceinline__ void make_turns(const HeadsArgs &p, float2 *turns, in
     }
 }
 
-// The pairs of z (a's E values, then b's) turned; `back`: by the opposite angle.
+// A lane's pairs: cos and sin of each.
 template <int E>
-__device__ __forceinline__ void rotate(float *z, const float2 *turns, int n, bool interleaved, float back)
-{
-    float2 t[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) t[j] = j < n ? turns[j] : make_float2(0.f, 0.f);
-    if (interleaved) {
+struct Turns {
+    float c[E], s[E];
+    __device__ __forceinline__ void load(const float2 *turns, int n)
+    {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const float a = z[2 * j], b = z[2 * j + 1], s = t[j].y * back;
-            z[2 * j] = fmaf(a, t[j].x, -(b * s));
-            z[2 * j + 1] = fmaf(b, t[j].x, a * s);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float a = z[j], b = z[E + j], s = t[j].y * back;
-            z[j] = fmaf(a, t[j].x, -(b * s));
-            z[E + j] = fmaf(b, t[j].x, a * s);
+            // (beyond the pairs: another's, for channels that are not stored)
+            const float2 t = turns[j < n ? j : 0];
+            c[j] = t.x;
+            s[j] = t.y;
         }
     }
-}
+    // The pairs of z (the first vector's E values, then the second's) turned; BACK: by the
+    // opposite angle.
+    template <bool INTERLEAVED, bool BACK>
+    __device__ __forceinline__ void rotate(float *z) const
+    {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int ia = INTERLEAVED ? 2 * j : j, ib = INTERLEAVED ? 2 * j + 1 : E + j;
+            const float a = z[ia], b = z[ib], t = BACK ? -s[j] : s[j];
+            z[ia] = fmaf(a, c[j], -(b * t));
+            z[ib] = fmaf(b, c[j], a * t);
+        }
+    }
+};
 
-// z, a row over its team, times 1 / sqrt(mean z^2 + eps): the factor is up * root.
-// A sum of squares that leaves the 32 bits' range, or falls where eps does not cover
-// what it loses, is taken once more of z times a power of two.
+// 1 / sqrt(mean z^2 + eps) of a row z over its team: z times up times root is the row
+// normed.  A sum of squares that leaves the 32 bits' range, or falls where eps does not
+// cover what it loses, is taken once more of z times a power of two.
 struct Factor {
     float up, root;
 };
 
 template <int E>
-__device__ __forceinline__ Factor norm(float *z, int d, int team, float eps)
+__device__ __forceinline__ Factor norm(const float *z, int d, int team, float eps)
 {
     float ss = 0.f;
 #pragma unroll
@@ -199,40 +199,89 @@ __device__ __forceinline__ Factor norm(float *z, int d, int team, float eps)
         ss = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * E; ++j) {
-            z[j] *= f.up;
-            ss = fmaf(z[j], z[j], ss);
+            const float y = z[j] * f.up;
+            ss = fmaf(y, y, ss);
         }
         ss = team_sum(ss, team);
         eps = eps * f.up * f.up;  // one by one: 2^200 is no fp32 number
     }
     f.root = 1.f / sqrtf(ss / (float)d + eps);
-#pragma unroll
-    for (int j = 0; j < 2 * E; ++j) z[j] *= f.root;
     return f;
 }
 
-// One token's heads are its queries', its keys', then its values'.
-template <typename T, typename W>
+// How a call's pairs lie.
+enum { UNTURNED, HALVES, NEIGHBOURS };
+
+// Which of its work-group's tokens and of their rows a team begins with.
+struct Slot {
+    int t, r;
+    __device__ __forceinline__ explicit Slot(const HeadsArgs &p)
+    {
+        const int slot = threadIdx.x >> p.team_shift;
+        t = 0;
+        r = slot;
+        if (p.tokens > 1) {
+            t = slot / p.rows;
+            r = t < p.tokens ? slot - t * p.rows : p.rows;
+        }
+    }
+};
+
+// One token's heads are its queries', its keys', then its values'.  Bound by memory
+// where tokens are many: 8192 tokens of 40 heads of 128 bf16, 168 MB.
+template <typename T, typename W, bool NORM, int PAIRS>
 __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T);
+    typedef typename Pack<W, E>::V VW;
     extern __shared__ float2 s_turns[];
-    const int c = threadIdx.x & (p.team - 1), slot = threadIdx.x >> p.team_shift;
-    int t = 0, r = slot;
-    if (p.tokens > 1) {
-        t = slot / p.rows;
-        r = t < p.tokens ? slot - t * p.rows : p.rows;
-    }
-    const int64_t first = p.first + (int64_t)blockIdx.x * p.tokens, m = first + t;
-    const Chunk ck = chunk_of<E>(c, p.d, p.pairs, p.pair_chunks, p.interleaved);
+    const int c = threadIdx.x & (p.team - 1);
+    const Slot slot(p);
+    int r = slot.r;
+    const int64_t first = p.first + (int64_t)blockIdx.x * p.tokens, m = first + slot.t;
+    const Chunk ck = chunk_of<E>(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, PAIRS == NEIGHBOURS);
     const Chunk cv = chunk_of<E>(c, p.d, 0, 0, false);
-    const float2 *turns = s_turns + t * p.pairs + c * E;
 
-    // the token's place in the cache
-    int64_t page = 0, place = 0;
-    bool kept = true;
-    if (p.slots && m < p.M) {
+    struct Row {
+        Vec<T> a, b;
+        VW wa, wb;
+        T *to;
+        bool on, plain, weighed;
+    };
+    // a row's channels, and its weights, on their way
+    auto fetch = [&](int row) {
+        Row x;
+        x.on = m < p.M && row < p.rows;
+        x.plain = row >= p.Hq + p.Hk;
+        x.weighed = false;
+        x.a = x.b = (Vec<T>)(T)0.f;
+        x.wa = x.wb = (VW)(W)1.f;
+        x.to = nullptr;
+        if (!x.on) return x;
+        const bool query = row < p.Hq;
+        const int h = query ? row : x.plain ? row - p.Hq - p.Hk : row - p.Hq;
+        const Place &from = query ? p.q : x.plain ? p.v : p.k;
+        const T *at = (const T *)from.p + m * from.token + h * from.head;
+        const Chunk &k = x.plain ? cv : ck;
+        x.a = get(at + k.oa, k.na);
+        x.b = get(at + k.ob, k.nb);
+        if constexpr (NORM) {
+            const W *w = (const W *)(query ? p.q_weight : p.k_weight);
+            x.weighed = w && !x.plain;
+            if (x.weighed) {
+                x.wa = get_weights<W, E>(w + k.oa, k.na);
+                x.wb = get_weights<W, E>(w + k.ob, k.nb);
+            }
+        }
+        const Place &to = query ? p.q_out : x.plain ? p.v_out : p.k_out;
+        x.to = (T *)to.p + h * to.head;
+        if (query || !p.slots) {
+            x.to += m * to.token;
+            return x;
+        }
+        // the token's place in the cache
         const int64_t s = p.slots[m];
+        int64_t page, place;
         if ((uint64_t)s >> 32) {
             page = (int64_t)((uint64_t)s / (unsigned)p.page_size);
             place = s - page * p.page_size;
@@ -240,66 +289,41 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
             page = (unsigned)s / (unsigned)p.page_size;
             place = (unsigned)s - (unsigned)page * (unsigned)p.page_size;
         }
-        kept = s >= 0 && page < p.pages;
-    }
-
-    struct Row {
-        Chunk k;
-        Vec<T> a, b;
-        T *to;
-        const W *w;
-        bool on, plain;
-    };
-    auto fetch = [&](int row) {
-        Row x;
-        x.on = m < p.M && row < p.rows && (row < p.Hq || kept);
-        x.plain = row >= p.Hq + p.Hk;
-        x.k = x.plain ? cv : ck;
-        x.a = x.b = (Vec<T>)(T)0.f;
-        x.w = nullptr;
-        x.to = nullptr;
-        if (!x.on) return x;
-        const bool query = row < p.Hq;
-        const int h = query ? row : x.plain ? row - p.Hq - p.Hk : row - p.Hq;
-        const Place &from = query ? p.q : x.plain ? p.v : p.k;
-        const Place &to = query ? p.q_out : x.plain ? p.v_out : p.k_out;
-        const T *at = (const T *)from.p + m * from.token + h * from.head;
-        x.to = (T *)to.p + h * to.head + (query || !p.slots ? m * to.token
-                                                            : page * (x.plain ? p.value_page : p.key_page) + place * to.token);
-        x.a = get(at + x.k.oa, x.k.na);
-        x.b = get(at + x.k.ob, x.k.nb);
-        x.w = x.plain ? nullptr : (const W *)(query ? p.q_weight : p.k_weight);
+        x.on = s >= 0 && page < p.pages;
+        x.to += page * (x.plain ? p.value_page : p.key_page) + place * to.token;
         return x;
     };
 
     Row x = fetch(r);
-    if (p.pairs) {
+    if constexpr (PAIRS != UNTURNED) {
         make_turns(p, s_turns, first);
         __syncthreads();
     }
     for (int i = 0;;) {
-        if (p.q_weight || p.k_weight || p.pairs) {
+        if constexpr (NORM || PAIRS != UNTURNED) {
             float z[2 * E];
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 z[j] = (float)x.a[j];
                 z[E + j] = (float)x.b[j];
             }
-            if (p.q_weight || p.k_weight) {
-                float y[2 * E];
+            if constexpr (NORM) {
+                Factor f = norm<E>(z, p.d, p.team, p.eps);  // every lane of the wave, whatever its row
+                if (!x.weighed) f = {1.f, 1.f};
 #pragma unroll
-                for (int j = 0; j < 2 * E; ++j) y[j] = z[j];
-                norm<E>(y, p.d, p.team, p.eps);  // every lane of the wave, whatever its row
-                if (x.w) {
-                    float w[2 * E];
-                    get_weights<W, E>(x.w + x.k.oa, x.k.na, w);
-                    get_weights<W, E>(x.w + x.k.ob, x.k.nb, w + E);
-#pragma unroll
-                    for (int j = 0; j < 2 * E; ++j) z[j] = y[j] * w[j];
+                for (int j = 0; j < E; ++j) {
+                    z[j] = z[j] * f.up * f.root * (float)x.wa[j];
+                    z[E + j] = z[E + j] * f.up * f.root * (float)x.wb[j];
+                }
+            }
+            if constexpr (PAIRS != UNTURNED) {
+                if (ck.pair) {
+                    Turns<E> turns;
+                    turns.load(s_turns + slot.t * p.pairs + c * E, p.pairs - c * E);
+                    turns.template rotate<PAIRS == NEIGHBOURS, false>(z);
                 }
             }
             if (!x.plain) {
-                if (x.k.pair) rotate<E>(z, turns, p.pairs - c * E, p.interleaved, 1.f);
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     x.a[j] = rounded<T>(z[j]);
@@ -308,8 +332,9 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
             }
         }
         if (x.on) {
-            put(x.to + x.k.oa, x.k.na, x.a);
-            put(x.to + x.k.ob, x.k.nb, x.b);
+            const Chunk &k = x.plain ? cv : ck;
+            put(x.to + k.oa, k.na, x.a);
+            put(x.to + k.ob, k.nb, x.b);
         }
         if (++i >= p.rounds) break;
         r += p.teams;
@@ -321,91 +346,117 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
 //   dx = n (g w - u mean(g w u)),  dw = sum g u.
 // A lane has the same channels of every row, so a work-group keeps its part of dw
 // in registers over all its tokens; its rows are added up by weights_kernel in the
-// order of the work-groups.
-template <typename T, typename W>
-__global__ void __launch_bounds__(pk::kMostHeadThreads) heads_grad_kernel(HeadsArgs p)
+// order of the work-groups.  The next token's rows are on their way while one is
+// worked on.
+template <typename T, typename W, bool NORM, int PAIRS>
+__global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(HeadsArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T);
+    typedef typename Pack<W, E>::V VW;
     extern __shared__ float2 s_turns[];
-    const int c = threadIdx.x & (p.team - 1), slot = threadIdx.x >> p.team_shift;
-    int t = 0, r0 = slot;
-    if (p.tokens > 1) {
-        t = slot / p.rows;
-        r0 = t < p.tokens ? slot - t * p.rows : p.rows;
-    }
-    const Chunk ck = chunk_of<E>(c, p.d, p.pairs, p.pair_chunks, p.interleaved);
-    float sum_q[2 * E], sum_k[2 * E];
+    const int c = threadIdx.x & (p.team - 1);
+    const Slot slot(p);
+    const Chunk ck = chunk_of<E>(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, PAIRS == NEIGHBOURS);
+    constexpr int SUMS = NORM ? 2 * E : 1;
+    float sum_q[SUMS], sum_k[SUMS];
 #pragma unroll
-    for (int j = 0; j < 2 * E; ++j) sum_q[j] = sum_k[j] = 0.f;
+    for (int j = 0; j < SUMS; ++j) sum_q[j] = sum_k[j] = 0.f;
 
+    struct Row {
+        Vec<T> a, b, xa, xb;  // the gradient, the input
+        int64_t m;
+        int h;
+        bool on, query;
+    };
+    auto fetch = [&](int64_t first, int row) {
+        Row x;
+        x.m = first + slot.t;
+        x.on = x.m < p.M && row < p.rows;
+        x.query = row < p.Hq;
+        x.h = x.query ? row : row - p.Hq;
+        x.a = x.b = x.xa = x.xb = (Vec<T>)(T)0.f;
+        if (!x.on) return x;
+        const Place &from = x.query ? p.q : p.k;
+        const T *at = (const T *)from.p + x.m * from.token + x.h * from.head;
+        x.a = get(at + ck.oa, ck.na);
+        x.b = get(at + ck.ob, ck.nb);
+        if constexpr (NORM) {
+            if (x.query ? p.q_weight : p.k_weight) {
+                const Place &in = x.query ? p.q_in : p.k_in;
+                const T *px = (const T *)in.p + x.m * in.token + x.h * in.head;
+                x.xa = get(px + ck.oa, ck.na);
+                x.xb = get(px + ck.ob, ck.nb);
+            }
+        }
+        return x;
+    };
+
+    const int64_t step = (int64_t)gridDim.x * p.tokens;
     int half = 0;
-    for (int64_t first = (int64_t)blockIdx.x * p.tokens; first < p.M; first += (int64_t)gridDim.x * p.tokens, half ^= 1) {
-        const int64_t m = first + t;
-        float2 *turns = s_turns + half * p.tokens * p.pairs;
-        if (p.pairs) {
+    int64_t first = (int64_t)blockIdx.x * p.tokens;
+    Row x = fetch(first, slot.r);
+    for (; first < p.M; first += step, half ^= 1) {
+        float2 *turns_here = s_turns + half * p.tokens * p.pairs;
+        if constexpr (PAIRS != UNTURNED) {
             // the other half may still be read
-            make_turns(p, turns, first);
+            make_turns(p, turns_here, first);
             __syncthreads();
         }
-        turns += t * p.pairs + c * E;
-        int r = r0;
-        for (int i = 0; i < p.rounds; ++i, r += p.teams) {
-            const bool on = m < p.M && r < p.rows, query = r < p.Hq;
-            const int h = query ? r : r - p.Hq;
-            const W *weight = (const W *)(query ? p.q_weight : p.k_weight);
-            Vec<T> a = (Vec<T>)(T)0.f, b = a, xa = a, xb = a;
-            if (on) {
-                const Place &from = query ? p.q : p.k, &in = query ? p.q_in : p.k_in;
-                const T *at = (const T *)from.p + m * from.token + h * from.head;
-                a = get(at + ck.oa, ck.na);
-                b = get(at + ck.ob, ck.nb);
-                if (weight) {
-                    const T *px = (const T *)in.p + m * in.token + h * in.head;
-                    xa = get(px + ck.oa, ck.na);
-                    xb = get(px + ck.ob, ck.nb);
-                }
-            }
+        int r = slot.r;
+        for (int i = 0; i < p.rounds; ++i) {
+            const Row now = x;
+            if (i + 1 < p.rounds)
+                x = fetch(first, r + p.teams);
+            else
+                x = fetch(first + step, slot.r);
+            r += p.teams;
+            const W *weight = NORM ? (const W *)(now.query ? p.q_weight : p.k_weight) : nullptr;
             float g[2 * E];
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                g[j] = (float)a[j];
-                g[E + j] = (float)b[j];
+                g[j] = (float)now.a[j];
+                g[E + j] = (float)now.b[j];
             }
-            if (ck.pair) rotate<E>(g, turns, p.pairs - c * E, p.interleaved, -1.f);
-            if (p.q_weight || p.k_weight) {
-                float u[2 * E], w[2 * E], dot = 0.f;
+            if constexpr (PAIRS != UNTURNED) {
+                if (ck.pair) {
+                    Turns<E> turns;
+                    turns.load(turns_here + slot.t * p.pairs + c * E, p.pairs - c * E);
+                    turns.template rotate<PAIRS == NEIGHBOURS, true>(g);
+                }
+            }
+            if constexpr (NORM) {
+                float u[2 * E], dot = 0.f;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    u[j] = (float)xa[j];
-                    u[E + j] = (float)xb[j];
+                    u[j] = (float)now.xa[j];
+                    u[E + j] = (float)now.xb[j];
                 }
                 const Factor f = norm<E>(u, p.d, p.team, p.eps);
-                if (on && weight) {
-                    get_weights<W, E>(weight + ck.oa, ck.na, w);
-                    get_weights<W, E>(weight + ck.ob, ck.nb, w + E);
-                    // rows that are not there, and sides without a weight, add nothing
-                    if (query) {
-#pragma unroll
-                        for (int j = 0; j < 2 * E; ++j) sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 2 * E; ++j) sum_k[j] = fmaf(g[j], u[j], sum_k[j]);
-                    }
+                // rows that are not there, and sides without a weight, add nothing
+                const bool weighed = now.on && weight;
+                if (weighed) {
+                    const VW wa = get_weights<W, E>(weight + ck.oa, ck.na), wb = get_weights<W, E>(weight + ck.ob, ck.nb);
 #pragma unroll
                     for (int j = 0; j < 2 * E; ++j) {
-                        w[j] *= g[j];
-                        dot = fmaf(w[j], u[j], dot);
+                        u[j] = u[j] * f.up * f.root;
+                        if (now.query)
+                            sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
+                        else
+                            sum_k[j] = fmaf(g[j], u[j], sum_k[j]);
+                        g[j] *= (float)(j < E ? wa[j % E] : wb[j % E]);
+                        dot = fmaf(g[j], u[j], dot);
                     }
                 }
                 dot = team_sum(dot, p.team) / (float)p.d;
-                if (on && weight) {
+                if (weighed) {
 #pragma unroll
-                    for (int j = 0; j < 2 * E; ++j) g[j] = fmaf(-u[j], dot, w[j]) * f.root * f.up;
+                    for (int j = 0; j < 2 * E; ++j) g[j] = fmaf(-u[j], dot, g[j]) * f.root * f.up;
                 }
             }
-            if (on) {
-                const Place &to = query ? p.q_out : p.k_out;
-                T *at = (T *)to.p + m * to.token + h * to.head;
+            if (now.on) {
+                const Place &to = now.query ? p.q_out : p.k_out;
+                T *at = (T *)to.p + now.m * to.token + now.h * to.head;
+                Vec<T> a, b;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     a[j] = rounded<T>(g[j]);
@@ -416,56 +467,60 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_grad_kernel(HeadsA
             }
         }
     }
-    if (!p.q_weight && !p.k_weight) return;
-
-    // over the teams of a wave, then over the waves
-    for (int o = p.team; o < 64; o *= 2) {
+    if constexpr (NORM) {
+        // over the teams of a wave, then over the waves
+        for (int o = p.team; o < 64; o *= 2) {
 #pragma unroll
-        for (int j = 0; j < 2 * E; ++j) {
-            sum_q[j] += __shfl_xor(sum_q[j], o);
-            sum_k[j] += __shfl_xor(sum_k[j], o);
-        }
-    }
-    float *s_sum = (float *)s_turns;
-    __syncthreads();  // the turns have been read
-    const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
-    if (threadIdx.x % 64 < p.team) {
-        float *q = s_sum + wave * 2 * p.d, *k = q + p.d;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if (j < ck.na) {
-                q[ck.oa + j] = sum_q[j];
-                k[ck.oa + j] = sum_k[j];
-            }
-            if (j < ck.nb) {
-                q[ck.ob + j] = sum_q[E + j];
-                k[ck.ob + j] = sum_k[E + j];
+            for (int j = 0; j < 2 * E; ++j) {
+                sum_q[j] += __shfl_xor(sum_q[j], o);
+                sum_k[j] += __shfl_xor(sum_k[j], o);
             }
         }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * p.d; i += blockDim.x) {
-        float v = 0.f;
-        for (int w = 0; w < waves; ++w) v += s_sum[w * 2 * p.d + i];
-        p.partial[(int64_t)blockIdx.x * 2 * p.d + i] = v;
+        float *s_sum = (float *)s_turns;
+        __syncthreads();  // the turns have been read
+        const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+        if (threadIdx.x % 64 < p.team) {
+            float *q = s_sum + wave * 2 * p.d, *k = q + p.d;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if (j < ck.na) {
+                    q[ck.oa + j] = sum_q[j];
+                    k[ck.oa + j] = sum_k[j];
+                }
+                if (j < ck.nb) {
+                    q[ck.ob + j] = sum_q[E + j];
+                    k[ck.ob + j] = sum_k[E + j];
+                }
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * p.d; i += blockDim.x) {
+            float v = 0.f;
+            for (int w = 0; w < waves; ++w) v += s_sum[w * 2 * p.d + i];
+            p.partial[(int64_t)blockIdx.x * 2 * p.d + i] = v;
+        }
     }
 }
 
-// The rows of `partial` added up, 64 columns a work-group, sixteen lanes a column.
+// The rows of `partial` added up: 16 columns a work-group, 64 lanes a column.
 template <typename W>
 __global__ void __launch_bounds__(1024) weights_kernel(const float *partial, int groups, int d, W *q, W *k)
 {
-    __shared__ float s_v[16][64];
-    const int x = threadIdx.x % 64, y = threadIdx.x / 64, col = blockIdx.x * 64 + x;
+    __shared__ float s_v[16][17];
+    const int x = threadIdx.x % 16, y = threadIdx.x / 16, col = blockIdx.x * 16 + x;
     float v = 0.f;
     if (col < 2 * d) {
-#pragma unroll 8
-        for (int g = y; g < groups; g += 16) v += partial[(int64_t)g * 2 * d + col];
+#pragma unroll 16
+        for (int g = y; g < groups; g += 64) v += partial[(int64_t)g * 2 * d + col];
     }
-    s_v[y][x] = v;
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    if (y % 4 == 0) s_v[y / 4][x] = v;
     __syncthreads();
     if (y || col >= 2 * d) return;
-    for (int i = 1; i < 16; ++i) v += s_v[i][x];
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += s_v[i][x];
     W *to = col < d ? q : k;
     if (to) to[col < d ? col : col - d] = (W)v;
 }
@@ -473,7 +528,7 @@ __global__ void __launch_bounds__(1024) weights_kernel(const float *partial, int
 // ---------------------------------------------------------------- launches
 
 constexpr int64_t kMostGroups = 1 << 22;  // of a launch: 512 work-items each stay below 2^32
-constexpr int kGradGroups = 1024;         // four work-groups a CU
+constexpr int kGradGroups = 1024;         // rows of partial sums, at most
 
 int log2_of(int v)
 {
@@ -497,40 +552,75 @@ pk::HeadGroup lay_out(HeadsArgs &a, int rows, int size)
     return g;
 }
 
-template <typename T, typename W>
+template <typename T, typename W, bool NORM, int PAIRS>
 int launch_heads(HeadsArgs a, int rows, hipStream_t s)
 {
     const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
     const size_t lds = (size_t)a.tokens * a.pairs * sizeof(float2);
     for (int64_t left = (a.M + a.tokens - 1) / a.tokens; left > 0; left -= kMostGroups) {
         const int64_t now = left < kMostGroups ? left : kMostGroups;
-        hipLaunchKernelGGL((heads_kernel<T, W>), dim3((unsigned)now), dim3(g.threads), lds, s, a);
+        hipLaunchKernelGGL((heads_kernel<T, W, NORM, PAIRS>), dim3((unsigned)now), dim3(g.threads), lds, s, a);
         if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
         a.first += now * a.tokens;
     }
     return PK_OK;
 }
 
-template <typename T, typename W>
-int launch_grad(HeadsArgs a, int rows, void *q_weight_grad, void *k_weight_grad, hipStream_t s)
+template <typename T, typename W, bool NORM, int PAIRS>
+int launch_grad(HeadsArgs a, int rows, int64_t *groups, hipStream_t s)
+{
+    const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
+    // what the card holds at once, by the registers (four waves a SIMD)
+    const int resident = (NORM ? 12 : 20) / (g.threads / 64) > 0 ? (NORM ? 12 : 20) / (g.threads / 64) : 1;
+    *groups = (a.M + a.tokens - 1) / a.tokens;
+    if (*groups > 256 * resident) *groups = 256 * resident;
+    if (*groups > kGradGroups) *groups = kGradGroups;
+    size_t lds = (size_t)2 * a.tokens * a.pairs * sizeof(float2);
+    const size_t sums = NORM ? (size_t)(g.threads / 64) * 2 * a.d * sizeof(float) : 0;
+    if (lds < sums) lds = sums;
+    hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
+    return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
+}
+
+// The instance for a call's types, weights and pairs.
+#define PK_HEADS(FN, T, W, NORM, ...)                                  \
+    (!a.pairs         ? FN<T, W, NORM, UNTURNED>(__VA_ARGS__)          \
+     : a.interleaved  ? FN<T, W, NORM, NEIGHBOURS>(__VA_ARGS__)        \
+                      : FN<T, W, NORM, HALVES>(__VA_ARGS__))
+#define PK_HEADS_TYPES(FN, ...)                                                                                       \
+    (!a.q_weight && !a.k_weight ? (dtype == PK_F32    ? PK_HEADS(FN, float, float, false, __VA_ARGS__)                 \
+                                   : dtype == PK_BF16 ? PK_HEADS(FN, bf16, bf16, false, __VA_ARGS__)                   \
+                                                      : PK_HEADS(FN, f16, f16, false, __VA_ARGS__))                    \
+     : dtype == PK_F32         ? PK_HEADS(FN, float, float, true, __VA_ARGS__)                                         \
+     : weight_dtype == PK_F32  ? (dtype == PK_BF16 ? PK_HEADS(FN, bf16, float, true, __VA_ARGS__)                       \
+                                                   : PK_HEADS(FN, f16, float, true, __VA_ARGS__))                       \
+     : dtype == PK_BF16        ? PK_HEADS(FN, bf16, bf16, true, __VA_ARGS__)                                           \
+                               : PK_HEADS(FN, f16, f16, true, __VA_ARGS__))
+
+int run_heads(int dtype, int weight_dtype, const HeadsArgs &a, int rows, hipStream_t s)
+{
+    return PK_HEADS_TYPES(launch_heads, a, rows, s);
+}
+
+template <typename W>
+int launch_weights(const HeadsArgs &a, int64_t groups, void *q, void *k, hipStream_t s)
+{
+    hipLaunchKernelGGL((weights_kernel<W>), dim3((2 * a.d + 15) / 16), dim3(1024), 0, s, a.partial, (int)groups, a.d, (W *)q,
+                       (W *)k);
+    return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
+}
+
+int run_grad(int dtype, int weight_dtype, const HeadsArgs &a, int rows, void *q_weight_grad, void *k_weight_grad, hipStream_t s)
 {
     int64_t groups = 0;
     if (rows && a.M) {
-        const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
-        groups = (a.M + a.tokens - 1) / a.tokens;
-        if (groups > kGradGroups) groups = kGradGroups;
-        size_t lds = (size_t)2 * a.tokens * a.pairs * sizeof(float2);
-        const size_t sums = (size_t)(g.threads / 64) * 2 * a.d * sizeof(float);
-        if (lds < sums) lds = sums;
-        hipLaunchKernelGGL((heads_grad_kernel<T, W>), dim3((unsigned)groups), dim3(g.threads), lds, s, a);
-        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
+        const int st = PK_HEADS_TYPES(launch_grad, a, rows, &groups, s);
+        if (st != PK_OK) return st;
     }
-    if (q_weight_grad || k_weight_grad) {
-        hipLaunchKernelGGL((weights_kernel<W>), dim3((2 * a.d + 63) / 64), dim3(1024), 0, s, a.partial, (int)groups, a.d,
-                           (W *)q_weight_grad, (W *)k_weight_grad);
-        if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
-    }
-    return PK_OK;
+    if (!q_weight_grad && !k_weight_grad) return PK_OK;
+    return weight_dtype == PK_F32    ? launch_weights<float>(a, groups, q_weight_grad, k_weight_grad, s)
+           : weight_dtype == PK_BF16 ? launch_weights<bf16>(a, groups, q_weight_grad, k_weight_grad, s)
+                                     : launch_weights<f16>(a, groups, q_weight_grad, k_weight_grad, s);
 }
 
 // What every call checks of its rotation: 0, or the status.
@@ -568,12 +658,6 @@ bool over_small(const pk::heads::Region &out, const pk_rotation *rot, int64_t M,
         return true;
     return (qw && shared(out, flat(qw, wbytes))) || (kw && shared(out, flat(kw, wbytes)));
 }
-
-#define PK_HEADS_TYPES(FN, ...)                                                                        \
-    (dtype == PK_F32           ? FN<float, float>(__VA_ARGS__)                                         \
-     : weight_dtype == PK_F32  ? (dtype == PK_BF16 ? FN<bf16, float>(__VA_ARGS__) : FN<f16, float>(__VA_ARGS__)) \
-     : dtype == PK_BF16        ? FN<bf16, bf16>(__VA_ARGS__)                                           \
-                               : FN<f16, f16>(__VA_ARGS__))
 
 }  // namespace
 
@@ -628,7 +712,7 @@ int pk_rope_qk(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_head
     a.d = (int)d;
     a.eps = eps;
     set_rotation(a, rotation);
-    st = PK_HEADS_TYPES(launch_heads, a, (int)(Hq + Hk), (hipStream_t)stream);
+    st = run_heads(dtype, weight_dtype, a, (int)(Hq + Hk), (hipStream_t)stream);
     if (st == PK_OK) api_ran("rope_qk");
     return st;
 }
@@ -724,7 +808,7 @@ int pk_rope_qk_backward(int dtype, int64_t M, int64_t d, const pk_heads *dq, con
     a.d = (int)d;
     a.eps = eps;
     set_rotation(a, rotation);
-    st = PK_HEADS_TYPES(launch_grad, a, (int)(Hq + Hk), q_weight_grad, k_weight_grad, (hipStream_t)stream);
+    st = run_grad(dtype, weight_dtype, a, (int)(Hq + Hk), q_weight_grad, k_weight_grad, (hipStream_t)stream);
     if (st == PK_OK) api_ran("rope_qk_backward");
     return st;
 }
@@ -791,7 +875,7 @@ int pk_cache_append(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk
     a.d = (int)d;
     a.eps = eps;
     set_rotation(a, rotation);
-    st = PK_HEADS_TYPES(launch_heads, a, (int)(Hq + 2 * Hk), (hipStream_t)stream);
+    st = run_heads(dtype, weight_dtype, a, (int)(Hq + 2 * Hk), (hipStream_t)stream);
     if (st == PK_OK) api_ran("cache_append");
     return st;
 }
