@@ -22,95 +22,93 @@ using pk::f16;
 using pk::Pack;
 using pk::rounded;
 
-// Where a side's heads lie: m * token + h * head, in elements.
+// Where a side's heads lie: m * token + h * head, in elements.  (32 bits: a product of
+// two and its sum to an address are one instruction.)
 struct Place {
     void *p;
-    int64_t token, head;
+    unsigned token, head;
+    template <typename T>
+    __device__ __forceinline__ T *at(unsigned m, unsigned h) const
+    {
+        return (T *)p + ((uint64_t)m * token + (uint64_t)h * head);
+    }
+};
+
+// The same of a cache.
+struct Pages {
+    void *p;
+    int64_t page, place, head;
 };
 
 struct HeadsArgs {
-    Place q, k, v, q_out, k_out, v_out;  // gradient: q_out, k_out the inputs' gradients
-    Place q_in, k_in;                    // gradient: the forward call's inputs
+    Place q, k, v, q_out, k_out;  // gradient: q_out, k_out the inputs' gradients
+    Place q_in, k_in;             // gradient: the forward call's inputs
+    Pages key, value;             // cache: where k and v go
     const void *q_weight, *k_weight;
-    const int64_t *slots;  // cache: where k and v go
+    const int64_t *slots;  // cache: a position for each token
     const int64_t *positions;
     const double *frequencies;
     float *partial;  // gradient of the weights: a row of 2 d for each work-group
-    int64_t first, M;
-    int64_t pages, key_page, value_page;  // cache: k_out.token and v_out.token are a position's strides
+    int64_t pages;
+    unsigned first, M;
     int page_size, Hq, Hk, rows;
-    int d, pairs, pair_chunks, team, team_shift, teams, tokens, rounds, interleaved;
-    float amplitude, eps;
+    int d, pairs, pair_chunks, chunks, team, team_shift, teams, tokens, rounds, interleaved;
+    float amplitude, eps, inv_d;
 };
 
-// The channels of a lane's two vectors: a at oa (na of them), b at ob (nb).
+// The channels of a lane's two vectors: a at oa (na of them), b at ob (nb).  FULL: all of
+// them, or (on false) none.
+template <int E, bool FULL>
 struct Chunk {
     int oa, na, ob, nb;
-    bool pair;
-};
-
-template <int E>
-__device__ __forceinline__ Chunk chunk_of(int c, int d, int pairs, int pair_chunks, bool interleaved)
-{
-    Chunk k;
-    k.pair = c < pair_chunks;
-    int end = d, at = 2 * pairs + (c - pair_chunks) * 2 * E;
-    if (k.pair) {
-        end = 2 * pairs;
-        at = c * 2 * E;
-        if (!interleaved) {
-            k.oa = c * E;
-            k.ob = pairs + c * E;
-            k.na = k.nb = pairs - c * E < E ? pairs - c * E : E;
-            return k;
+    bool pair, on;
+    __device__ __forceinline__ Chunk(int c, int d, int pairs, int pair_chunks, int chunks, bool halves)
+    {
+        pair = c < pair_chunks;
+        on = c < chunks;
+        const int at = (pair ? c : c - pair_chunks) * 2 * E + (pair ? 0 : 2 * pairs);
+        oa = pair && halves ? c * E : at;
+        ob = pair && halves ? pairs + c * E : at + E;
+        na = nb = E;
+        if constexpr (!FULL) {
+            if (pair && halves) {
+                na = nb = pairs - c * E < E ? pairs - c * E : E;
+            } else {
+                const int n = (pair ? 2 * pairs : d) - at;
+                na = n < 0 ? 0 : n < E ? n : E;
+                nb = n < E ? 0 : n < 2 * E ? n - E : E;
+            }
         }
     }
-    const int n = end - at;
-    k.oa = at;
-    k.ob = at + E;
-    k.na = n < 0 ? 0 : n < E ? n : E;
-    k.nb = n < E ? 0 : n < 2 * E ? n - E : E;
-    return k;
-}
+};
 
 template <typename T>
 using Vec = typename Pack<T>::V;
 
-template <typename T>
-__device__ __forceinline__ Vec<T> get(const T *p, int n)
+// N elements from p on, of which n are there (N of them, where FULL).
+template <bool FULL, typename T, int N = 16 / (int)sizeof(T)>
+__device__ __forceinline__ typename Pack<T, N>::V get(const T *p, int n)
 {
-    constexpr int E = 16 / (int)sizeof(T);
-    if (n == E) return *reinterpret_cast<const typename Pack<T>::U *>(p);
-    Vec<T> v = (Vec<T>)(T)0.f;
+    typedef typename Pack<T, N>::V V;
+    if (FULL || n == N) return *reinterpret_cast<const typename Pack<T, N>::U *>(p);
+    V v = (V)(T)0.f;
 #pragma unroll
-    for (int j = 0; j < E; ++j)
+    for (int j = 0; j < N; ++j)
         if (j < n) v[j] = p[j];
     return v;
 }
 
-template <typename T>
+template <bool FULL, typename T>
 __device__ __forceinline__ void put(T *p, int n, const Vec<T> &v)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    if (n == E) {
+    if (FULL || n == E) {
         *reinterpret_cast<typename Pack<T>::U *>(p) = v;
         return;
     }
 #pragma unroll
     for (int j = 0; j < E; ++j)
         if (j < n) p[j] = v[j];
-}
-
-// E weights from p on
-template <typename W, int E>
-__device__ __forceinline__ typename Pack<W, E>::V get_weights(const W *p, int n)
-{
-    if (n == E) return *reinterpret_cast<const typename Pack<W, E>::U *>(p);
-    typename Pack<W, E>::V v = (typename Pack<W, E>::V)(W)0.f;
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-        if (j < n) v[j] = p[j];
-    return v;
 }
 
 // The sum of v over the lanes of a team, in each of them.  Every lane of the wave
@@ -140,11 +138,11 @@ __device__ __forceinline__ float2 turn_of(int64_t position, double frequency, fl
 }
 
 // The turns of `tokens` tokens from `first` on.
-__device__ __forceinline__ void make_turns(const HeadsArgs &p, float2 *turns, int64_t first)
+__device__ __forceinline__ void make_turns(const HeadsArgs &p, float2 *turns, unsigned first)
 {
     for (int i = threadIdx.x; i < p.tokens * p.pairs; i += blockDim.x) {
-        const int t = i / p.pairs;
-        const int64_t m = first + t;
+        const int t = p.tokens > 1 ? i / p.pairs : 0;
+        const unsigned m = first + t;
         turns[i] = m < p.M ? turn_of(p.positions[m], p.frequencies[i - t * p.pairs], p.amplitude) : make_float2(0.f, 0.f);
     }
 }
@@ -153,12 +151,13 @@ __device__ __forceinline__ void make_turns(const HeadsArgs &p, float2 *turns, in
 template <int E>
 struct Turns {
     float c[E], s[E];
+    template <bool FULL>
     __device__ __forceinline__ void load(const float2 *turns, int n)
     {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             // (beyond the pairs: another's, for channels that are not stored)
-            const float2 t = turns[j < n ? j : 0];
+            const float2 t = turns[FULL || j < n ? j : 0];
             c[j] = t.x;
             s[j] = t.y;
         }
@@ -178,35 +177,34 @@ struct Turns {
     }
 };
 
-// 1 / sqrt(mean z^2 + eps) of a row z over its team: z times up times root is the row
-// normed.  A sum of squares that leaves the 32 bits' range, or falls where eps does not
-// cover what it loses, is taken once more of z times a power of two.
+// 1 / sqrt(mean z^2 + eps) of a row z over its team: z times root is the row normed.  A
+// sum of squares that leaves the 32 bits' range, or falls where eps does not cover what
+// it loses, is taken once more of z times a power of two, `up`, and z left so.
 struct Factor {
-    float up, root;
+    float root, up;
 };
 
 template <int E>
-__device__ __forceinline__ Factor norm(const float *z, int d, int team, float eps)
+__device__ __forceinline__ Factor norm(float *z, float inv_d, int team, float eps)
 {
     float ss = 0.f;
 #pragma unroll
     for (int j = 0; j < 2 * E; ++j) ss = fmaf(z[j], z[j], ss);
     ss = team_sum(ss, team);
-    Factor f = {1.f, 0.f};
+    float up = 1.f;
     const bool above = !(ss < 0x1p120f), below = ss < 0x1p-80f && eps < 0x1p-100f;
     if (__any(above || below)) {  // the whole wave: the sum is across lanes
-        f.up = above ? 0x1p-70f : below ? 0x1p100f : 1.f;
+        up = above ? 0x1p-70f : below ? 0x1p100f : 1.f;
         ss = 0.f;
 #pragma unroll
         for (int j = 0; j < 2 * E; ++j) {
-            const float y = z[j] * f.up;
-            ss = fmaf(y, y, ss);
+            z[j] *= up;
+            ss = fmaf(z[j], z[j], ss);
         }
         ss = team_sum(ss, team);
-        eps = eps * f.up * f.up;  // one by one: 2^200 is no fp32 number
+        eps = eps * up * up;  // one by one: 2^200 is no fp32 number
     }
-    f.root = 1.f / sqrtf(ss / (float)d + eps);
-    return f;
+    return {__builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps)), up};
 }
 
 // How a call's pairs lie.
@@ -227,9 +225,27 @@ struct Slot {
     }
 };
 
-// One token's heads are its queries', its keys', then its values'.  Bound by memory
-// where tokens are many: 8192 tokens of 40 heads of 128 bf16, 168 MB.
-template <typename T, typename W, bool NORM, int PAIRS>
+// The sides that lanes of this wave have, one after the other, each as a scalar: its
+// addresses and strides then need no selection for each lane, and most waves have
+// rows of one side.
+template <typename F>
+__device__ __forceinline__ void each_side(int side, F f)
+{
+    for (bool left = true; left;) {
+        const int s = __builtin_amdgcn_readfirstlane(side);
+        if (side == s) {
+            f(s);
+            left = false;
+        }
+    }
+}
+
+enum { QUERY, KEY, VALUE, NONE };
+
+// One token's heads are its queries', its keys', then its values'.  Few instructions
+// count here as much as bytes: a work-group for each token (several, where its heads
+// are few), whose waves' number hides what memory takes.
+template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
 __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T);
@@ -238,59 +254,56 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
     const int c = threadIdx.x & (p.team - 1);
     const Slot slot(p);
     int r = slot.r;
-    const int64_t first = p.first + (int64_t)blockIdx.x * p.tokens, m = first + slot.t;
-    const Chunk ck = chunk_of<E>(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, PAIRS == NEIGHBOURS);
-    const Chunk cv = chunk_of<E>(c, p.d, 0, 0, false);
+    const unsigned first = p.first + blockIdx.x * p.tokens, m = first + slot.t;
+    const Chunk<E, FULL> k(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, p.chunks, PAIRS == HALVES);
 
     struct Row {
         Vec<T> a, b;
         VW wa, wb;
         T *to;
-        bool on, plain, weighed;
+        int side;
+        bool weighed;
     };
     // a row's channels, and its weights, on their way
     auto fetch = [&](int row) {
         Row x;
-        x.on = m < p.M && row < p.rows;
-        x.plain = row >= p.Hq + p.Hk;
-        x.weighed = false;
         x.a = x.b = (Vec<T>)(T)0.f;
         x.wa = x.wb = (VW)(W)1.f;
         x.to = nullptr;
-        if (!x.on) return x;
-        const bool query = row < p.Hq;
-        const int h = query ? row : x.plain ? row - p.Hq - p.Hk : row - p.Hq;
-        const Place &from = query ? p.q : x.plain ? p.v : p.k;
-        const T *at = (const T *)from.p + m * from.token + h * from.head;
-        const Chunk &k = x.plain ? cv : ck;
-        x.a = get(at + k.oa, k.na);
-        x.b = get(at + k.ob, k.nb);
-        if constexpr (NORM) {
-            const W *w = (const W *)(query ? p.q_weight : p.k_weight);
-            x.weighed = w && !x.plain;
-            if (x.weighed) {
-                x.wa = get_weights<W, E>(w + k.oa, k.na);
-                x.wb = get_weights<W, E>(w + k.ob, k.nb);
+        x.weighed = false;
+        x.side = m >= p.M || row >= p.rows || !k.on ? NONE : row < p.Hq ? QUERY : row < p.Hq + p.Hk ? KEY : VALUE;
+        each_side(x.side, [&](int s) {
+            if (s == NONE) return;
+            const unsigned h = row - (s == QUERY ? 0 : s == KEY ? p.Hq : p.Hq + p.Hk);
+            const T *at = (s == QUERY ? p.q : s == KEY ? p.k : p.v).template at<const T>(m, h);
+            x.a = get<FULL>(at + k.oa, k.na);
+            x.b = get<FULL>(at + k.ob, k.nb);
+            if constexpr (NORM) {
+                const W *w = (const W *)(s == QUERY ? p.q_weight : s == KEY ? p.k_weight : nullptr);
+                if (w) {
+                    x.weighed = true;
+                    x.wa = get<FULL, W, E>(w + k.oa, k.na);
+                    x.wb = get<FULL, W, E>(w + k.ob, k.nb);
+                }
             }
-        }
-        const Place &to = query ? p.q_out : x.plain ? p.v_out : p.k_out;
-        x.to = (T *)to.p + h * to.head;
-        if (query || !p.slots) {
-            x.to += m * to.token;
-            return x;
-        }
-        // the token's place in the cache
-        const int64_t s = p.slots[m];
-        int64_t page, place;
-        if ((uint64_t)s >> 32) {
-            page = (int64_t)((uint64_t)s / (unsigned)p.page_size);
-            place = s - page * p.page_size;
-        } else {
-            page = (unsigned)s / (unsigned)p.page_size;
-            place = (unsigned)s - (unsigned)page * (unsigned)p.page_size;
-        }
-        x.on = s >= 0 && page < p.pages;
-        x.to += page * (x.plain ? p.value_page : p.key_page) + place * to.token;
+            if (s == QUERY || !p.slots) {
+                x.to = (s == QUERY ? p.q_out : p.k_out).template at<T>(m, h);
+                return;
+            }
+            // the token's place in the cache
+            const int64_t at_slot = p.slots[m];
+            int64_t page, place;
+            if ((uint64_t)at_slot >> 32) {
+                page = (int64_t)((uint64_t)at_slot / (unsigned)p.page_size);
+                place = at_slot - page * p.page_size;
+            } else {
+                page = (unsigned)at_slot / (unsigned)p.page_size;
+                place = (unsigned)at_slot - (unsigned)page * (unsigned)p.page_size;
+            }
+            const Pages &to = s == KEY ? p.key : p.value;
+            x.to = (T *)to.p + page * to.page + place * to.place + h * to.head;
+            if (at_slot < 0 || page >= p.pages) x.side = NONE;  // has no place: nothing is stored
+        });
         return x;
     };
 
@@ -308,22 +321,26 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
                 z[E + j] = (float)x.b[j];
             }
             if constexpr (NORM) {
-                Factor f = norm<E>(z, p.d, p.team, p.eps);  // every lane of the wave, whatever its row
-                if (!x.weighed) f = {1.f, 1.f};
+                float y[2 * E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    z[j] = z[j] * f.up * f.root * (float)x.wa[j];
-                    z[E + j] = z[E + j] * f.up * f.root * (float)x.wb[j];
+                for (int j = 0; j < 2 * E; ++j) y[j] = z[j];
+                const Factor f = norm<E>(y, p.inv_d, p.team, p.eps);  // every lane of the wave, whatever its row
+                if (x.weighed) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        z[j] = y[j] * f.root * (float)x.wa[j];
+                        z[E + j] = y[E + j] * f.root * (float)x.wb[j];
+                    }
                 }
             }
-            if constexpr (PAIRS != UNTURNED) {
-                if (ck.pair) {
-                    Turns<E> turns;
-                    turns.load(s_turns + slot.t * p.pairs + c * E, p.pairs - c * E);
-                    turns.template rotate<PAIRS == NEIGHBOURS, false>(z);
+            if (x.side < VALUE) {
+                if constexpr (PAIRS != UNTURNED) {
+                    if (k.pair) {
+                        Turns<E> turns;
+                        turns.template load<FULL>(s_turns + slot.t * p.pairs + c * E, p.pairs - c * E);
+                        turns.template rotate<PAIRS == NEIGHBOURS, false>(z);
+                    }
                 }
-            }
-            if (!x.plain) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     x.a[j] = rounded<T>(z[j]);
@@ -331,10 +348,9 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
                 }
             }
         }
-        if (x.on) {
-            const Chunk &k = x.plain ? cv : ck;
-            put(x.to + k.oa, k.na, x.a);
-            put(x.to + k.ob, k.nb, x.b);
+        if (x.side != NONE) {
+            put<FULL>(x.to + k.oa, k.na, x.a);
+            put<FULL>(x.to + k.ob, k.nb, x.b);
         }
         if (++i >= p.rounds) break;
         r += p.teams;
@@ -348,7 +364,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
 // in registers over all its tokens; its rows are added up by weights_kernel in the
 // order of the work-groups.  The next token's rows are on their way while one is
 // worked on.
-template <typename T, typename W, bool NORM, int PAIRS>
+template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
 __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(HeadsArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T);
@@ -356,7 +372,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
     extern __shared__ float2 s_turns[];
     const int c = threadIdx.x & (p.team - 1);
     const Slot slot(p);
-    const Chunk ck = chunk_of<E>(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, PAIRS == NEIGHBOURS);
+    const Chunk<E, FULL> ck(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, p.chunks, PAIRS == HALVES);
     constexpr int SUMS = NORM ? 2 * E : 1;
     float sum_q[SUMS], sum_k[SUMS];
 #pragma unroll
@@ -364,36 +380,36 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
 
     struct Row {
         Vec<T> a, b, xa, xb;  // the gradient, the input
-        int64_t m;
-        int h;
-        bool on, query;
+        T *to;
+        int side;
     };
-    auto fetch = [&](int64_t first, int row) {
+    auto fetch = [&](unsigned first, int row) {
         Row x;
-        x.m = first + slot.t;
-        x.on = x.m < p.M && row < p.rows;
-        x.query = row < p.Hq;
-        x.h = x.query ? row : row - p.Hq;
+        const unsigned m = first + slot.t;
         x.a = x.b = x.xa = x.xb = (Vec<T>)(T)0.f;
-        if (!x.on) return x;
-        const Place &from = x.query ? p.q : p.k;
-        const T *at = (const T *)from.p + x.m * from.token + x.h * from.head;
-        x.a = get(at + ck.oa, ck.na);
-        x.b = get(at + ck.ob, ck.nb);
-        if constexpr (NORM) {
-            if (x.query ? p.q_weight : p.k_weight) {
-                const Place &in = x.query ? p.q_in : p.k_in;
-                const T *px = (const T *)in.p + x.m * in.token + x.h * in.head;
-                x.xa = get(px + ck.oa, ck.na);
-                x.xb = get(px + ck.ob, ck.nb);
+        x.to = nullptr;
+        x.side = m >= p.M || row >= p.rows || !ck.on ? NONE : row < p.Hq ? QUERY : KEY;
+        each_side(x.side, [&](int s) {
+            if (s == NONE) return;
+            const unsigned h = row - (s == QUERY ? 0 : p.Hq);
+            const T *at = (s == QUERY ? p.q : p.k).template at<const T>(m, h);
+            x.a = get<FULL>(at + ck.oa, ck.na);
+            x.b = get<FULL>(at + ck.ob, ck.nb);
+            if constexpr (NORM) {
+                if (s == QUERY ? p.q_weight : p.k_weight) {
+                    const T *px = (s == QUERY ? p.q_in : p.k_in).template at<const T>(m, h);
+                    x.xa = get<FULL>(px + ck.oa, ck.na);
+                    x.xb = get<FULL>(px + ck.ob, ck.nb);
+                }
             }
-        }
+            x.to = (s == QUERY ? p.q_out : p.k_out).template at<T>(m, h);
+        });
         return x;
     };
 
-    const int64_t step = (int64_t)gridDim.x * p.tokens;
+    const unsigned step = gridDim.x * p.tokens;
     int half = 0;
-    int64_t first = (int64_t)blockIdx.x * p.tokens;
+    unsigned first = blockIdx.x * p.tokens;
     Row x = fetch(first, slot.r);
     for (; first < p.M; first += step, half ^= 1) {
         float2 *turns_here = s_turns + half * p.tokens * p.pairs;
@@ -404,13 +420,9 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
         }
         int r = slot.r;
         for (int i = 0; i < p.rounds; ++i) {
-            const Row now = x;
-            if (i + 1 < p.rounds)
-                x = fetch(first, r + p.teams);
-            else
-                x = fetch(first + step, slot.r);
+            Row now = x;
+            x = i + 1 < p.rounds ? fetch(first, r + p.teams) : fetch(first + step, slot.r);
             r += p.teams;
-            const W *weight = NORM ? (const W *)(now.query ? p.q_weight : p.k_weight) : nullptr;
             float g[2 * E];
 #pragma unroll
             for (int j = 0; j < E; ++j) {
@@ -420,50 +432,56 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
             if constexpr (PAIRS != UNTURNED) {
                 if (ck.pair) {
                     Turns<E> turns;
-                    turns.load(turns_here + slot.t * p.pairs + c * E, p.pairs - c * E);
+                    turns.template load<FULL>(turns_here + slot.t * p.pairs + c * E, p.pairs - c * E);
                     turns.template rotate<PAIRS == NEIGHBOURS, true>(g);
                 }
             }
             if constexpr (NORM) {
+                const W *weight = (const W *)(now.side == QUERY ? p.q_weight : p.k_weight);
                 float u[2 * E], dot = 0.f;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     u[j] = (float)now.xa[j];
                     u[E + j] = (float)now.xb[j];
                 }
-                const Factor f = norm<E>(u, p.d, p.team, p.eps);
+                const Factor f = norm<E>(u, p.inv_d, p.team, p.eps);
                 // rows that are not there, and sides without a weight, add nothing
-                const bool weighed = now.on && weight;
+                const bool weighed = now.side != NONE && weight;
                 if (weighed) {
-                    const VW wa = get_weights<W, E>(weight + ck.oa, ck.na), wb = get_weights<W, E>(weight + ck.ob, ck.nb);
+                    const VW wa = get<FULL, W, E>(weight + ck.oa, ck.na), wb = get<FULL, W, E>(weight + ck.ob, ck.nb);
+#pragma unroll
+                    for (int j = 0; j < 2 * E; ++j) u[j] *= f.root;
+                    if (now.side == QUERY) {
+#pragma unroll
+                        for (int j = 0; j < 2 * E; ++j) sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2 * E; ++j) sum_k[j] = fmaf(g[j], u[j], sum_k[j]);
+                    }
 #pragma unroll
                     for (int j = 0; j < 2 * E; ++j) {
-                        u[j] = u[j] * f.up * f.root;
-                        if (now.query)
-                            sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
-                        else
-                            sum_k[j] = fmaf(g[j], u[j], sum_k[j]);
                         g[j] *= (float)(j < E ? wa[j % E] : wb[j % E]);
                         dot = fmaf(g[j], u[j], dot);
                     }
                 }
-                dot = team_sum(dot, p.team) / (float)p.d;
+                dot = team_sum(dot, p.team) * p.inv_d;
                 if (weighed) {
 #pragma unroll
-                    for (int j = 0; j < 2 * E; ++j) g[j] = fmaf(-u[j], dot, g[j]) * f.root * f.up;
+                    for (int j = 0; j < 2 * E; ++j) g[j] = fmaf(-u[j], dot, g[j]) * f.root;
+                    if (f.up != 1.f) {
+#pragma unroll
+                        for (int j = 0; j < 2 * E; ++j) g[j] *= f.up;
+                    }
                 }
             }
-            if (now.on) {
-                const Place &to = now.query ? p.q_out : p.k_out;
-                T *at = (T *)to.p + now.m * to.token + now.h * to.head;
-                Vec<T> a, b;
+            if (now.side != NONE) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    a[j] = rounded<T>(g[j]);
-                    b[j] = rounded<T>(g[E + j]);
+                    now.a[j] = rounded<T>(g[j]);
+                    now.b[j] = rounded<T>(g[E + j]);
                 }
-                put(at + ck.oa, ck.na, a);
-                put(at + ck.ob, ck.nb, b);
+                put<FULL>(now.to + ck.oa, ck.na, now.a);
+                put<FULL>(now.to + ck.ob, ck.nb, now.b);
             }
         }
     }
@@ -479,7 +497,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
         float *s_sum = (float *)s_turns;
         __syncthreads();  // the turns have been read
         const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
-        if (threadIdx.x % 64 < p.team) {
+        if (threadIdx.x % 64 < p.team && ck.on) {
             float *q = s_sum + wave * 2 * p.d, *k = q + p.d;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
@@ -544,6 +562,7 @@ pk::HeadGroup lay_out(HeadsArgs &a, int rows, int size)
     const pk::HeadGroup g = pk::head_group(rows, t.team, a.pairs);
     a.rows = rows;
     a.pair_chunks = t.pair_chunks;
+    a.chunks = t.chunks;
     a.team = t.team;
     a.team_shift = log2_of(t.team);
     a.teams = g.teams;
@@ -552,41 +571,45 @@ pk::HeadGroup lay_out(HeadsArgs &a, int rows, int size)
     return g;
 }
 
-template <typename T, typename W, bool NORM, int PAIRS>
+template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
 int launch_heads(HeadsArgs a, int rows, hipStream_t s)
 {
     const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
     const size_t lds = (size_t)a.tokens * a.pairs * sizeof(float2);
-    for (int64_t left = (a.M + a.tokens - 1) / a.tokens; left > 0; left -= kMostGroups) {
+    for (int64_t left = ((int64_t)a.M + a.tokens - 1) / a.tokens; left > 0; left -= kMostGroups) {
         const int64_t now = left < kMostGroups ? left : kMostGroups;
-        hipLaunchKernelGGL((heads_kernel<T, W, NORM, PAIRS>), dim3((unsigned)now), dim3(g.threads), lds, s, a);
+        hipLaunchKernelGGL((heads_kernel<T, W, NORM, PAIRS, FULL>), dim3((unsigned)now), dim3(g.threads), lds, s, a);
         if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
-        a.first += now * a.tokens;
+        a.first += (unsigned)(now * a.tokens);
     }
     return PK_OK;
 }
 
-template <typename T, typename W, bool NORM, int PAIRS>
+template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
 int launch_grad(HeadsArgs a, int rows, int64_t *groups, hipStream_t s)
 {
     const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
     // what the card holds at once, by the registers (four waves a SIMD)
     const int resident = (NORM ? 12 : 20) / (g.threads / 64) > 0 ? (NORM ? 12 : 20) / (g.threads / 64) : 1;
-    *groups = (a.M + a.tokens - 1) / a.tokens;
+    *groups = ((int64_t)a.M + a.tokens - 1) / a.tokens;
     if (*groups > 256 * resident) *groups = 256 * resident;
     if (*groups > kGradGroups) *groups = kGradGroups;
     size_t lds = (size_t)2 * a.tokens * a.pairs * sizeof(float2);
     const size_t sums = NORM ? (size_t)(g.threads / 64) * 2 * a.d * sizeof(float) : 0;
     if (lds < sums) lds = sums;
-    hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
+    hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS, FULL>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 
-// The instance for a call's types, weights and pairs.
-#define PK_HEADS(FN, T, W, NORM, ...)                                  \
-    (!a.pairs         ? FN<T, W, NORM, UNTURNED>(__VA_ARGS__)          \
-     : a.interleaved  ? FN<T, W, NORM, NEIGHBOURS>(__VA_ARGS__)        \
-                      : FN<T, W, NORM, HALVES>(__VA_ARGS__))
+// The instance for a call's types, weights and pairs; FULL: every lane's vectors are whole.
+#define PK_HEADS_FULL(FN, T, W, NORM, PAIRS, ...)                                                            \
+    (a.pairs % (16 / (int)sizeof(T)) == 0 && (a.d - 2 * a.pairs) % (32 / (int)sizeof(T)) == 0                 \
+         ? FN<T, W, NORM, PAIRS, true>(__VA_ARGS__)                                                          \
+         : FN<T, W, NORM, PAIRS, false>(__VA_ARGS__))
+#define PK_HEADS(FN, T, W, NORM, ...)                                                  \
+    (!a.pairs         ? PK_HEADS_FULL(FN, T, W, NORM, UNTURNED, __VA_ARGS__)          \
+     : a.interleaved  ? PK_HEADS_FULL(FN, T, W, NORM, NEIGHBOURS, __VA_ARGS__)        \
+                      : PK_HEADS_FULL(FN, T, W, NORM, HALVES, __VA_ARGS__))
 #define PK_HEADS_TYPES(FN, ...)                                                                                       \
     (!a.q_weight && !a.k_weight ? (dtype == PK_F32    ? PK_HEADS(FN, float, float, false, __VA_ARGS__)                 \
                                    : dtype == PK_BF16 ? PK_HEADS(FN, bf16, bf16, false, __VA_ARGS__)                   \
@@ -647,7 +670,7 @@ void set_rotation(HeadsArgs &a, const pk_rotation *rot)
 Place place(const pk_heads *t)
 {
     if (!t) return {nullptr, 0, 0};
-    return {t->data, t->token_stride, t->head_stride};
+    return {t->data, (unsigned)t->token_stride, (unsigned)t->head_stride};
 }
 
 // Whether an output shares memory with the rotation's arrays or a weight.
@@ -706,11 +729,12 @@ int pk_rope_qk(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk_head
     a.k_out = place(k_out);
     a.q_weight = q_weight;
     a.k_weight = k_weight;
-    a.M = M;
+    a.M = (unsigned)M;
     a.Hq = (int)Hq;
     a.Hk = (int)Hk;
     a.d = (int)d;
     a.eps = eps;
+    a.inv_d = 1.f / (float)d;
     set_rotation(a, rotation);
     st = run_heads(dtype, weight_dtype, a, (int)(Hq + Hk), (hipStream_t)stream);
     if (st == PK_OK) api_ran("rope_qk");
@@ -802,11 +826,12 @@ int pk_rope_qk_backward(int dtype, int64_t M, int64_t d, const pk_heads *dq, con
     a.q_weight = q_weight;
     a.k_weight = k_weight;
     a.partial = (float *)workspace;
-    a.M = M;
+    a.M = (unsigned)M;
     a.Hq = (int)Hq;
     a.Hk = (int)Hk;
     a.d = (int)d;
     a.eps = eps;
+    a.inv_d = 1.f / (float)d;
     set_rotation(a, rotation);
     st = run_grad(dtype, weight_dtype, a, (int)(Hq + Hk), q_weight_grad, k_weight_grad, (hipStream_t)stream);
     if (st == PK_OK) api_ran("rope_qk_backward");
@@ -860,20 +885,19 @@ int pk_cache_append(int dtype, int64_t M, int64_t d, const pk_heads *q, const pk
     a.k = place(k);
     a.v = place(v);
     a.q_out = place(q_out);
-    a.k_out = {cache->key, cache->key_stride[1], cache->key_stride[2]};
-    a.v_out = {cache->value, cache->value_stride[1], cache->value_stride[2]};
+    a.key = {cache->key, cache->key_stride[0], cache->key_stride[1], cache->key_stride[2]};
+    a.value = {cache->value, cache->value_stride[0], cache->value_stride[1], cache->value_stride[2]};
     a.slots = slots;
     a.pages = cache->pages;
     a.page_size = (int)cache->page_size;
-    a.key_page = cache->key_stride[0];
-    a.value_page = cache->value_stride[0];
     a.q_weight = q_weight;
     a.k_weight = k_weight;
-    a.M = M;
+    a.M = (unsigned)M;
     a.Hq = (int)Hq;
     a.Hk = (int)Hk;
     a.d = (int)d;
     a.eps = eps;
+    a.inv_d = 1.f / (float)d;
     set_rotation(a, rotation);
     st = run_heads(dtype, weight_dtype, a, (int)(Hq + 2 * Hk), (hipStream_t)stream);
     if (st == PK_OK) api_ran("cache_append");

@@ -18,9 +18,6 @@ constexpr HeadTiling head_tiling(int d, int pairs, int E)
 {
     HeadTiling t = {(pairs + E - 1) / E, 0, 1};
     t.chunks = t.pair_chunks + (d - 2 * pairs + 2 * E - 1) / (2 * E);
-    // a value's head has no pairs: it may need one lane more than this, never two
-    const int plain = (d + 2 * E - 1) / (2 * E);
-    if (plain > t.chunks) t.chunks = plain;
     while (t.team < t.chunks) t.team *= 2;
     return t;
 }
