@@ -364,8 +364,10 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
 // in registers over all its tokens; its rows are added up by weights_kernel in the
 // order of the work-groups.  The next token's rows are on their way while one is
 // worked on.
-template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
-__global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(HeadsArgs p)
+// ONE: a team has the same head of every token, so that its lanes have one side's
+// weights and sums.
+template <typename T, typename W, bool NORM, int PAIRS, bool FULL, bool ONE>
+__global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_kernel(HeadsArgs p)
 {
     constexpr int E = 16 / (int)sizeof(T);
     typedef typename Pack<W, E>::V VW;
@@ -374,9 +376,15 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
     const Slot slot(p);
     const Chunk<E, FULL> ck(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, p.chunks, PAIRS == HALVES);
     constexpr int SUMS = NORM ? 2 * E : 1;
-    float sum_q[SUMS], sum_k[SUMS];
+    float sum_q[SUMS], sum_k[SUMS];  // ONE: sum_q is that side's
 #pragma unroll
     for (int j = 0; j < SUMS; ++j) sum_q[j] = sum_k[j] = 0.f;
+    const W *const weight_one = NORM ? (const W *)(slot.r < p.Hq ? p.q_weight : p.k_weight) : nullptr;
+    VW wa = (VW)(W)0.f, wb = wa;
+    if (NORM && ONE && weight_one && ck.on) {
+        wa = get<FULL, W, E>(weight_one + ck.oa, ck.na);
+        wb = get<FULL, W, E>(weight_one + ck.ob, ck.nb);
+    }
 
     struct Row {
         Vec<T> a, b, xa, xb;  // the gradient, the input
@@ -419,9 +427,9 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
             __syncthreads();
         }
         int r = slot.r;
-        for (int i = 0; i < p.rounds; ++i) {
+        for (int i = 0; i < (ONE ? 1 : p.rounds); ++i) {
             Row now = x;
-            x = i + 1 < p.rounds ? fetch(first, r + p.teams) : fetch(first + step, slot.r);
+            x = !ONE && i + 1 < p.rounds ? fetch(first, r + p.teams) : fetch(first + step, slot.r);
             r += p.teams;
             float g[2 * E];
 #pragma unroll
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
                 }
             }
             if constexpr (NORM) {
-                const W *weight = (const W *)(now.side == QUERY ? p.q_weight : p.k_weight);
+                const W *weight = ONE ? weight_one : (const W *)(now.side == QUERY ? p.q_weight : p.k_weight);
                 float u[2 * E], dot = 0.f;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
@@ -448,10 +456,13 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
                 // rows that are not there, and sides without a weight, add nothing
                 const bool weighed = now.side != NONE && weight;
                 if (weighed) {
-                    const VW wa = get<FULL, W, E>(weight + ck.oa, ck.na), wb = get<FULL, W, E>(weight + ck.ob, ck.nb);
+                    if constexpr (!ONE) {
+                        wa = get<FULL, W, E>(weight + ck.oa, ck.na);
+                        wb = get<FULL, W, E>(weight + ck.ob, ck.nb);
+                    }
 #pragma unroll
                     for (int j = 0; j < 2 * E; ++j) u[j] *= f.root;
-                    if (now.side == QUERY) {
+                    if (ONE || now.side == QUERY) {
 #pragma unroll
                         for (int j = 0; j < 2 * E; ++j) sum_q[j] = fmaf(g[j], u[j], sum_q[j]);
                     } else {
@@ -486,6 +497,14 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, 3) heads_grad_kernel(Hea
         }
     }
     if constexpr (NORM) {
+        if (ONE) {
+            const bool query = slot.r < p.Hq;
+#pragma unroll
+            for (int j = 0; j < 2 * E; ++j) {
+                sum_k[j] = query ? 0.f : sum_q[j];
+                sum_q[j] = query ? sum_q[j] : 0.f;
+            }
+        }
         // over the teams of a wave, then over the waves
         for (int o = p.team; o < 64; o *= 2) {
 #pragma unroll
@@ -589,15 +608,22 @@ template <typename T, typename W, bool NORM, int PAIRS, bool FULL>
 int launch_grad(HeadsArgs a, int rows, int64_t *groups, hipStream_t s)
 {
     const pk::HeadGroup g = lay_out(a, rows, (int)sizeof(T));
-    // what the card holds at once, by the registers (four waves a SIMD)
-    const int resident = (NORM ? 12 : 20) / (g.threads / 64) > 0 ? (NORM ? 12 : 20) / (g.threads / 64) : 1;
+    // what the card holds at once, by the registers, and as many tokens to each
+    const bool one = a.rounds == 1;
+    const int waves = g.threads / 64, resident = (one ? 16 : 12) / waves > 0 ? (one ? 16 : 12) / waves : 1;
     *groups = ((int64_t)a.M + a.tokens - 1) / a.tokens;
-    if (*groups > 256 * resident) *groups = 256 * resident;
+    if (*groups > 256 * resident) {
+        const int64_t turns = (*groups + 256 * resident - 1) / (256 * resident);
+        *groups = (*groups + turns - 1) / turns;
+    }
     if (*groups > kGradGroups) *groups = kGradGroups;
     size_t lds = (size_t)2 * a.tokens * a.pairs * sizeof(float2);
     const size_t sums = NORM ? (size_t)(g.threads / 64) * 2 * a.d * sizeof(float) : 0;
     if (lds < sums) lds = sums;
-    hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS, FULL>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
+    if (one)
+        hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS, FULL, true>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
+    else
+        hipLaunchKernelGGL((heads_grad_kernel<T, W, NORM, PAIRS, FULL, false>), dim3((unsigned)*groups), dim3(g.threads), lds, s, a);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 
