@@ -162,7 +162,8 @@ struct Line {
         s.ends[t] = end;
         __syncthreads();
     }
-    // sequence b's indices
+    // sequence b's indices (of a share's first; those after it are read when it gets there: held
+    // in lanes they would take registers from the whole of it)
     __device__ __forceinline__ Sequence get(int b) const
     {
         if (!few) return sequence_of(p, b);
@@ -347,29 +348,24 @@ struct Mover {
     typedef Lds<T, D> L;
     typedef typename Pack<T>::V V;
     static constexpr int kCopies = ROWS / L::kRows;
-    static constexpr int kTurns = L::kRows >= 16 ? 1 : 16 / L::kRows < kCopies ? 16 / L::kRows : kCopies;  // until turn() repeats
     static_assert(kCopies * L::kRows == ROWS, "whole copies");
     const Args &p;
     const char *key, *value;  // the head's
     const int32_t *table;
     int first, chunks;
-    unsigned key_off[COPIED ? kTurns : 1], value_off[COPIED ? kTurns : 1];
-    unsigned copies;  // bit t: this lane has a chunk in copies of turn t
+    // COPIED: a lane's row in a copy, in bytes of K and of V, and its chunk in copies that turn nothing
+    unsigned key_row, value_row, chunk;
     V in_k[COPIED ? 1 : kCopies], in_v[COPIED ? 1 : kCopies];
 
-    __device__ __forceinline__ Mover(const Args &args, int first_row) : p(args), first(first_row), copies(0)
+    __device__ __forceinline__ Mover(const Args &args, int first_row) : p(args), first(first_row)
     {
-        const int lane = threadIdx.x % 64;
+        const int lane = threadIdx.x % 64, r = lane / L::kChunks;
         chunks = (p.d + L::kElements - 1) / L::kElements;
-        if constexpr (COPIED) {
-#pragma unroll
-            for (int t = 0; t < kTurns; ++t) {
-                const int r = lane / L::kChunks, c = lane % L::kChunks ^ L::turn(first + t * L::kRows + r);
-                key_off[t] = (unsigned)(r * (int)p.key_place * (int)sizeof(T) + c * 16);
-                value_off[t] = (unsigned)(r * (int)p.value_place * (int)sizeof(T) + c * 16);
-                copies |= (c < chunks ? 1u : 0u) << t;
-            }
-        }
+        key_row = (unsigned)(r * (int)p.key_place * (int)sizeof(T));
+        value_row = (unsigned)(r * (int)p.value_place * (int)sizeof(T));
+        // turn(first + i kRows + r) = turn(first + r) ^ turn(i kRows): rows of a copy, of copies and
+        // of the tile are different bits of what turn() takes
+        chunk = lane % L::kChunks ^ L::turn(first + r);
     }
     __device__ __forceinline__ void head(int b, int h)
     {
@@ -397,19 +393,24 @@ struct Mover {
                 const unsigned lo = __builtin_amdgcn_readlane((int)off, r), hi = __builtin_amdgcn_readlane((int)(off >> 32), r);
                 return start + (int64_t)((uint64_t)hi << 32 | lo);
             };
+            // (made here each time: a register for each copy's would be held through the loop)
+            unsigned chunk_here = chunk;
+            asm volatile("" : "+v"(chunk_here));
             // all of K, then all of V; rows without a page, and chunks beyond the head's, are left out
             auto copy = [&]<bool ALL>(unsigned there) {
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
                     if (ALL || there >> (i * L::kRows) & 1) {
                         const char *start = from(key, k, i * L::kRows);
-                        if (ALL || copies >> (i % kTurns) & 1) copy16(s_k + (first + i * L::kRows) * L::kRow, start, key_off[i % kTurns]);
+                        const unsigned c = chunk_here ^ L::turn(i * L::kRows);
+                        if (ALL || c < (unsigned)chunks) copy16(s_k + (first + i * L::kRows) * L::kRow, start, key_row + c * 16);
                     }
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i)
                     if (ALL || there >> (i * L::kRows) & 1) {
                         const char *start = from(value, v, i * L::kRows);
-                        if (ALL || copies >> (i % kTurns) & 1) copy16(s_v + (first + i * L::kRows) * L::kRow, start, value_off[i % kTurns]);
+                        const unsigned c = chunk_here ^ L::turn(i * L::kRows);
+                        if (ALL || c < (unsigned)chunks) copy16(s_v + (first + i * L::kRows) * L::kRow, start, value_row + c * 16);
                     }
             };
             if (p.d == D && __all(page >= 0))
@@ -485,6 +486,8 @@ __device__ __forceinline__ void own_lds()
 }
 
 // ------------------------------------------------------------------ the attention
+
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
 // The larger of v in lanes 16 and 32 apart, in all of them.
 __device__ __forceinline__ float across(float v)
@@ -587,10 +590,8 @@ struct Rows {
         // the first columns of V on their way while the weights are made
         constexpr int G = N < kGroup ? N : kGroup;
         V8 v[G];
-        if (!odd) {
 #pragma unroll
-            for (int i = 0; i < G; ++i) v[i] = L::column(s_v, i, lane);
-        }
+        for (int i = 0; i < G; ++i) v[i] = L::column(s_v, i, lane);
         __builtin_amdgcn_sched_barrier(0);
 
         const bool drafted = at + kTile > length;
@@ -656,22 +657,27 @@ struct Rows {
                 weight[n][e] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
             }
         }
-        if (!odd) {
 #pragma unroll
-            for (int from = 0; from < N; from += G) {
-                if (from) {
+        for (int from = 0; from < N; from += G) {
+            if (from) {
 #pragma unroll
-                    for (int i = 0; i < G; ++i) v[i] = L::column(s_v, from + i, lane);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int i = 0; i < G; ++i) v[i] = L::column(s_v, from + i, lane);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (odd) {
 #pragma unroll
                 for (int i = 0; i < G; ++i)
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n], o[n][from + i]);
+                    for (int j = 0; j < 8; ++j) v[i][j] = finite((float)v[i][j]) ? v[i][j] : (T)0.f;
             }
-            return;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n], o[n][from + i]);
         }
-        // a NaN or an infinity reaches the rows that see it and no other: position by position
+        if (!odd) return;
+        // a NaN or an infinity reaches the rows that see it and no other: the products were made
+        // with zeros in their places, and here what they add is added position by position
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             own_lds();
@@ -687,8 +693,8 @@ struct Rows {
                     const int here = lane_here() / 16 * 4;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const float v = L::at(s_v, j, i * 16 + here + c);
-                        o[n][i][c] += sees ? w * v : 0.f;
+                        const float one = L::at(s_v, j, i * 16 + here + c);
+                        if (sees && !finite(one)) o[n][i][c] += w * one;
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -710,12 +716,11 @@ struct Walk {
     bool whole;
 
     // from unit u on
-    template <int THREADS>
-    __device__ __forceinline__ void at(const Args &p, const Line<THREADS> &line, unsigned u)
+    __device__ __forceinline__ void at(const Args &p, unsigned u)
     {
         while (u >= base + seq.cost(p.shape.heads)) {
             base += seq.cost(p.shape.heads);
-            seq = line.get(++b);
+            seq = sequence_of(p, ++b);
         }
         const unsigned item = (u - base) / (unsigned)seq.units;
         item_begin = base + item * seq.units;
@@ -762,7 +767,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     Rows<T, D, NQ> rows;
 
     for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
-        walk.at(p, line, u);
+        walk.at(p, u);
         mover.head(walk.b, walk.head);
         const int end = walk.end, length = walk.seq.length;
         // the first turn only brings the first tile: what brings a tile is here once
@@ -840,7 +845,8 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     constexpr int N = D / 16, ROWS = 64 * NQ, TILE = wide_tile<T, D>(), OWN = TILE / 4, kHalf = TILE * L::kRow;
     __shared__ __align__(16) char s_raw[4 * kHalf];
     __shared__ typename Line<256>::Shared s_line;
-    __shared__ float s_scratch[4][kTile * 16];
+    static_assert(ROWS * D * 4 <= 4 * kHalf, "the sums fit the stages");
+    __shared__ float s_scratch[4][kTile * 16], s_m[ROWS], s_l[ROWS];
     __shared__ int s_odd[2][4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     PK_WALK(256);
@@ -848,7 +854,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     Rows<T, D, NQ> rows;
 
     for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
-        walk.at(p, line, u);
+        walk.at(p, u);
         mover.head(walk.b, walk.head);
         const int end = walk.end, length = walk.seq.length, row0 = wave * 16 * NQ;
         int at = walk.begin - TILE, stage = 0;
@@ -886,28 +892,39 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
             }
         }
 
-        float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
+        // each wave's sums through LDS, where the tiles were, so that what stores them is here once
+        __syncthreads();  // the last tile has been read
+        if (mine) {
+            f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw) + row0 * (D / 4);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const int r = row0 + n * 16 + col;
-            float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
-            l += __shfl_xor(l, 32);
-            const float m = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
-            if (r >= walk.rows) continue;
-            if (walk.whole) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (i * 16 + g * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, i * 16 + g * 4, rows.o[n][i], l, m);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(part + r * D + i * 16 + g * 4) = rows.o[n][i];
+            for (int n = 0; n < NQ; ++n) {
+                float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
+                l += __shfl_xor(l, 32);
                 if (g == 0) {
-                    part[ROWS * D + r] = m;
-                    part[ROWS * (D + 1) + r] = l;
+                    s_m[row0 + n * 16 + col] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+                    s_l[row0 + n * 16 + col] = l;
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) s_o[(n * 16 + col) * (D / 4) + ((i * 4 + g) ^ col)] = rows.o[n][i];
+            }
+            own_lds();
+            float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
+            const int count = walk.rows - row0 < 16 * NQ ? walk.rows - row0 : 16 * NQ;
+            for (int i = lane; i < count * (D / 4); i += 64) {
+                const int r = i / (D / 4), c = i % (D / 4);
+                const f32x4 o = s_o[r * (D / 4) + (c ^ (r & 15))];
+                if (walk.whole) {
+                    if (c * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + row0 + r, c * 4, o, s_l[row0 + r], s_m[row0 + r]);
+                } else {
+                    *reinterpret_cast<f32x4 *>(part + (row0 + r) * D + c * 4) = o;
+                    if (c == 0) {
+                        part[ROWS * D + row0 + r] = s_m[row0 + r];
+                        part[ROWS * (D + 1) + row0 + r] = s_l[row0 + r];
+                    }
                 }
             }
         }
-        __syncthreads();  // the last tile has been read
+        __syncthreads();  // and the sums
     }
 }
 
