@@ -260,11 +260,11 @@ __device__ __forceinline__ float weight_of(float m, float most)
 // The lane's number as the compiler cannot know it ahead: addresses made of it are made
 // where they are used.  Left alone, they are made once before all loops and held in
 // registers that the sums need.
-__device__ __forceinline__ int lane_here()
+__device__ __forceinline__ unsigned lane_here()
 {
-    int lane = threadIdx.x % 64;
+    unsigned lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));
-    return lane;
+    return lane & 63;
 }
 
 // Rows of K or V in LDS as copies leave them: 1 KiB an instruction, 16 bytes a lane, so
@@ -277,48 +277,79 @@ struct Lds {
     static constexpr int kRow = kChunks * 16;
     static constexpr int kRows = 64 / kChunks;  // of a copy
 
-    static __device__ __forceinline__ int turn(int r) { return kChunks >= 16 ? r & 15 : r >> 1 & 7; }
+    static __device__ __forceinline__ unsigned turn(unsigned r) { return kChunks >= 16 ? r & 15 : r >> 1 & 7; }
 
-    // channels 8 i on of row r, for the product's operand; chunks from `chunks` on are zero
-    template <bool PART>
-    static __device__ __forceinline__ typename Eight<T>::V row(const char *s, int r, int i, int chunks)
+    typedef __attribute__((address_space(3))) const char *At;
+    static __device__ __forceinline__ unsigned address(const char *s) { return (unsigned)(uintptr_t)(At)s; }
+    template <typename X>
+    static __device__ __forceinline__ X load(unsigned at)
     {
-        typedef typename Eight<T>::V V;
-        if constexpr (sizeof(T) == 2) {
-            const V v = *reinterpret_cast<const V *>(s + r * kRow + (i ^ turn(r)) * 16);
-            return PART && i >= chunks ? (V)(T)0.f : v;
-        } else {
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(s + r * kRow + (2 * i ^ turn(r)) * 16);
-            const f32x4 hi = *reinterpret_cast<const f32x4 *>(s + r * kRow + ((2 * i + 1) ^ turn(r)) * 16);
-            return __builtin_shufflevector(PART && 2 * i >= chunks ? (f32x4)0.f : lo, PART && 2 * i + 1 >= chunks ? (f32x4)0.f : hi,
-                                           0, 1, 2, 3, 4, 5, 6, 7);
-        }
+        return *(__attribute__((address_space(3))) const X *)(uintptr_t)at;
     }
 
-    // channel 16 n + lane % 16 of rows 4 (lane / 16) + 0..3 and those + 16
-    static __device__ __forceinline__ typename Eight<T>::V column(const char *s, int n, int lane)
-    {
-        typename Eight<T>::V v;
-        if constexpr (sizeof(T) == 2) {
-            typedef short S4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) S4 *P;
-            const int r = lane / 4;
-            const char *p = s + r * kRow + ((2 * n + lane / 2 % 2) ^ turn(r)) * 16 + lane % 2 * 8;
-            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
-            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * kRow));
-            const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            v = __builtin_bit_cast(typename Eight<T>::V, both);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = lane / 16 * 4 + j;
-                const char *p = s + r * kRow + ((4 * n + lane / 4 % 4) ^ turn(r)) * 16 + lane % 4 * 4;
-                v[j] = *reinterpret_cast<const float *>(p);
-                v[4 + j] = *reinterpret_cast<const float *>(p + 16 * kRow);
+    // Operands for the product: channels 8 (4 c + lane / 16) on of rows lane % 16 and those + 16
+    // of a tile at s.  A tile lies at a multiple of 1 KiB, so that another column's chunk is
+    // another value of the address's bits within a row: one xor, one read.
+    struct RowReader {
+        unsigned base, g;
+        __device__ __forceinline__ RowReader(const char *s, unsigned lane) : g(lane / 16)
+        {
+            const unsigned col = lane % 16;
+            base = address(s) + col * kRow + (((sizeof(T) == 2 ? g : 2 * g) ^ turn(col)) << 4);
+        }
+        // chunks from `chunks` on are zero
+        template <bool PART>
+        __device__ __forceinline__ typename Eight<T>::V get(int h, int c, int chunks) const
+        {
+            typedef typename Eight<T>::V V;
+            const unsigned i = 4 * c + g;
+            if constexpr (sizeof(T) == 2) {
+                const V v = load<V>((base ^ c << 6) + h * 16 * kRow);
+                return PART && i >= (unsigned)chunks ? (V)(T)0.f : v;
+            } else {
+                const f32x4 lo = load<f32x4>((base ^ c << 7) + h * 16 * kRow), hi = load<f32x4>((base ^ c << 7 ^ 16) + h * 16 * kRow);
+                return __builtin_shufflevector(PART && 2 * i >= (unsigned)chunks ? (f32x4)0.f : lo,
+                                               PART && 2 * i + 1 >= (unsigned)chunks ? (f32x4)0.f : hi, 0, 1, 2, 3, 4, 5, 6, 7);
             }
         }
-        return v;
-    }
+    };
+
+    // channel 16 n + lane % 16 of rows 4 (lane / 16) + 0..3 and those + 16
+    struct ColumnReader {
+        unsigned base;
+        __device__ __forceinline__ ColumnReader(const char *s, unsigned lane)
+        {
+            if constexpr (sizeof(T) == 2) {
+                const unsigned r = lane / 4;
+                base = address(s) + r * kRow + ((lane / 2 % 2 ^ turn(r)) << 4) + lane % 2 * 8;
+            } else {
+                const unsigned r = lane / 16 * 4;
+                base = address(s) + r * kRow + ((lane / 4 % 4 ^ turn(r)) << 4) + lane % 4 * 4;
+            }
+        }
+        __device__ __forceinline__ typename Eight<T>::V get(int n) const
+        {
+            typename Eight<T>::V v;
+            if constexpr (sizeof(T) == 2) {
+                typedef short S4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) S4 *P;
+                const unsigned at = base ^ n << 5;
+                const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at);
+                const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at + 16 * kRow));
+                const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                v = __builtin_bit_cast(typename Eight<T>::V, both);
+            } else {
+                static_assert(kChunks >= 16, "turn(r + j) = turn(r) ^ j");
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned at = (base ^ n << 6 ^ j << 4) + j * kRow;
+                    v[j] = load<float>(at);
+                    v[4 + j] = load<float>(at + 16 * kRow);
+                }
+            }
+            return v;
+        }
+    };
 
     static __device__ __forceinline__ float at(const char *s, int r, int channel)
     {
@@ -386,8 +417,15 @@ struct Mover {
     {
         const int lane = threadIdx.x % 64, j = at + first + lane % ROWS;
         const int place = p.page_shift >= 0 ? j & (p.page_size - 1) : (int)((unsigned)j % (unsigned)p.page_size);
-        const int64_t k = (page * p.key_page + place * p.key_place) * (int)sizeof(T);
-        const int64_t v = (page * p.value_page + place * p.value_place) * (int)sizeof(T);
+        // (COPIED: strides in bytes have 32 bits, and so has the offset of a position in its page)
+        const auto offset = [&](int64_t of_page, int64_t of_place) {
+            if constexpr (COPIED)
+                return (int64_t)((uint64_t)(unsigned)page * ((unsigned)of_page * (unsigned)sizeof(T)) +
+                                 (unsigned)place * ((unsigned)of_place * (unsigned)sizeof(T)));
+            else
+                return (page * of_page + place * of_place) * (int)sizeof(T);
+        };
+        const int64_t k = offset(p.key_page, p.key_place), v = offset(p.value_page, p.value_place);
         if constexpr (COPIED) {
             auto from = [&](const char *start, int64_t off, int r) {
                 const unsigned lo = __builtin_amdgcn_readlane((int)off, r), hi = __builtin_amdgcn_readlane((int)(off >> 32), r);
@@ -450,7 +488,7 @@ struct Mover {
             if ((there & all) != all) {
                 f32x4 *to = reinterpret_cast<f32x4 *>(s_v + first * L::kRow);
 #pragma unroll 1
-                for (int i = lane_here(); i < ROWS * L::kChunks; i += 64)
+                for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64)
                     if (!(there >> (i / L::kChunks) & 1)) to[i] = (f32x4)0.f;
             }
         } else {
@@ -467,11 +505,11 @@ struct Mover {
     {
         bool odd = false;
 #pragma unroll 1
-        for (int i = lane_here(); i < ROWS * L::kChunks; i += 64) {
-            const int r = first + i / L::kChunks, c = i % L::kChunks ^ L::turn(r);
+        for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64) {
+            const unsigned r = first + i / L::kChunks, c = i % L::kChunks ^ L::turn(r);
             const V v = *reinterpret_cast<const V *>(s_v + r * L::kRow + i % L::kChunks * 16);
 #pragma unroll
-            for (int j = 0; j < L::kElements; ++j) odd |= c < chunks && !(fabsf((float)v[j]) < __builtin_inff());
+            for (int j = 0; j < L::kElements; ++j) odd |= c < (unsigned)chunks && !(fabsf((float)v[j]) < __builtin_inff());
         }
         return __any(odd);
     }
@@ -492,8 +530,14 @@ __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_in
 // The larger of v in lanes 16 and 32 apart, in all of them.
 __device__ __forceinline__ float across(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    // a swap of the odd rows of sixteen of the one with the even ones of the other, both v, leaves
+    // each row beside its neighbour; then the same of halves
+    const unsigned u = __float_as_uint(v);
+    const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = fmaxf(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    const unsigned w = __float_as_uint(v);
+    const auto halves = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
 }
 
 // 16 NQ rows of an item, a wave's: lane l has row l % 16 of each sixteen.
@@ -559,11 +603,12 @@ struct Rows {
     __device__ __forceinline__ void step(const Args &p, const char *s_k, const char *s_v, int at, int length, unsigned there,
                                          bool odd, int chunks, float *scratch)
     {
-        const int lane = lane_here(), col = lane % 16, g = lane / 16;
+        const unsigned lane = lane_here(), col = lane % 16, g = lane / 16;
         f32x4 x[NQ][2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = (f32x4)0.f;
         // (reads in groups before their products: one by one each product would wait for its own)
+        const typename L::RowReader row(s_k, lane);
         auto scores = [&]<bool PART>() {
             constexpr int G = C < kGroup / 2 ? C : kGroup / 2;
 #pragma unroll
@@ -572,7 +617,7 @@ struct Rows {
 #pragma unroll
                 for (int c = 0; c < G; ++c)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) k[c][h] = L::template row<PART>(s_k, h * 16 + col, (from + c) * 4 + g, chunks);
+                    for (int h = 0; h < 2; ++h) k[c][h] = row.template get<PART>(h, from + c, chunks);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int c = 0; c < G; ++c)
@@ -590,8 +635,9 @@ struct Rows {
         // the first columns of V on their way while the weights are made
         constexpr int G = N < kGroup ? N : kGroup;
         V8 v[G];
+        const typename L::ColumnReader column(s_v, lane);
 #pragma unroll
-        for (int i = 0; i < G; ++i) v[i] = L::column(s_v, i, lane);
+        for (int i = 0; i < G; ++i) v[i] = column.get(i);
         __builtin_amdgcn_sched_barrier(0);
 
         const bool drafted = at + kTile > length;
@@ -661,7 +707,7 @@ struct Rows {
         for (int from = 0; from < N; from += G) {
             if (from) {
 #pragma unroll
-                for (int i = 0; i < G; ++i) v[i] = L::column(s_v, from + i, lane);
+                for (int i = 0; i < G; ++i) v[i] = column.get(from + i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (odd) {
@@ -690,7 +736,7 @@ struct Rows {
                 const bool sees = seen[n] >> j & 1;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int here = lane_here() / 16 * 4;
+                    const unsigned here = lane_here() / 16 * 4;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const float one = L::at(s_v, j, i * 16 + here + c);
@@ -756,8 +802,9 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     typedef Lds<T, D> L;
     constexpr int N = D / 16, ROWS = 16 * NQ, THREADS = WAVES * 64, STEP = WAVES * kTile;
     constexpr int kHalf = kTile * L::kRow, kStages = COPIED ? 2 : 1, kWave = kStages * 2 * kHalf;
-    constexpr int kSum = ROWS * (D + 4) * 4, kOwn = kWave > kSum ? kWave : kSum;
-    __shared__ __align__(16) char s_raw[WAVES * kOwn];
+    constexpr int kSum = ROWS * (D + 4) * 4, kOwn = kWave > kSum ? kWave : (kSum + 1023) / 1024 * 1024;
+    __shared__ __align__(1024) char s_raw[WAVES * kOwn];
+    static_assert(kHalf % 1024 == 0 && kOwn % 1024 == 0, "tiles lie at multiples of 1 KiB");
     __shared__ typename Line<THREADS>::Shared s_line;
     __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_scratch[WAVES][kTile * 16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
@@ -843,7 +890,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
 {
     typedef Lds<T, D> L;
     constexpr int N = D / 16, ROWS = 64 * NQ, TILE = wide_tile<T, D>(), OWN = TILE / 4, kHalf = TILE * L::kRow;
-    __shared__ __align__(16) char s_raw[4 * kHalf];
+    __shared__ __align__(1024) char s_raw[4 * kHalf];
     __shared__ typename Line<256>::Shared s_line;
     static_assert(ROWS * D * 4 <= 4 * kHalf, "the sums fit the stages");
     __shared__ float s_scratch[4][kTile * 16], s_m[ROWS], s_l[ROWS];
@@ -1077,13 +1124,15 @@ int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s
 }
 
 // Whether K and V can be copied in whole chunks: 16-byte rows at 16-byte places, the
-// rows of a copy (up to 8) in one page and within 32-bit offsets of each other.
+// rows of a copy (up to 8) in one page, pages and places at 32-bit strides.
 bool can_copy(const pk_cache &c, int64_t d, int size)
 {
     if (d * size % 16 || (uintptr_t)c.key % 16 || (uintptr_t)c.value % 16 || c.page_size % 8) return false;
     for (int i = 0; i < 3; ++i)
         if (c.key_stride[i] * size % 16 || c.value_stride[i] * size % 16) return false;
-    return c.key_stride[1] < 1 << 24 && c.value_stride[1] < 1 << 24;
+    for (const int64_t *stride : {c.key_stride, c.value_stride})
+        if (stride[0] * size >= (int64_t)1 << 32 || stride[1] * size * c.page_size >= (int64_t)1 << 31) return false;
+    return true;
 }
 
 }  // namespace
