@@ -327,13 +327,14 @@ struct Lds {
                 base = address(s) + r * kRow + ((lane / 4 % 4 ^ turn(r)) << 4) + lane % 4 * 4;
             }
         }
-        __device__ __forceinline__ typename Eight<T>::V get(int n) const
+        // (of tile h)
+        __device__ __forceinline__ typename Eight<T>::V get(int n, int h) const
         {
             typename Eight<T>::V v;
             if constexpr (sizeof(T) == 2) {
                 typedef short S4 __attribute__((ext_vector_type(4)));
                 typedef __attribute__((address_space(3))) S4 *P;
-                const unsigned at = base ^ n << 5;
+                const unsigned at = (base ^ n << 5) + h * kTile * kRow;
                 const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)at);
                 const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at + 16 * kRow));
                 const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -342,7 +343,7 @@ struct Lds {
                 static_assert(kChunks >= 16, "turn(r + j) = turn(r) ^ j");
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const unsigned at = (base ^ n << 6 ^ j << 4) + j * kRow;
+                    const unsigned at = (base ^ n << 6 ^ j << 4) + j * kRow + h * kTile * kRow;
                     v[j] = load<float>(at);
                     v[4 + j] = load<float>(at + 16 * kRow);
                 }
@@ -436,20 +437,22 @@ struct Mover {
             asm volatile("" : "+v"(chunk_here));
             // all of K, then all of V; rows without a page, and chunks beyond the head's, are left out
             auto copy = [&]<bool ALL>(unsigned there) {
+                auto side = [&](const char *head, int64_t off, unsigned row, unsigned step, char *to) {
+                    const char *start = nullptr;
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i)
-                    if (ALL || there >> (i * L::kRows) & 1) {
-                        const char *start = from(key, k, i * L::kRows);
+                    for (int i = 0; i < kCopies; ++i) {
+                        // eight rows lie in one page
+                        if (i * L::kRows % 8 == 0)
+                            start = from(head, off, i * L::kRows);
+                        else
+                            start += step;
                         const unsigned c = chunk_here ^ L::turn(i * L::kRows);
-                        if (ALL || c < (unsigned)chunks) copy16(s_k + (first + i * L::kRows) * L::kRow, start, key_row + c * 16);
+                        if (ALL || (there >> (i * L::kRows) & 1 && c < (unsigned)chunks))
+                            copy16(to + (first + i * L::kRows) * L::kRow, start, row + c * 16);
                     }
-#pragma unroll
-                for (int i = 0; i < kCopies; ++i)
-                    if (ALL || there >> (i * L::kRows) & 1) {
-                        const char *start = from(value, v, i * L::kRows);
-                        const unsigned c = chunk_here ^ L::turn(i * L::kRows);
-                        if (ALL || c < (unsigned)chunks) copy16(s_v + (first + i * L::kRows) * L::kRow, start, value_row + c * 16);
-                    }
+                };
+                side(key, k, key_row, (unsigned)p.key_place * (unsigned)(L::kRows * sizeof(T)), s_k);
+                side(value, v, value_row, (unsigned)p.value_place * (unsigned)(L::kRows * sizeof(T)), s_v);
             };
             if (p.d == D && __all(page >= 0))
                 copy.template operator()<true>(0);
@@ -598,85 +601,96 @@ struct Rows {
                 for (int j = 0; j < 8; ++j) q[n][c][j] = (T)((float)q[n][c][j] * p.sign);
     }
 
-    // One tile, at position `at`; `there`: its positions that hold something; `odd`: values
-    // among them that are no numbers, some of which a row may not see; `scratch`: 2 KiB of LDS.
-    __device__ __forceinline__ void step(const Args &p, const char *s_k, const char *s_v, int at, int length, unsigned there,
+    // H tiles of 32 positions, from position `at` on; `there`: the positions that hold something;
+    // `odd`: values among them that are no numbers, some of which a row may not see; `scratch`: 2 KiB
+    // of LDS.
+    template <int H>
+    __device__ __forceinline__ void step(const Args &p, const char *s_k, const char *s_v, int at, int length, uint64_t there,
                                          bool odd, int chunks, float *scratch)
     {
+        constexpr uint64_t ALL = H == 2 ? ~0ull : 0xffffffffull;
+        constexpr int kHalf = kTile * L::kRow;
         const unsigned lane = lane_here(), col = lane % 16, g = lane / 16;
-        f32x4 x[NQ][2];
+        // x[n][2 h + i]: positions 32 h + 16 i + 4 g + 0..3 of row 16 n + col
+        f32x4 x[NQ][2 * H];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = (f32x4)0.f;
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int h = 0; h < 2 * H; ++h) x[n][h] = (f32x4)0.f;
         // (reads in groups before their products: one by one each product would wait for its own)
         const typename L::RowReader row(s_k, lane);
         auto scores = [&]<bool PART>() {
             constexpr int G = C < kGroup / 2 ? C : kGroup / 2;
 #pragma unroll
-            for (int from = 0; from < C; from += G) {
-                V8 k[G][2];
+            for (int h = 0; h < 2 * H; h += 2)
 #pragma unroll
-                for (int c = 0; c < G; ++c)
+                for (int from = 0; from < C; from += G) {
+                    V8 k[G][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) k[c][h] = row.template get<PART>(h, from + c, chunks);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int c = 0; c < G; ++c)
 #pragma unroll
-                for (int c = 0; c < G; ++c)
+                        for (int i = 0; i < 2; ++i) k[c][i] = row.template get<PART>(h + i, from + c, chunks);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int c = 0; c < G; ++c)
 #pragma unroll
-                        for (int n = 0; n < NQ; ++n) x[n][h] = product(k[c][h], q[n][from + c], x[n][h]);
-            }
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) x[n][h + i] = product(k[c][i], q[n][from + c], x[n][h + i]);
+                }
         };
         if (p.d == D)
             scores.template operator()<false>();
         else
             scores.template operator()<true>();
-
         // the first columns of V on their way while the weights are made
         constexpr int G = N < kGroup ? N : kGroup;
         V8 v[G];
         const typename L::ColumnReader column(s_v, lane);
 #pragma unroll
-        for (int i = 0; i < G; ++i) v[i] = column.get(i);
+        for (int i = 0; i < G; ++i) v[i] = column.get(i, 0);
         __builtin_amdgcn_sched_barrier(0);
 
-        const bool drafted = at + kTile > length;
-        V8 weight[NQ];
-        unsigned seen[NQ];
+        const bool drafted = at + H * kTile > length;
+        V8 weight[NQ][H];
         float scale = p.scale;
         if (p.cap != 0.f) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < 8 * H; ++e) {
                     x[n][e / 4][e % 4] = tanh_of(x[n][e / 4][e % 4] * scale) * p.cap;
                     if (e % 2) __builtin_amdgcn_sched_barrier(0);
                 }
             scale = 1.f;
         }
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            seen[n] = there;
+        // the positions of these that row 16 n + col sees
+        auto seen = [&](int n) {
+            uint64_t s = there;
             if (drafted) {
-                const int off = length - at;  // the tile's first token
-                seen[n] &= off > 0 ? (unsigned)(word[n] << off) | ((1u << off) - 1) : -off < 64 ? (unsigned)(word[n] >> -off) : 0u;
+                const int off = length - at;  // the first token
+                s &= off > 0 ? word[n] << off | ((1ull << off) - 1) : -off < 64 ? word[n] >> -off : 0ull;
             }
-        }
-        if (drafted || there != ~0u) {
+            return s;
+        };
+        if (drafted || there != ALL) {
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+            for (int n = 0; n < NQ; ++n) {
+                const uint64_t s = seen(n) >> (g * 4);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (!(seen[n] >> (e / 4 * 16 + g * 4 + e % 4) & 1)) x[n][e / 4][e % 4] = -__builtin_inff();
+                for (int e = 0; e < 8 * H; ++e)
+                    if (!(s >> (e / 4 * 16 + e % 4) & 1)) x[n][e / 4][e % 4] = -__builtin_inff();
+            }
         }
         float most[NQ];
         bool move = false;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            most[n] = fmaxf(fmaxf(x[n][0][0], x[n][0][1]), x[n][0][2]);
-            most[n] = fmaxf(fmaxf(most[n], x[n][0][3]), x[n][1][0]);
-            most[n] = fmaxf(fmaxf(most[n], x[n][1][1]), x[n][1][2]);
-            most[n] = across(fmaxf(most[n], x[n][1][3]));
+            most[n] = x[n][0][0];
+#pragma unroll
+            for (int e = 1; e + 1 < 8 * H; e += 2)
+                most[n] = fmaxf(fmaxf(most[n], x[n][e / 4][e % 4]), x[n][(e + 1) / 4][(e + 1) % 4]);
+            most[n] = across(fmaxf(most[n], x[n][2 * H - 1][3]));
             // (both -infinity: nothing seen yet)
             move |= (most[n] - m[n]) * scale > 8.f;
         }
@@ -697,55 +711,60 @@ struct Rows {
         for (int n = 0; n < NQ; ++n) {
             const float origin = m[n] == -__builtin_inff() ? 0.f : -m[n] * scale;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8 * H; ++e) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e / 4][e % 4], scale, origin));
                 l[n] += w;
-                weight[n][e] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
+                weight[n][e / 8][e % 8] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
             }
         }
 #pragma unroll
-        for (int from = 0; from < N; from += G) {
-            if (from) {
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int i = 0; i < G; ++i) v[i] = column.get(from + i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (odd) {
+            for (int from = 0; from < N; from += G) {
+                if (h || from) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) v[i] = column.get(from + i, h);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (odd) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[i][j] = finite((float)v[i][j]) ? v[i][j] : (T)0.f;
+                }
 #pragma unroll
                 for (int i = 0; i < G; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[i][j] = finite((float)v[i][j]) ? v[i][j] : (T)0.f;
+                    for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n][h], o[n][from + i]);
             }
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n], o[n][from + i]);
-        }
         if (!odd) return;
         // a NaN or an infinity reaches the rows that see it and no other: the products were made
         // with zeros in their places, and here what they add is added position by position
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            own_lds();
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) scratch[(e / 4 * 16 + g * 4 + e % 4) * 16 + col] = (float)weight[n][e];
-            own_lds();
+            for (int h = 0; h < H; ++h) {
+                own_lds();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) scratch[(e / 4 * 16 + g * 4 + e % 4) * 16 + col] = (float)weight[n][h][e];
+                own_lds();
+                const unsigned s = (unsigned)(seen(n) >> (h * kTile));
 #pragma unroll 1
-            for (int j = 0; j < kTile; ++j) {
-                const float w = scratch[j * 16 + col];
-                const bool sees = seen[n] >> j & 1;
+                for (int j = 0; j < kTile; ++j) {
+                    const float w = scratch[j * 16 + col];
+                    const bool sees = s >> j & 1;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const unsigned here = lane_here() / 16 * 4;
+                    for (int i = 0; i < N; ++i) {
+                        const unsigned here = lane_here() / 16 * 4;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float one = L::at(s_v, j, i * 16 + here + c);
-                        if (sees && !finite(one)) o[n][i][c] += w * one;
+                        for (int c = 0; c < 4; ++c) {
+                            const float one = L::at(s_v + h * kHalf, j, i * 16 + here + c);
+                            if (sees && !finite(one)) o[n][i][c] += w * one;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-        }
     }
 };
 
@@ -833,7 +852,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             if (first) continue;
             own_lds();
             const bool odd = at + kTile > length && mover.odd(s_k + kHalf);
-            rows.step(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
+            rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
         }
 
         // the waves' sums together
@@ -910,7 +929,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
         rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + (mine ? row0 : 0), walk.row0 + walk.rows, mover.chunks);
         for (bool first = true; at < end; at += TILE, first = false) {
             char *const s_k = s_raw + stage * 2 * kHalf, *const s_v = s_k + kHalf;
-            const uint64_t there = __ballot(page >= 0);
+            const uint64_t there = __ballot(page >= 0) & (TILE == 64 ? ~0ull : 0xffffffffull);
             const bool drafted = at + TILE > length;
             if (!first) {
                 mover.end(there >> wave * OWN, s_k, s_v);
@@ -932,11 +951,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
             if (first || !mine) continue;
             bool odd = false;
             if (drafted) odd = s_odd[now][0] | s_odd[now][1] | s_odd[now][2] | s_odd[now][3];
-#pragma unroll 1
-            for (int h = 0; h < TILE; h += kTile) {
-                const unsigned here = (unsigned)(there >> h);
-                if (here) rows.step(p, s_k + h * L::kRow, s_v + h * L::kRow, at + h, length, here, odd, mover.chunks, s_scratch[wave]);
-            }
+            rows.template step<TILE / kTile>(p, s_k, s_v, at, length, there, odd, mover.chunks, s_scratch[wave]);
         }
 
         // each wave's sums through LDS, where the tiles were, so that what stores them is here once
