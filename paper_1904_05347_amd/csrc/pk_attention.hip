@@ -556,15 +556,15 @@ struct Rows {
     float l[NQ];        // sums of exponentials: of this lane's positions
     float m[NQ];        // their origin, in the products' units
 
-    // Rows from row0 on; those from `rows` on are the last one again, and are not stored.
-    // WHOLE: rows are whole chunks of 16 bytes.
+    // Sixteens of rows from row0 on, `step` rows from one to the next; those from `rows` on are
+    // the last one again, and are not stored.  WHOLE: rows are whole chunks of 16 bytes.
     template <bool WHOLE>
-    __device__ __forceinline__ void load(const Args &p, const Sequence &seq, int head, int row0, int rows, int chunks)
+    __device__ __forceinline__ void load(const Args &p, const Sequence &seq, int head, int row0, int step, int rows, int chunks)
     {
         const int lane = threadIdx.x % 64, col = lane % 16, g = lane / 16;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const int r = row0 + n * 16 + col;
+            const int r = row0 + n * step + col;
             const RowAt row = row_at(p, seq, head, r < rows ? r : rows - 1);
             const T *from = (const T *)p.q + row.m * p.q_token + row.h * p.q_head;
             word[n] = p.mask ? p.mask[row.m] : ~0ull >> (63 - (int)(row.m - seq.first));
@@ -839,7 +839,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
         // the first turn only brings the first tile: what brings a tile is here once
         int at = walk.begin + (wave - WAVES) * kTile, stage = 0;
         int page = -1, next = mover.page_at(at + STEP + lane % kTile, end);
-        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, walk.row0 + walk.rows, mover.chunks);
+        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, 16, walk.row0 + walk.rows, mover.chunks);
         for (bool first = true; at < end; at += STEP, first = false) {
             char *const s_k = s_own + stage * 2 * kHalf;
             const unsigned there = (unsigned)__ballot(page >= 0);
@@ -922,11 +922,12 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
         walk.at(p, u);
         mover.head(walk.b, walk.head);
-        const int end = walk.end, length = walk.seq.length, row0 = wave * 16 * NQ;
+        const int end = walk.end, length = walk.seq.length, row0 = wave * 16;
         int at = walk.begin - TILE, stage = 0;
         int page = -1, next = mover.page_at(at + TILE + lane % TILE, end);
-        const bool mine = row0 < walk.rows;
-        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + (mine ? row0 : 0), walk.row0 + walk.rows, mover.chunks);
+        const int sixteens = row0 >= walk.rows ? 0 : NQ == 2 && row0 + 64 < walk.rows ? 2 : 1;
+        const bool mine = sixteens > 0;
+        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + row0, 64, walk.row0 + walk.rows, mover.chunks);
         for (bool first = true; at < end; at += TILE, first = false) {
             char *const s_k = s_raw + stage * 2 * kHalf, *const s_v = s_k + kHalf;
             const uint64_t there = __ballot(page >= 0) & (TILE == 64 ? ~0ull : 0xffffffffull);
@@ -957,31 +958,32 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
         // each wave's sums through LDS, where the tiles were, so that what stores them is here once
         __syncthreads();  // the last tile has been read
         if (mine) {
-            f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw) + row0 * (D / 4);
+            f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
+                const int r = row0 + n * 64 + col;
                 float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
                 l += __shfl_xor(l, 32);
                 if (g == 0) {
-                    s_m[row0 + n * 16 + col] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
-                    s_l[row0 + n * 16 + col] = l;
+                    s_m[r] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+                    s_l[r] = l;
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) s_o[(n * 16 + col) * (D / 4) + ((i * 4 + g) ^ col)] = rows.o[n][i];
+                for (int i = 0; i < N; ++i) s_o[r * (D / 4) + ((i * 4 + g) ^ col)] = rows.o[n][i];
             }
             own_lds();
             float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
-            const int count = walk.rows - row0 < 16 * NQ ? walk.rows - row0 : 16 * NQ;
-            for (int i = lane; i < count * (D / 4); i += 64) {
-                const int r = i / (D / 4), c = i % (D / 4);
+            for (int i = lane; i < sixteens * 16 * (D / 4); i += 64) {
+                const int c = i % (D / 4), r = row0 + i / (D / 4) / 16 * 64 + i / (D / 4) % 16;
+                if (r >= walk.rows) break;
                 const f32x4 o = s_o[r * (D / 4) + (c ^ (r & 15))];
                 if (walk.whole) {
-                    if (c * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + row0 + r, c * 4, o, s_l[row0 + r], s_m[row0 + r]);
+                    if (c * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, c * 4, o, s_l[r], s_m[r]);
                 } else {
-                    *reinterpret_cast<f32x4 *>(part + (row0 + r) * D + c * 4) = o;
+                    *reinterpret_cast<f32x4 *>(part + r * D + c * 4) = o;
                     if (c == 0) {
-                        part[ROWS * D + row0 + r] = s_m[row0 + r];
-                        part[ROWS * (D + 1) + row0 + r] = s_l[row0 + r];
+                        part[ROWS * D + r] = s_m[r];
+                        part[ROWS * (D + 1) + r] = s_l[r];
                     }
                 }
             }
@@ -990,19 +992,18 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     }
 }
 
-constexpr int kJoinThreads = 1024;
-
 // Joins the parts of items that more than one work-group had.  A work-group for each
 // border between shares; the first border in an item does it.  Its lanes take four
 // channels of a row each, and where there are fewer of them than lanes, the parts in
 // turn: many parts (a long sequence alone) would else be read one after the other.
-// Sums are made in an order that the call's sizes alone decide.
-template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned groups)
+// Items of many rows have a work-group for each `some` of them.  Sums are made in an
+// order that the call's sizes alone decide.
+template <typename T, int D, int THREADS>
+__global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, int some)
 {
-    __shared__ typename Line<kJoinThreads>::Shared s_line;
-    __shared__ float s_sum[kJoinThreads][7];  // a maximum, a sum of exponentials, four of values; odd, for the banks
-    const Line<kJoinThreads> line(p, s_line);
+    __shared__ typename Line<THREADS>::Shared s_line;
+    __shared__ float s_sum[THREADS][7];  // a maximum, a sum of exponentials, four of values; odd, for the banks
+    const Line<THREADS> line(p, s_line);
     const unsigned total = line.total, each = share(total, groups), border = (blockIdx.x + 1) * each;
     if (border >= total) return;
     int b;
@@ -1014,6 +1015,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned gro
     const int most_rows = 1 << p.shape.rows_shift, head = (int)(item / (unsigned)seq.groups);
     const int row0 = (int)(item % (unsigned)seq.groups) * most_rows;
     const int rows = seq.tokens * p.shape.group - row0 < most_rows ? seq.tokens * p.shape.group - row0 : most_rows;
+    const int from_row = blockIdx.y * some;
+    if (from_row >= rows) return;
+    const int count = rows - from_row < some ? rows - from_row : some;
     const unsigned first = blockIdx.x, parts = (end - 1) / each - first + 1;
     auto part = [&](unsigned i) {
         const unsigned from = (first + i) * each;
@@ -1021,11 +1025,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args p, unsigned gro
     };
     // lanes to a part's sums: a power of two (with turns, one round: all elements have a lane)
     int lanes = D / 4;
-    while (lanes < rows * (D / 4) && lanes < kJoinThreads) lanes *= 2;
-    const int turns = kJoinThreads / lanes, turn = threadIdx.x / lanes;
-    for (int i = threadIdx.x % lanes; i - (int)(threadIdx.x % lanes) < rows * (D / 4); i += lanes) {
-        const int r = i / (D / 4), c = i % (D / 4) * 4;
-        const bool on = r < rows;
+    while (lanes < count * (D / 4) && lanes < THREADS) lanes *= 2;
+    const int turns = THREADS / lanes, turn = threadIdx.x / lanes;
+    for (int i = threadIdx.x % lanes; i - (int)(threadIdx.x % lanes) < count * (D / 4); i += lanes) {
+        const int r = from_row + i / (D / 4), c = i % (D / 4) * 4;
+        const bool on = i < count * (D / 4);
         float most = -__builtin_inff(), all = 0.f;
         f32x4 sum = (f32x4)0.f;
         auto add = [&](float m, float l, f32x4 o) {
@@ -1077,6 +1081,7 @@ int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 struct Form {
     int D, nq;
     bool wide;
+    int rows;                    // of an item, at most
     int rows_shift, unit_shift;  // of an item; of a unit: what a work-group's waves have in work
     int64_t groups;              // work-groups: what the card's LDS holds at once
     int64_t items;
@@ -1097,6 +1102,7 @@ Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64
     f.wide = rows > (f.D == 256 ? 16 : 32);
     f.nq = f.D < 256 && rows > (f.wide ? 64 : 16) ? 2 : 1;
     f.rows_shift = (f.wide ? 6 : 4) + (f.nq == 2);
+    f.rows = rows < 1 << f.rows_shift ? (int)rows : 1 << f.rows_shift;
     const int unit = f.wide ? 128 : stream_waves(row_bytes) * kTile;
     f.unit_shift = unit == 128 ? 7 : unit == 64 ? 6 : 5;
     f.items = B * heads * ((rows + (1 << f.rows_shift) - 1) >> f.rows_shift);
@@ -1120,7 +1126,11 @@ int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
     }
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
     if (!joined || f.groups == 1) return PK_OK;
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)(f.groups - 1)), dim3(kJoinThreads), 0, s, a, (unsigned)f.groups);
+    if (f.wide)
+        hipLaunchKernelGGL((join_kernel<T, D, 512>), dim3((unsigned)(f.groups - 1), (unsigned)(f.rows + 15) / 16), dim3(512), 0, s, a,
+                           (unsigned)f.groups, 16);
+    else
+        hipLaunchKernelGGL((join_kernel<T, D, 1024>), dim3((unsigned)(f.groups - 1)), dim3(1024), 0, s, a, (unsigned)f.groups, 32);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 
