@@ -812,15 +812,18 @@ struct Walk {
     line.find(walk.share_begin, walk.b, walk.base);                                                            \
     walk.seq = line.get(walk.b)
 
-// Few rows: the waves divide the positions.  Each has its own tiles, one on its way
-// while the one before is worked on, and nothing waits for another wave until their
-// sums are joined.
-template <typename T, int D, int NQ, int WAVES, bool COPIED>
+// Few rows: the waves divide the positions.  Each has its own tiles, with two STAGES one
+// on its way while the one before is worked on, and nothing waits for another wave until
+// their sums are joined.  One stage leaves room for twice the work-groups on a CU: for
+// calls in which each of them has a tile or two a wave.
+template <typename T, int D, int NQ, int WAVES, bool COPIED, int STAGES>
 __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
 {
     typedef Lds<T, D> L;
     constexpr int N = D / 16, ROWS = 16 * NQ, THREADS = WAVES * 64, STEP = WAVES * kTile;
-    constexpr int kHalf = kTile * L::kRow, kStages = COPIED ? 2 : 1, kWave = kStages * 2 * kHalf;
+    constexpr int kHalf = kTile * L::kRow, kWave = STAGES * 2 * kHalf;
+    constexpr bool kAhead = !COPIED || STAGES == 2;  // the next tile is begun before this one is worked on
+    static_assert(COPIED || STAGES == 1, "what is not copied waits in registers");
     constexpr int kSum = ROWS * (D + 4) * 4, kOwn = kWave > kSum ? kWave : (kSum + 1023) / 1024 * 1024;
     __shared__ __align__(1024) char s_raw[WAVES * kOwn];
     static_assert(kHalf % 1024 == 0 && kOwn % 1024 == 0, "tiles lie at multiples of 1 KiB");
@@ -828,8 +831,8 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_scratch[WAVES][kTile * 16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     char *const s_own = s_raw + wave * kOwn;
-    PK_WALK(THREADS);
     Mover<T, D, kTile, COPIED> mover(p, 0);
+    PK_WALK(THREADS);
     Rows<T, D, NQ> rows;
 
     for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
@@ -844,15 +847,20 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             char *const s_k = s_own + stage * 2 * kHalf;
             const unsigned there = (unsigned)__ballot(page >= 0);
             if (!first) mover.end(there, s_k, s_k + kHalf);
-            if (COPIED) stage ^= 1;
+            if (STAGES == 2) stage ^= 1;
             char *const s_next = s_own + stage * 2 * kHalf;
-            if (at + STEP < end) mover.begin(at + STEP, next, s_next, s_next + kHalf);
+            if (kAhead && at + STEP < end) mover.begin(at + STEP, next, s_next, s_next + kHalf);
             page = next;
             next = mover.page_at(at + 2 * STEP + lane % kTile, end);
-            if (first) continue;
-            own_lds();
-            const bool odd = at + kTile > length && mover.odd(s_k + kHalf);
-            rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
+            if (!first) {
+                own_lds();
+                const bool odd = at + kTile > length && mover.odd(s_k + kHalf);
+                rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
+            }
+            if (!kAhead && at + STEP < end) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this one has been read
+                mover.begin(at + STEP, page, s_next, s_next + kHalf);
+            }
         }
 
         // the waves' sums together
@@ -915,8 +923,8 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     __shared__ float s_scratch[4][kTile * 16], s_m[ROWS], s_l[ROWS];
     __shared__ int s_odd[2][4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
-    PK_WALK(256);
     Mover<T, D, OWN, COPIED> mover(p, wave * OWN);
+    PK_WALK(256);
     Rows<T, D, NQ> rows;
 
     for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
@@ -1064,11 +1072,21 @@ __global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, 
 #pragma unroll
             for (int j = 0; j < 4; ++j) mine[2 + j] = sum[j];
             __syncthreads();
-            if (turn == 0)
+            if (turn == 0) {
+                // their largest first, so that no turn's sum waits for another's
+#pragma unroll 4
+                for (int t = 1; t < turns; ++t) most = fmaxf(most, s_sum[threadIdx.x + t * lanes][0]);
+                float f = weight_of(mine[0], most);
+                all *= f;
+                sum *= f;
+#pragma unroll 4
                 for (int t = 1; t < turns; ++t) {
                     const float *other = s_sum[threadIdx.x + t * lanes];
-                    add(other[0], other[1], f32x4{other[2], other[3], other[4], other[5]});
+                    f = weight_of(other[0], most);
+                    all = fmaf(other[1], f, all);
+                    sum += f32x4{other[2], other[3], other[4], other[5]} * f;
                 }
+            }
         }
         if (turn == 0 && on && c < p.d) finish<T>(p, seq, head, row0 + r, c, sum, all, most);
     }
@@ -1080,7 +1098,7 @@ int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct Form {
     int D, nq;
-    bool wide;
+    bool wide, single;           // single: stream_kernel with one stage
     int rows;                    // of an item, at most
     int rows_shift, unit_shift;  // of an item; of a unit: what a work-group's waves have in work
     int64_t groups;              // work-groups: what the card's LDS holds at once
@@ -1110,6 +1128,8 @@ Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64
     const bool divided = f.items <= kMostLine / units;  // else an item is a unit
     const int64_t line = divided ? f.items * units : f.items;
     f.groups = 256 * (f.wide ? (row_bytes <= 512 ? 2 : 1) : row_bytes <= 128 ? 2 : 1);
+    f.single = !f.wide && line <= 4 * f.groups;
+    if (f.single) f.groups *= 2;
     if (f.groups > line) f.groups = line;
     f.bytes = units == 1 || !divided ? 0 : ((size_t)f.groups * 2 * (f.D + 2) << f.rows_shift) * sizeof(float);
     return f;
@@ -1122,7 +1142,10 @@ int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
         hipLaunchKernelGGL((wide_kernel<T, D, NQ, COPIED>), dim3((unsigned)f.groups), dim3(256), 0, s, a);
     } else {
         constexpr int WAVES = stream_waves(D * (int)sizeof(T));
-        hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES, COPIED>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
+        if (f.single || !COPIED)
+            hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES, COPIED, 1>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
+        else if constexpr (COPIED)
+            hipLaunchKernelGGL((stream_kernel<T, D, NQ, WAVES, COPIED, 2>), dim3((unsigned)f.groups), dim3(WAVES * 64), 0, s, a);
     }
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
     if (!joined || f.groups == 1) return PK_OK;
