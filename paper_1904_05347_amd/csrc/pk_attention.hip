@@ -233,7 +233,7 @@ template <typename T>
 __device__ __forceinline__ void finish(const Args &p, const Sequence &q, int head, int r, int c, f32x4 o, float l, float most)
 {
     const RowAt at = row_at(p, q, head, r);
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that saw nothing
+    const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);  // 0: a row that saw nothing
     T *to = (T *)p.out + at.m * p.out_token + at.h * p.out_head + c;
     typename Pack<T, 4>::V v;
 #pragma unroll
@@ -435,8 +435,9 @@ struct Mover {
             // (made here each time: a register for each copy's would be held through the loop)
             unsigned chunk_here = chunk;
             asm volatile("" : "+v"(chunk_here));
-            // all of K, then all of V; rows without a page, and chunks beyond the head's, are left out
-            auto copy = [&]<bool ALL>(unsigned there) {
+            const unsigned here = (unsigned)__ballot(page >= 0) & (unsigned)((1ull << ROWS) - 1);
+            if (here == (unsigned)((1ull << ROWS) - 1) && p.d == D) {
+                // all of K, then all of V
                 auto side = [&](const char *head, int64_t off, unsigned row, unsigned step, char *to) {
                     const char *start = nullptr;
 #pragma unroll
@@ -446,18 +447,28 @@ struct Mover {
                             start = from(head, off, i * L::kRows);
                         else
                             start += step;
-                        const unsigned c = chunk_here ^ L::turn(i * L::kRows);
-                        if (ALL || (there >> (i * L::kRows) & 1 && c < (unsigned)chunks))
-                            copy16(to + (first + i * L::kRows) * L::kRow, start, row + c * 16);
+                        copy16(to + (first + i * L::kRows) * L::kRow, start, row + (chunk_here ^ L::turn(i * L::kRows)) * 16);
                     }
                 };
                 side(key, k, key_row, (unsigned)p.key_place * (unsigned)(L::kRows * sizeof(T)), s_k);
                 side(value, v, value_row, (unsigned)p.value_place * (unsigned)(L::kRows * sizeof(T)), s_v);
-            };
-            if (p.d == D && __all(page >= 0))
-                copy.template operator()<true>(0);
-            else
-                copy.template operator()<false>((unsigned)__ballot(page >= 0));
+            } else if (here) {
+                // A sequence's end, or pages that are none: in the place of rows that hold nothing come
+                // others that do, so that nothing but these is ever read: their weights are 0, and a
+                // value that is no number is told by odd().  Chunks beyond the head's are left out.
+                const int any = __builtin_ctz(here);
+#pragma unroll 1
+                for (int i = 0; i < 2 * kCopies; ++i) {
+                    const bool is_key = i < kCopies;
+                    const int r0 = (is_key ? i : i - kCopies) * L::kRows, from_row = here >> r0 & 1 ? r0 : any;
+                    const unsigned c = chunk_here ^ L::turn(r0);
+                    // rows of a copy lie in one page, those that hold something before the others
+                    const bool holds = here >> (from_row + lane / L::kChunks) & 1;
+                    const unsigned row = holds ? (is_key ? key_row : value_row) : 0;
+                    const char *start = from(is_key ? key : value, is_key ? k : v, from_row);
+                    if (c < (unsigned)chunks) copy16((is_key ? s_k : s_v) + (first + r0) * L::kRow, start, row + c * 16);
+                }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) {
@@ -480,19 +491,18 @@ struct Mover {
             if (j < n) v[j] = from[j];
         return v;
     }
-    // What begin() began is in LDS (of this wave); `there`: the rows that hold something.  V's
-    // others become zeros: their weights are, but what was copied with them may be NaN.
+    // What begin() began is in LDS (of this wave); `there`: the rows that hold something.  Where
+    // there are none nothing was begun, and V's become zeros: their weights are, but LDS may hold NaN.
     __device__ __forceinline__ void end(uint64_t there, char *s_k, char *s_v) const
     {
         const int lane = threadIdx.x % 64;
         if constexpr (COPIED) {
-            constexpr uint64_t all = ROWS == 64 ? ~0ull : (1ull << ROWS % 64) - 1;
+            constexpr uint64_t all = (1ull << ROWS) - 1;
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            if ((there & all) != all) {
+            if (!(there & all)) {
                 f32x4 *to = reinterpret_cast<f32x4 *>(s_v + first * L::kRow);
 #pragma unroll 1
-                for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64)
-                    if (!(there >> (i / L::kChunks) & 1)) to[i] = (f32x4)0.f;
+                for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64) to[i] = (f32x4)0.f;
             }
         } else {
 #pragma unroll
@@ -503,12 +513,12 @@ struct Mover {
             }
         }
     }
-    // whether its rows of V have a NaN or an infinity
-    __device__ __forceinline__ bool odd(const char *s_v) const
+    // whether its rows of V, from row `from` of them on, have a NaN or an infinity
+    __device__ __forceinline__ bool odd(const char *s_v, int from) const
     {
         bool odd = false;
 #pragma unroll 1
-        for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64) {
+        for (unsigned i = (from < 0 ? 0 : from) * L::kChunks + lane_here(); i < ROWS * L::kChunks; i += 64) {
             const unsigned r = first + i / L::kChunks, c = i % L::kChunks ^ L::turn(r);
             const V v = *reinterpret_cast<const V *>(s_v + r * L::kRow + i % L::kChunks * 16);
 #pragma unroll
@@ -854,7 +864,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             next = mover.page_at(at + 2 * STEP + lane % kTile, end);
             if (!first) {
                 own_lds();
-                const bool odd = at + kTile > length && mover.odd(s_k + kHalf);
+                const bool odd = at + kTile > length && mover.odd(s_k + kHalf, length - at);
                 rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
             }
             if (!kAhead && at + STEP < end) {
@@ -944,7 +954,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
                 mover.end(there >> wave * OWN, s_k, s_v);
                 if (drafted) {
                     own_lds();
-                    const bool odd = mover.odd(s_v);
+                    const bool odd = mover.odd(s_v, length - at - wave * OWN);
                     if (lane == 0) s_odd[stage][wave] = odd;
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1278,7 +1288,10 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.value_place = cache->value_stride[1];
     a.value_head = cache->value_stride[2];
     a.pages = cache->pages;
-    a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.rows_shift, joined ? f.unit_shift : -1};
+    a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.rows_shift, joined ? f.unit_shift : -1,
+               // a few tokens after a context of a round length are no unit of their own, unless there are
+               // work-groups for it
+               f.single ? 0 : 1 << f.unit_shift >> 1};
     a.B = (int)B;
     a.d = (int)d;
     a.page_size = (int)cache->page_size;

@@ -33,6 +33,7 @@ struct Shape {
     int most;        // tokens of a sequence
     int rows_shift;  // rows of an item: a power of two
     int unit_shift;  // positions of a unit: a power of two; -1: an item is one unit
+    int tail;        // positions that an item's last unit takes beyond a unit's
 };
 
 struct Sequence {
@@ -59,9 +60,8 @@ PK_PLAN Sequence sequence(const Shape &s, int start, int end, int length)
     q.length = length < 0 ? 0 : length > s.capacity ? s.capacity : length;
     q.keys = q.length + (int)t < s.capacity ? q.length + (int)t : s.capacity;
     q.groups = ((int)t * s.group + (1 << s.rows_shift) - 1) >> s.rows_shift;
-    // An item without positions still writes its rows.  The last unit takes up to half a
-    // one more: a few tokens after a context of a round length are no unit of their own.
-    q.units = s.unit_shift < 0 ? 1 : (q.keys + (1 << s.unit_shift) / 2 - 1) >> s.unit_shift;
+    // An item without positions still writes its rows.
+    q.units = s.unit_shift < 0 ? 1 : (q.keys - s.tail + (1 << s.unit_shift) - 1) >> s.unit_shift;
     if (q.units < 1) q.units = 1;
     return q;
 }

@@ -30,13 +30,13 @@ void shim_tiling(int d, int pairs, int E, int64_t rows, int *out)
     out[5] = g.tokens;
 }
 
-void shim_sequence(int64_t M, int64_t capacity, int group, int most, int rows, int unit, int64_t start, int64_t end,
+void shim_sequence(int64_t M, int64_t capacity, int group, int most, int rows, int unit, int tail, int64_t start, int64_t end,
                    int64_t length, int64_t *out)
 {
     int rows_shift = 0, unit_shift = unit ? 0 : -1;
     while (1 << rows_shift < rows) ++rows_shift;
     while (unit && 1 << unit_shift < unit) ++unit_shift;
-    const pk::attention::Shape s = {(int)M, (int)capacity, 1, group, most, rows_shift, unit_shift};
+    const pk::attention::Shape s = {(int)M, (int)capacity, 1, group, most, rows_shift, unit_shift, tail};
     const pk::attention::Sequence q = pk::attention::sequence(s, (int)start, (int)end, (int)length);
     out[0] = q.first;
     out[1] = q.length;

@@ -228,12 +228,12 @@ def test_heads_fit_their_lanes(shim):
                         assert rounds * teams < rows + teams
 
 
-def _divide(shim, M, capacity, heads, group, most, rows, unit, starts, lengths, groups):
+def _divide(shim, M, capacity, heads, group, most, rows, unit, tail, starts, lengths, groups):
     """The kernel's walk: {(sequence, head, group): [(work-group, slot, begin, end)]}."""
     o = (ctypes.c_int64 * 6)()
     line = []
     for b in range(len(lengths)):
-        shim.shim_sequence(*(ctypes.c_int64(v) for v in (M, capacity)), group, most, rows, unit,
+        shim.shim_sequence(*(ctypes.c_int64(v) for v in (M, capacity)), group, most, rows, unit, tail,
                            *(ctypes.c_int64(v) for v in (starts[b], starts[b + 1], lengths[b])), o)
         for h in range(heads):
             for g in range(o[4]):
@@ -262,7 +262,7 @@ def test_units_are_divided_once(shim):
         starts = [0] + [int(x) for x in np.cumsum(tokens)]
         lengths = [int(x) for x in rng.integers(-3, 3000, B)]
         capacity, groups = int(rng.integers(1, 3000)), int(rng.integers(1, 40))
-        parts, total, each = _divide(shim, starts[-1], capacity, heads, group, 8, rows, 128, starts, lengths, groups)
+        parts, total, each = _divide(shim, starts[-1], capacity, heads, group, 8, rows, 128, int(rng.choice([0, 64])), starts, lengths, groups)
         used = {}
         for item, ps in parts.items():
             assert ps[0][2] == 0 and all(a[3] == b[2] for a, b in zip(ps, ps[1:]))
@@ -280,12 +280,12 @@ def test_indices_are_held_to_what_is_there(shim):
     o = (ctypes.c_int64 * 6)()
     odd = [0, 1, 5, 9, 10, 11, -1, -7, 2 ** 31 - 1, -2 ** 31, 64, 100]
     for start, end, length in itertools.product(odd, odd, odd):
-        for M, capacity, most in ((10, 48, 4), (10, 0, 64)):
-            shim.shim_sequence(ctypes.c_int64(M), ctypes.c_int64(capacity), 3, most, 16, 128, ctypes.c_int64(start), ctypes.c_int64(end),
+        for M, capacity, most, tail in ((10, 48, 4, 0), (10, 0, 64, 64), (10, 1000, 64, 64), (70, 1000, 64, 0)):
+            shim.shim_sequence(ctypes.c_int64(M), ctypes.c_int64(capacity), 3, most, 16, 128, tail, ctypes.c_int64(start), ctypes.c_int64(end),
                                ctypes.c_int64(length), o)
             first, n, keys, tokens, groups, units = o
             assert 0 <= tokens <= most and (tokens == 0 or 0 <= first and first + tokens <= M)
-            assert 0 <= n <= keys <= capacity and groups * 16 >= tokens * 3 and units >= 1 and units * 128 + 64 >= keys and (units == 1 or (units - 1) * 128 + 64 < keys)
+            assert 0 <= n <= keys <= capacity and groups * 16 >= tokens * 3 and units >= 1 and units * 128 + tail >= keys and (units == 1 or (units - 1) * 128 + tail < keys)
 
 
 # ------------------------------------------------------------------ the plain forms themselves
