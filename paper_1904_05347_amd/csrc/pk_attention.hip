@@ -1057,7 +1057,7 @@ __global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, 
             most = top;
         };
         if (on) {
-            constexpr int AT_ONCE = 4;
+            constexpr int AT_ONCE = THREADS == 1024 ? 4 : 8;  // (registers)
             for (unsigned w = turn; w < parts; w += turns * AT_ONCE) {
                 float m[AT_ONCE], l[AT_ONCE];
                 f32x4 o[AT_ONCE];
@@ -1113,6 +1113,7 @@ struct Form {
     int rows_shift, unit_shift;  // of an item; of a unit: what a work-group's waves have in work
     int64_t groups;              // work-groups: what the card's LDS holds at once
     int64_t items;
+    bool spare;    // no more units than work-groups
     size_t bytes;  // of the workspace
 };
 
@@ -1140,7 +1141,8 @@ Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64
     f.groups = 256 * (f.wide ? (row_bytes <= 512 ? 2 : 1) : row_bytes <= 128 ? 2 : 1);
     f.single = !f.wide && line <= 4 * f.groups;
     if (f.single) f.groups *= 2;
-    if (f.groups > line) f.groups = line;
+    f.spare = line <= f.groups;
+    if (f.spare) f.groups = line;
     f.bytes = units == 1 || !divided ? 0 : ((size_t)f.groups * 2 * (f.D + 2) << f.rows_shift) * sizeof(float);
     return f;
 }
@@ -1291,7 +1293,7 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     a.shape = {(int)M, (int)(P * cache->page_size), (int)heads, (int)group, (int)most, f.rows_shift, joined ? f.unit_shift : -1,
                // a few tokens after a context of a round length are no unit of their own, unless there are
                // work-groups for it
-               f.single ? 0 : 1 << f.unit_shift >> 1};
+               f.spare ? 0 : 1 << f.unit_shift >> 1};
     a.B = (int)B;
     a.d = (int)d;
     a.page_size = (int)cache->page_size;
