@@ -405,13 +405,16 @@ struct Mover {
         value = (const char *)((const T *)p.value + h * p.value_head);
         table = p.table + b * p.table_row;
     }
-    // the page that position j < end lies in, or -1
-    __device__ __forceinline__ int page_at(int j, int end) const
+    // What the table has for position j < end, else -1.  It is looked at, by page(), a tile later:
+    // here that would be waited for, and all copies that were begun before with it.
+    __device__ __forceinline__ int entry_at(int j, int end) const
     {
-        int page = -1;
-        if (j < end) page = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
-        return (unsigned)page < (uint64_t)p.pages ? page : -1;
+        int entry = -1;
+        if (j < end) entry = table[p.page_shift >= 0 ? j >> p.page_shift : (unsigned)j / (unsigned)p.page_size];
+        return entry;
     }
+    // the page, or -1
+    __device__ __forceinline__ int page(int entry) const { return (unsigned)entry < (uint64_t)p.pages ? entry : -1; }
     // The rows of the tile at position `at`, whose pages are `page` (row lane % 32 of what
     // this wave moves, or lane % 64 of 64), on their way to s_k and s_v, both at the tile's row 0.
     __device__ __forceinline__ void begin(int at, int page, char *s_k, char *s_v)
@@ -851,17 +854,18 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
         const int end = walk.end, length = walk.seq.length;
         // the first turn only brings the first tile: what brings a tile is here once
         int at = walk.begin + (wave - WAVES) * kTile, stage = 0;
-        int page = -1, next = mover.page_at(at + STEP + lane % kTile, end);
+        int page = -1, next = mover.entry_at(at + STEP + lane % kTile, end);
         rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, 16, walk.row0 + walk.rows, mover.chunks);
         for (bool first = true; at < end; at += STEP, first = false) {
             char *const s_k = s_own + stage * 2 * kHalf;
             const unsigned there = (unsigned)__ballot(page >= 0);
             if (!first) mover.end(there, s_k, s_k + kHalf);
             if (STAGES == 2) stage ^= 1;
+            next = mover.page(next);
             char *const s_next = s_own + stage * 2 * kHalf;
             if (kAhead && at + STEP < end) mover.begin(at + STEP, next, s_next, s_next + kHalf);
             page = next;
-            next = mover.page_at(at + 2 * STEP + lane % kTile, end);
+            next = mover.entry_at(at + 2 * STEP + lane % kTile, end);
             if (!first) {
                 own_lds();
                 const bool odd = at + kTile > length && mover.odd(s_k + kHalf, length - at);
@@ -942,7 +946,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
         mover.head(walk.b, walk.head);
         const int end = walk.end, length = walk.seq.length, row0 = wave * 16;
         int at = walk.begin - TILE, stage = 0;
-        int page = -1, next = mover.page_at(at + TILE + lane % TILE, end);
+        int page = -1, next = mover.entry_at(at + TILE + lane % TILE, end);
         const int sixteens = row0 >= walk.rows ? 0 : NQ == 2 && row0 + 64 < walk.rows ? 2 : 1;
         const bool mine = sixteens > 0;
         rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + row0, 64, walk.row0 + walk.rows, mover.chunks);
@@ -963,10 +967,11 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
             }
             const int now = stage;
             stage ^= 1;
+            next = mover.page(next);
             char *const s_next = s_raw + stage * 2 * kHalf;
             if (at + TILE < end) mover.begin(at + TILE, __shfl(next, wave * OWN + lane % OWN), s_next, s_next + kHalf);
             page = next;
-            next = mover.page_at(at + 2 * TILE + lane % TILE, end);
+            next = mover.entry_at(at + 2 * TILE + lane % TILE, end);
             if (first || !mine) continue;
             bool odd = false;
             if (drafted) odd = s_odd[now][0] | s_odd[now][1] | s_odd[now][2] | s_odd[now][3];
