@@ -868,7 +868,8 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             next = mover.entry_at(at + 2 * STEP + lane % kTile, end);
             if (!first) {
                 own_lds();
-                const bool odd = at + kTile > length && mover.odd(s_k + kHalf, length - at);
+                bool odd = false;
+                if (at + kTile > length || there != ~0u) odd = mover.odd(s_k + kHalf, there == ~0u ? length - at : 0);
                 rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
             }
             if (!kAhead && at + STEP < end) {
@@ -953,12 +954,12 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
         for (bool first = true; at < end; at += TILE, first = false) {
             char *const s_k = s_raw + stage * 2 * kHalf, *const s_v = s_k + kHalf;
             const uint64_t there = __ballot(page >= 0) & (TILE == 64 ? ~0ull : 0xffffffffull);
-            const bool drafted = at + TILE > length;
+            const bool some = at + TILE > length || there != (TILE == 64 ? ~0ull : 0xffffffffull);  // that not all rows see
             if (!first) {
                 mover.end(there >> wave * OWN, s_k, s_v);
-                if (drafted) {
+                if (some) {
                     own_lds();
-                    const bool odd = mover.odd(s_v, length - at - wave * OWN);
+                    const bool odd = mover.odd(s_v, there == (TILE == 64 ? ~0ull : 0xffffffffull) ? length - at - wave * OWN : 0);
                     if (lane == 0) s_odd[stage][wave] = odd;
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -974,7 +975,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
             next = mover.entry_at(at + 2 * TILE + lane % TILE, end);
             if (first || !mine) continue;
             bool odd = false;
-            if (drafted) odd = s_odd[now][0] | s_odd[now][1] | s_odd[now][2] | s_odd[now][3];
+            if (some) odd = s_odd[now][0] | s_odd[now][1] | s_odd[now][2] | s_odd[now][3];
             rows.template step<TILE / kTile>(p, s_k, s_v, at, length, there, odd, mover.chunks, s_scratch[wave]);
         }
 

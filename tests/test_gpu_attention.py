@@ -132,6 +132,62 @@ def test_nan_and_infinity_reach_the_rows_that_see_them(kind, D):
     assert out[5:, 3:].isnan().all() and torch.isfinite(out[:1]).all() and torch.isfinite(out[5, :3]).all()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_pages_that_are_none_beside_infinities(kind, D):
+    """Few rows and many: positions without a page, in tiles whose others hold infinities."""
+    torch, pk = require_gpu()
+    for T in (2, 40):
+        call = Call(torch, 21, [150], [T], 1, 2, D, kind, tree=False)
+        p = call.table[0].tolist()
+        call.vc[p[2], 3, 0, 5], call.vc[p[5], 1, 0, 6] = float("inf"), -float("inf")
+        call.table[0, 1], call.table[0, 4], call.table[0, 7] = -1, 1 << 20, -1
+        out, _ = call.check(pk, what="%d tokens" % T)
+        assert bool((out[..., 5] == float("inf")).all()) and bool((out[..., 6] == -float("inf")).all())
+        # a cache without pages at all
+        none = call.kc[:0]
+        out = pk.attention_tree(call.q, none, none, call.table, call.len, call.starts, T)
+        assert not out.any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,G,T", [(64, 2, 2), (128, 2, 2), (128, 8, 4), (200, 2, 2), (256, 1, 5)])
+def test_several_tiles_a_wave(kind, d, G, T):
+    """Long sequences: a wave goes from tile to tile, with two stages (a table of many more pages) and with one."""
+    torch, pk = require_gpu()
+    call = Call(torch, 5 + d, [20001, 77], [T, 1], 3, G, d, kind, page=16)
+    one, _ = call.check(pk, what="one stage")
+    call.table = torch.cat((call.table, torch.full((2, 20000), -1, dtype=torch.int32, device="cuda")), dim=1)
+    two, _ = call.check(pk, what="two stages")
+    if d <= 128:   # the shares are other ones, the sums' order too
+        assert float((one.double() - two.double()).abs().max()) < 0.02
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_many_rows_over_several_tiles(kind, d):
+    torch, pk = require_gpu()
+    call = Call(torch, 31 + d, [3001, 0, 700], [20, 5, 33], 2, 4, d, kind, page=48)
+    call.check(pk, what="wide")
+
+
+@pytest.mark.parametrize("page", [1, 7, 8, 16, 24, 40, 64, 256])
+def test_page_sizes_and_layouts_of_their_own(page):
+    """Keys and values laid out apart, from any element on."""
+    torch, pk = require_gpu()
+    for kind, d, T in (("bf16", 128, 1), ("f16", 80, 12), ("f32", 36, 3), ("bf16", 33, 20)):
+        call = Call(torch, page + d, [333, 1, 90], [T, 1, 2], 2, 4, d, kind, page)
+        n, size, Hk, _ = call.kc.shape
+        flat = torch.full((n * size * Hk * d + 1,), float("nan"), dtype=call.kc.dtype, device="cuda")
+        shifted = flat[1:].view(n, size, Hk, d)
+        shifted.copy_(call.kc)
+        call.kc = shifted
+        turned = torch.full((Hk, n, size, d + 8), float("nan"), dtype=call.vc.dtype, device="cuda")[..., :d].permute(1, 2, 0, 3)
+        turned.copy_(call.vc)
+        call.vc = turned
+        call.check(pk, what="page %d" % page)
+
+
 def test_scores_at_the_ends():
     """Large scores of both signs, and equal ones."""
     torch, pk = require_gpu()
@@ -143,7 +199,7 @@ def test_scores_at_the_ends():
 
 
 def test_indices_out_of_range_are_left_out():
-    """Host and device agree on what is left out (the same arithmetic as on the CPU in test_attention_cpu.py)."""
+    """Host and device agree on what is left out (its arithmetic is tested by itself on the CPU)."""
     torch, pk = require_gpu()
     call = Call(torch, 7, [100, 60, 30], [3, 2, 4], 2, 2, 64, "bf16")
     call.table[0, 1], call.table[1, 0], call.table[0, 3] = -5, 1 << 30, call.kc.shape[0]
