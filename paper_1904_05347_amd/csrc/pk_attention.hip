@@ -473,30 +473,50 @@ struct Mover {
                 }
             }
         } else {
+            // A head's last chunk is read with the elements before it, which whole() shifts out when
+            // they are there: element by element each load would be waited for (one sequence of
+            // 30000 positions, 4 heads of 255 fp16: 61 us, 342 so).
+            const auto each = [&](auto &&part) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const int r = i * L::kRows + lane / L::kChunks, c = lane % L::kChunks;
-                const int64_t ok = (int64_t)((uint64_t)(unsigned)__shfl((int)(k >> 32), r) << 32 | (unsigned)__shfl((int)k, r));
-                const int64_t ov = (int64_t)((uint64_t)(unsigned)__shfl((int)(v >> 32), r) << 32 | (unsigned)__shfl((int)v, r));
-                const int n = __shfl(page, r) >= 0 ? p.d - c * L::kElements : 0;
-                in_k[i] = part((const T *)(key + ok) + c * L::kElements, n);
-                in_v[i] = part((const T *)(value + ov) + c * L::kElements, n);
-            }
+                for (int i = 0; i < kCopies; ++i) {
+                    const int r = i * L::kRows + lane / L::kChunks, c = lane % L::kChunks;
+                    const int64_t ok = (int64_t)((uint64_t)(unsigned)__shfl((int)(k >> 32), r) << 32 | (unsigned)__shfl((int)k, r));
+                    const int64_t ov = (int64_t)((uint64_t)(unsigned)__shfl((int)(v >> 32), r) << 32 | (unsigned)__shfl((int)v, r));
+                    const int n = __shfl(page, r) >= 0 ? p.d - c * L::kElements : 0;
+                    in_k[i] = part((const T *)(key + ok) + c * L::kElements, n);
+                    in_v[i] = part((const T *)(value + ov) + c * L::kElements, n);
+                }
+            };
+            if (p.d >= L::kElements)
+                each([&](const T *from, int n) {
+                    V v = (V)(T)0.f;
+                    if (n > 0) v = *reinterpret_cast<const typename Pack<T>::U *>(from - lack(n));
+                    return v;
+                });
+            else
+                each([](const T *from, int n) {
+                    V v = (V)(T)0.f;
+#pragma unroll
+                    for (int j = 0; j < L::kElements; ++j)
+                        if (j < n) v[j] = from[j];
+                    return v;
+                });
         }
     }
-    // n elements from `from` on, zeros after them
-    static __device__ __forceinline__ V part(const T *from, int n)
+    // The elements that a head's last chunk lacks of a whole one (n are there), 0 for other chunks.
+    __device__ __forceinline__ int lack(int n) const
     {
-        V v = (V)(T)0.f;
-        if (n >= L::kElements) return *reinterpret_cast<const typename Pack<T>::U *>(from);
-#pragma unroll
-        for (int j = 0; j < L::kElements; ++j)
-            if (j < n) v[j] = from[j];
-        return v;
+        return n > 0 && n < L::kElements && p.d >= L::kElements ? L::kElements - n : 0;
+    }
+    // zeros after a last chunk's elements
+    static __device__ __forceinline__ V whole(V v, int lack)
+    {
+        typedef unsigned __int128 Bits;
+        return __builtin_bit_cast(V, __builtin_bit_cast(Bits, v) >> (lack * 8 * (int)sizeof(T)));
     }
     // What begin() began is in LDS (of this wave); `there`: the rows that hold something.  Where
     // there are none nothing was begun, and V's become zeros: their weights are, but LDS may hold NaN.
-    __device__ __forceinline__ void end(uint64_t there, char *s_k, char *s_v) const
+    __device__ __forceinline__ void end(uint64_t there, char *s_k, char *s_v)
     {
         const int lane = threadIdx.x % 64;
         if constexpr (COPIED) {
@@ -508,6 +528,11 @@ struct Mover {
                 for (unsigned i = lane_here(); i < ROWS * L::kChunks; i += 64) to[i] = (f32x4)0.f;
             }
         } else {
+            if (p.d % L::kElements) {
+                const int l = lack(p.d - lane % L::kChunks * L::kElements);
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) in_k[i] = whole(in_k[i], l), in_v[i] = whole(in_v[i], l);
+            }
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) {
                 const int r = first + i * L::kRows + lane / L::kChunks, c = lane % L::kChunks ^ L::turn(r);
@@ -1142,14 +1167,17 @@ Form form_of(int size, int64_t d, int64_t group, int64_t heads, int64_t B, int64
     f.unit_shift = unit == 128 ? 7 : unit == 64 ? 6 : 5;
     f.items = B * heads * ((rows + (1 << f.rows_shift) - 1) >> f.rows_shift);
     const int64_t units = capacity <= unit ? 1 : (capacity + unit - 1) / unit;
-    const bool divided = f.items <= kMostLine / units;  // else an item is a unit
+    // A few units are sooner done one after the other than joined by a second launch (32
+    // sequences of 400 positions, 8 heads of 128 bf16: 17.7 us, 24.5 divided; 1 of 250: 10.6 and
+    // 12.6; with four of 32 bits 1 of 250 takes 22.7, 16.8 divided).
+    const bool divided = units > (f.wide ? 1 : size == 2 ? 4 : 2) && f.items <= kMostLine / units;
     const int64_t line = divided ? f.items * units : f.items;
     f.groups = 256 * (f.wide ? (row_bytes <= 512 ? 2 : 1) : row_bytes <= 128 ? 2 : 1);
-    f.single = !f.wide && line <= 4 * f.groups;
+    f.single = !f.wide && (divided ? line <= 4 * f.groups : units == 1);
     if (f.single) f.groups *= 2;
     f.spare = line <= f.groups;
     if (f.spare) f.groups = line;
-    f.bytes = units == 1 || !divided ? 0 : ((size_t)f.groups * 2 * (f.D + 2) << f.rows_shift) * sizeof(float);
+    f.bytes = !divided ? 0 : ((size_t)f.groups * 2 * (f.D + 2) << f.rows_shift) * sizeof(float);
     return f;
 }
 

@@ -119,8 +119,8 @@ def test_append_arguments(lib):
 
 
 def test_attention_arguments(lib):
-    def wide(**more):   # three pages of 64: more than one unit, so that a workspace is used
-        return _cache(**{**dict(size=64, k=(1024, 16, 8), v=(1024, 16, 8)), **more})
+    def wide(**more):   # three pages of 256: enough units for a workspace to be used
+        return _cache(**{**dict(size=256, k=(4096, 16, 8), v=(4096, 16, 8)), **more})
 
     good = dict(dtype=0, M=3, d=8, q=_heads(1, 4, 32, 8), cache=wide(), table=4 * AT, B=2, P=3, ld=3, lengths=5 * AT, starts=6 * AT,
                 most=3, mask=7 * AT, scale=1.0, cap=0.0, out=_heads(8, 4, 32, 8), lse=9 * AT, ld_lse=4, ws=10 * AT, bytes=1 << 20)
@@ -143,7 +143,7 @@ def test_attention_workspace(lib):
     need = lib.pk_attention_tree_workspace_bytes
     # (type, channels, query heads, heads, sequences, pages, positions of a page, tokens)
     assert need(1, 128, 32, 8, 1, 256, 16, 1) > 0
-    assert need(1, 128, 32, 8, 1, 2, 16, 1) == 0          # one unit: nothing to divide
+    assert need(1, 128, 32, 8, 1, 32, 16, 1) == 0         # a few units: not divided
     for bad in ((3, 128, 32, 8, 1, 256, 16, 1), (1, 0, 32, 8, 1, 256, 16, 1), (1, 257, 32, 8, 1, 256, 16, 1), (1, 128, 31, 8, 1, 256, 16, 1),
                 (1, 128, 32, 0, 1, 256, 16, 1), (1, 128, 32, 8, 0, 256, 16, 1), (1, 128, 32, 8, 1, 0, 16, 1), (1, 128, 32, 8, 1, 256, 0, 1),
                 (1, 128, 32, 8, 1, 256, 16, 0), (1, 128, 32, 8, 1, 256, 16, 65), (1, 128, 32, 8, 1, 1 << 30, 1 << 30, 1)):

@@ -171,6 +171,21 @@ def test_many_rows_over_several_tiles(kind, d):
     call.check(pk, what="wide")
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [2, 3, 9, 10, 11, 12, 13, 14, 15, 250])
+def test_last_chunks_of_every_size(kind, d):
+    """A head's end inside 16 bytes, over several tiles of a few rows and of many; nothing beside a head's row is taken."""
+    torch, pk = require_gpu()
+    for T in (1, 9):
+        call = Call(torch, 71 + d, [700, 3], [T, 1], 3, 4, d, kind)
+        call.check(pk, what="T = %d" % T)
+        before = call.kc[:, :, 1:2].clone(), call.vc[:, :, 1:2].clone(), call.check(pk)[0][:, 4:8].clone()
+        call.kc.fill_(float("nan"))
+        call.vc.fill_(float("inf"))
+        call.kc[:, :, 1:2], call.vc[:, :, 1:2] = before[:2]
+        assert torch.equal(call(pk)[:, 4:8], before[2])
+
+
 @pytest.mark.parametrize("page", [1, 7, 8, 16, 24, 40, 64, 256])
 def test_page_sizes_and_layouts_of_their_own(page):
     """Keys and values laid out apart, from any element on."""

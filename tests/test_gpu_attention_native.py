@@ -86,7 +86,7 @@ def test_refusals(monkeypatch, native):
             lambda: attend(mask=s.mask.int()), lambda: attend(lse=s.lse.half()), lambda: attend(workspace=s.ws.half()), lambda: attend(q=None)],
         ValueError: [
             lambda: rope(q=s.q[0]), lambda: rope(k=s.k[:4]), lambda: rope(q=s.q[:, :, ::2]), lambda: rope(positions=s.positions[:4]),
-            lambda: rope(f=pk.rope_frequencies(33)), lambda: rope(f=None), lambda: rope(positions=None), lambda: rope(layout="neox"),
+            lambda: rope(f=pk.rope_frequencies(33)), lambda: rope(f=None), lambda: rope(positions=None), lambda: rope(layout="thirds"),
             lambda: rope(q_weight=s.w[:63]), lambda: rope(k=None, k_weight=s.w), lambda: rope(q_out=s.k), lambda: rope(k=None, k_out=s.k),
             lambda: back(q=None, q_weight=s.w), lambda: back(k=s.k[:4], k_weight=s.w), lambda: back(q_grad=s.k), lambda: back(dk=None, k_weight=s.w),
             lambda: append(v=s.v[:, :1]), lambda: append(kc=s.kc[0]), lambda: append(vc=s.vc[:8]), lambda: append(kc=s.kc[..., :63], vc=s.vc[..., :63]),
