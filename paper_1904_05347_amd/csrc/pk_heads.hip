@@ -13,7 +13,7 @@
 //
 // Memory bounds large calls: 8192 tokens of 40 heads of 128 bf16, normed, move 168 MB in
 // 40.8 us (4.1 TB/s, a large copy 5.1), 4100 tokens into a cache (50 heads of 128 fp16
-// with its v) 101 MB in 20.1 us, gradients of the first 252 MB in 66.8 us and 5.4.  One
+// with its v) 101 MB in 20.1 us, gradients of the first 252 MB in 67 us and 4.9.  One
 // token takes 3.6 us, which the launch and instructions from a cold cache fill.
 #include "pk_heads_checks.hpp"
 #include "pk_heads_launch.hpp"
@@ -548,8 +548,8 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
     }
 }
 
-// The rows of `partial` added up: 16 columns a work-group, 64 lanes a column.  (5.4 us for
-// 1.6 MB: a launch, a lane's dozen loads and the columns' sums, each a wait.)
+// The rows of `partial` added up: 16 columns a work-group, 64 lanes a column.  (3.5 us
+// for 1003 rows of 192: a launch, a lane's 16 loads and the columns' sums.)
 template <typename W>
 __global__ void __launch_bounds__(1024) weights_kernel(const float *partial, int groups, int d, W *q, W *k)
 {
@@ -557,8 +557,18 @@ __global__ void __launch_bounds__(1024) weights_kernel(const float *partial, int
     const int x = threadIdx.x % 16, y = threadIdx.x / 16, col = blockIdx.x * 16 + x;
     float v = 0.f;
     if (col < 2 * d) {
-#pragma unroll 16
-        for (int g = y; g < groups; g += 64) v += partial[(int64_t)g * 2 * d + col];
+        // 16 rows at once, the last in the place of those beyond it: the loads of a loop over
+        // what is left of them would be waited for one by one (7.2 us)
+        for (int g = y; g < groups; g += 16 * 64) {
+            float row[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = g + 64 * i;
+                row[i] = partial[(int64_t)(at < groups ? at : groups - 1) * 2 * d + col];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v += g + 64 * i < groups ? row[i] : 0.f;
+        }
     }
     v += __shfl_xor(v, 16);
     v += __shfl_xor(v, 32);
