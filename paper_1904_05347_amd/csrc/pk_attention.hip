@@ -17,7 +17,7 @@
 //
 // Few rows: bound by reading the cache (32 sequences of up to 8192 positions, 8 heads of
 // 128 bf16: 675 MB in 129 us, 5.2 TB/s; a large copy 5.1).  Many: by the matrix cores,
-// from about 400 rows a head (reached: 480 to 690 Tflop/s of a large product's 1234).
+// from about 400 rows a head (reached: 490 to 690 Tflop/s of a large product's 1234).
 // Small calls: by what is waited for one after the other, instructions from a cold cache
 // (about 30 ns for each 64 bytes), lengths, table, K, V, the joining launch.
 #include "pk_attention_plan.hpp"
@@ -182,13 +182,15 @@ struct Line {
         q.units = __builtin_amdgcn_readlane(mine.units, b);
         return q;
     }
+    // the units before sequence b, of up to 64
+    __device__ __forceinline__ unsigned before(int b) const { return b ? __builtin_amdgcn_readlane(end, b - 1) : 0; }
     // the sequence that has unit u < total, and the units before it
     __device__ __forceinline__ void find(unsigned u, int &b, unsigned &base) const
     {
         const int t = threadIdx.x;
         if (few) {
             b = __builtin_ctzll(__ballot(u < end));
-            base = b ? __builtin_amdgcn_readlane(end, b - 1) : 0;
+            base = before(b);
             return;
         }
         const unsigned before = t ? s.ends[t - 1] : 0;
@@ -860,7 +862,7 @@ struct Walk {
 // on its way while the one before is worked on, and nothing waits for another wave until
 // their sums are joined.  One stage leaves room for twice the work-groups on a CU: for
 // calls in which each of them has a tile or two a wave (3 sequences of 5000 positions, 4
-// heads of 64 fp32: 18.5 us in all, 2.5 less than with two; one token over 4096 positions,
+// heads of 64 fp32: 17.0 us in all, 2.5 less than with two; one token over 4096 positions,
 // 8 heads of 128 bf16: 11.0 us and 4.4 to join).
 template <typename T, int D, int NQ, int WAVES, bool COPIED, int STAGES>
 __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
@@ -958,7 +960,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
 // and V, of which each brings a fourth.  One barrier a tile: the one on its way goes
 // where the one before the last was read.
 // 16 trees of 16 tokens over 16384 positions, 8 heads of 128 bf16 with 4 query heads each:
-// 681 MB in 129 us (5.3 TB/s).  4 trees of 64 over 32768 with 8 query heads: 204 us, 98
+// 681 MB in 129 us (5.3 TB/s).  4 trees of 64 over 32768 with 8 query heads: 200 us, 98
 // Gflop, matrix cores busy 22 %: a tile of 64 positions takes a wave about 5600 clocks,
 // more of them the softmax's arithmetic and waits than products; and row groups of one
 // head at different places of their sequence read K and V past L2 each (1.03 GB; lengths
@@ -1057,33 +1059,56 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
 }
 
 // Joins the parts of items that more than one work-group had.  A work-group for each
-// border between shares; the first border in an item does it.  Its lanes take four
-// channels of a row each, and where there are fewer of them than lanes, the parts in
-// turn: many parts (a long sequence alone) would else be read one after the other.
-// Items of many rows have a work-group for each `some` of them (5 trees of 35 rows: 20.7 us
-// in all with 16, 22.4 with 32; 4 of 64 tokens, 4 heads of 256: 50 and 56).  Sums are made in an
-// order that the call's sizes alone decide.
+// border between shares (the first border in an item does it), or for each item where
+// these are fewer and sequences are lanes' (work-groups without anything to join take
+// their time too: 4 trees of 64 tokens, 4 heads of 256: 43 us in all, 50 by borders).  Its
+// lanes take four channels of a row each, and where there are fewer of them than lanes,
+// the parts in turn: many parts (a long sequence alone) would else be read one after the
+// other.  Items of many rows have a work-group for each `some` of them (the same trees by
+// borders: 50 us with 16, 56 with 32).  Sums are made in an order that the call's sizes
+// alone decide.
 template <typename T, int D, int THREADS>
-__global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, int some)
+__global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, int some, bool by_item)
 {
     __shared__ typename Line<THREADS>::Shared s_line;
     __shared__ float s_sum[THREADS][7];  // a maximum, a sum of exponentials, four of values; odd, for the banks
     const Line<THREADS> line(p, s_line);
-    const unsigned total = line.total, each = share(total, groups), border = (blockIdx.x + 1) * each;
-    if (border >= total) return;
-    int b;
+    const unsigned total = line.total, each = share(total, groups);
+    const int most_rows = 1 << p.shape.rows_shift;
+    int b, head, group = 0, from_row;
     unsigned base;
-    line.find(border, b, base);
-    const Sequence seq = line.get(b);
-    const unsigned item = (border - base) / (unsigned)seq.units, begin = base + item * seq.units, end = begin + seq.units;
-    if (begin == border || begin + each < border) return;
-    const int most_rows = 1 << p.shape.rows_shift, head = (int)(item / (unsigned)seq.groups);
-    const int row0 = (int)(item % (unsigned)seq.groups) * most_rows;
+    Sequence seq;
+    if (by_item) {
+        b = blockIdx.z;
+        head = blockIdx.y;
+        unsigned chunk = blockIdx.x;
+        if (THREADS == 512) {  // (few rows are one group)
+            const unsigned most_groups = (unsigned)(p.shape.most * p.shape.group + most_rows - 1) >> p.shape.rows_shift;
+            group = (int)(chunk % most_groups);
+            chunk /= most_groups;
+        }
+        from_row = (int)chunk * some;
+        base = line.before(b);
+        seq = line.get(b);
+        if (group >= seq.groups) return;
+    } else {
+        const unsigned border = (blockIdx.x + 1) * each;
+        if (border >= total) return;
+        line.find(border, b, base);
+        seq = line.get(b);
+        const unsigned item = (border - base) / (unsigned)seq.units;
+        head = (int)(item / (unsigned)seq.groups);
+        group = (int)(item % (unsigned)seq.groups);
+        from_row = blockIdx.y * some;
+    }
+    const unsigned begin = base + (unsigned)(head * seq.groups + group) * seq.units, end = begin + seq.units, first = begin / each;
+    // nothing to join, or an earlier border's
+    if ((end - 1) / each == first || (!by_item && first != blockIdx.x)) return;
+    const int row0 = group * most_rows;
     const int rows = seq.tokens * p.shape.group - row0 < most_rows ? seq.tokens * p.shape.group - row0 : most_rows;
-    const int from_row = blockIdx.y * some;
     if (from_row >= rows) return;
     const int count = rows - from_row < some ? rows - from_row : some;
-    const unsigned first = blockIdx.x, parts = (end - 1) / each - first + 1;
+    const unsigned parts = (end - 1) / each - first + 1;
     auto part = [&](unsigned i) {
         const unsigned from = (first + i) * each;
         return part_of<D>(p, first + i, slot_of(i ? from : begin, from));
@@ -1211,11 +1236,20 @@ int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
     }
     if (hipGetLastError() != hipSuccess) return PK_ERR_LAUNCH;
     if (!joined || f.groups == 1) return PK_OK;
+    const bool by_item = a.B <= 64 && a.shape.heads <= 65535 && f.items < f.groups;
+    // Rows of a work-group: of few items fewer, down to what gives a row's parts 16 turns of
+    // lanes (one tree of 16 tokens over 30000 positions, 1 head with 8 query heads: 26 us in
+    // all, 67 with 16 rows; 5 trees of 35 rows 18.4, 20.7).
+    int some = f.wide ? 16 : 32;
+    const int turn = (f.wide ? 512 : 1024) / 16 / (D / 4), least = turn > 1 ? turn : 1;
+    while (by_item && some > least && f.items * ((f.rows + some - 1) / some) < 256) some /= 2;
+    const unsigned chunks = (unsigned)(f.rows + some - 1) / some;
+    const dim3 grid = by_item ? dim3((unsigned)(f.items / a.B / a.shape.heads) * chunks, a.shape.heads, a.B)
+                              : dim3((unsigned)f.groups - 1, chunks);
     if (f.wide)
-        hipLaunchKernelGGL((join_kernel<T, D, 512>), dim3((unsigned)(f.groups - 1), (unsigned)(f.rows + 15) / 16), dim3(512), 0, s, a,
-                           (unsigned)f.groups, 16);
+        hipLaunchKernelGGL((join_kernel<T, D, 512>), grid, dim3(512), 0, s, a, (unsigned)f.groups, some, by_item);
     else
-        hipLaunchKernelGGL((join_kernel<T, D, 1024>), dim3((unsigned)(f.groups - 1)), dim3(1024), 0, s, a, (unsigned)f.groups, 32);
+        hipLaunchKernelGGL((join_kernel<T, D, 1024>), grid, dim3(1024), 0, s, a, (unsigned)f.groups, some, by_item);
     return hipGetLastError() == hipSuccess ? PK_OK : PK_ERR_LAUNCH;
 }
 

@@ -172,6 +172,19 @@ def test_many_rows_over_several_tiles(kind, d):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,Hk,T", [(70, 1, 1), (70, 2, 17), (40, 16, 1), (6, 1, 17), (1, 1, 33)])
+def test_joins_of_many_items_and_of_few(B, Hk, T, kind):
+    """Parts joined by borders (more than 64 sequences, more items than work-groups) and by items, uneven and empty ones among them."""
+    torch, pk = require_gpu()
+    lengths = [(997 * b * b) % 2500 if b % 5 else 0 for b in range(B)]
+    lengths[-1] = 3000
+    tokens = [1 + (b * 7) % T if b % 3 else T for b in range(B)]
+    tokens[B // 2] = 0 if B > 1 else T
+    call = Call(torch, B + Hk + T, lengths, tokens, Hk, 2, 64, kind)
+    call.check(pk, what="B = %d" % B)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("d", [2, 3, 9, 10, 11, 12, 13, 14, 15, 250])
 def test_last_chunks_of_every_size(kind, d):
     """A head's end inside 16 bytes, over several tiles of a few rows and of many; nothing beside a head's row is taken."""
