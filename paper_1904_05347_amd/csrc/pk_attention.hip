@@ -596,11 +596,21 @@ struct Rows {
     typedef Lds<T, D> L;
     static constexpr int C = D / 32, N = D / 16;
     static constexpr int kGroup = sizeof(T) == 2 ? 8 : 4;  // operands read from LDS at once: 32 registers
+    // Weights are exp2(score - origin + kLift), multiplied in T and summed in 32 bits.  bf16 holds
+    // them however small they are.  fp16 ends at 2^-25, and many positions that each have less than
+    // that beside one far above them may hold a share of the row together (one 17.5 above 2^17
+    // others: 0.3 %).  So in fp16 weights go up to 2^15, and a tile whose largest would have less
+    // than 2^(kLift - kFall) moves the origin down to it: the sums' 32 bits have room for what they then
+    // hold, for kSpan powers of two from the highest origin on.  (4 trees of 64 tokens over 32768
+    // positions, 64 heads over 8, of 128 fp16: 360 us, 355 without; what memory bounds is as it was.)
+    static constexpr bool kNarrow = sizeof(T) == 2 && !__is_same(T, bf16);
+    static constexpr float kLift = kNarrow ? 8.f : 0.f, kRise = kNarrow ? 7.f : 8.f, kFall = 12.f, kSpan = 60.f;
     V8 q[NQ][C];
     uint64_t word[NQ];  // the sequence's tokens that a row sees
     f32x4 o[NQ][N];     // sums of values: channels 16 i + 4 (l / 16) + 0..3
     float l[NQ];        // sums of exponentials: of this lane's positions
     float m[NQ];        // their origin, in the products' units
+    float highest[kNarrow ? NQ : 1];  // the highest that it had
 
     // Sixteens of rows from row0 on, `step` rows from one to the next; those from `rows` on are
     // the last one again, and are not stored.  WHOLE: rows are whole chunks of 16 bytes.
@@ -634,6 +644,7 @@ struct Rows {
                 }
             }
             m[n] = -__builtin_inff();
+            if constexpr (kNarrow) highest[n] = m[n];
             l[n] = 0.f;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
@@ -645,6 +656,16 @@ struct Rows {
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q[n][c][j] = (T)((float)q[n][c][j] * p.sign);
+    }
+
+    // What the sums of row n are relative to, in powers of two.
+    __device__ __forceinline__ float origin(const Args &p, int n) const { return m[n] * (p.cap != 0.f ? 1.f : p.scale) - kLift; }
+
+    // Whether a tile whose largest score is `most` moves the origin of row n down to it.
+    __device__ __forceinline__ bool falls(int n, float most, float scale) const
+    {
+        if constexpr (kNarrow) return (m[n] - most) * scale > kFall && (highest[n] - most) * scale <= kSpan;
+        return false;
     }
 
     // H tiles of 32 positions, from position `at` on; `there`: the positions that hold something;
@@ -738,14 +759,15 @@ struct Rows {
                 most[n] = fmaxf(fmaxf(most[n], x[n][e / 4][e % 4]), x[n][(e + 1) / 4][(e + 1) % 4]);
             most[n] = across(fmaxf(most[n], x[n][2 * H - 1][3]));
             // (both -infinity: nothing seen yet)
-            move |= (most[n] - m[n]) * scale > 8.f;
+            move |= (most[n] - m[n]) * scale > kRise || falls(n, most[n], scale);
         }
-        // the sums' origins move only where a weight would pass 2^8: they stay in range, and
+        // the sums' origins move only where a weight would pass 2^(kLift + kRise), or all be too small:
         // nearly no tile has them multiplied
         if (__any(move)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const float top = fmaxf(most[n], m[n]);
+                const float top = falls(n, most[n], scale) ? most[n] : fmaxf(most[n], m[n]);
+                if constexpr (kNarrow) highest[n] = fmaxf(highest[n], top);
                 const float shrink = m[n] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m[n] - top) * scale);
                 m[n] = top;
                 l[n] *= shrink;
@@ -755,10 +777,10 @@ struct Rows {
         }
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const float origin = m[n] == -__builtin_inff() ? 0.f : -m[n] * scale;
+            const float from = m[n] == -__builtin_inff() ? 0.f : kLift - m[n] * scale;
 #pragma unroll
             for (int e = 0; e < 8 * H; ++e) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e / 4][e % 4], scale, origin));
+                const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e / 4][e % 4], scale, from));
                 l[n] += w;
                 weight[n][e / 8][e % 8] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
             }
@@ -921,7 +943,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
             l += __shfl_xor(l, 32);
             if (g == 0) {
-                s_m[wave][n * 16 + col] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+                s_m[wave][n * 16 + col] = rows.origin(p, n);
                 s_l[wave][n * 16 + col] = l;
             }
 #pragma unroll
@@ -1031,7 +1053,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
                 float l = rows.l[n] + __shfl_xor(rows.l[n], 16);
                 l += __shfl_xor(l, 32);
                 if (g == 0) {
-                    s_m[r] = rows.m[n] * (p.cap != 0.f ? 1.f : p.scale);
+                    s_m[r] = rows.origin(p, n);
                     s_l[r] = l;
                 }
 #pragma unroll
