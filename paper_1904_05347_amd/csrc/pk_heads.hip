@@ -215,21 +215,6 @@ __device__ __forceinline__ Factor norm(float *z, float inv_d, int team, float ep
 // How a call's pairs lie.
 enum { UNTURNED, HALVES, NEIGHBOURS };
 
-// Which of its work-group's tokens and of their rows a team begins with.
-struct Slot {
-    int t, r;
-    __device__ __forceinline__ explicit Slot(const HeadsArgs &p)
-    {
-        const int slot = threadIdx.x >> p.team_shift;
-        t = 0;
-        r = slot;
-        if (p.tokens > 1) {
-            t = slot / p.rows;
-            r = t < p.tokens ? slot - t * p.rows : p.rows;
-        }
-    }
-};
-
 // The sides that lanes of this wave have, one after the other, each as a scalar: its
 // addresses and strides then need no selection for each lane, and most waves have
 // rows of one side.
@@ -259,9 +244,9 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
     typedef typename Pack<W, E>::V VW;
     extern __shared__ float2 s_turns[];
     const int c = threadIdx.x & (p.team - 1);
-    const Slot slot(p);
-    int r = slot.r;
-    const unsigned first = p.first + blockIdx.x * p.tokens, m = first + slot.t;
+    const pk::HeadStart slot = pk::head_start(threadIdx.x >> p.team_shift, p.tokens, p.rows);
+    int r = slot.row;
+    const unsigned first = p.first + blockIdx.x * p.tokens, m = first + slot.token;
     const Chunk<E, FULL> k(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, p.chunks, PAIRS == HALVES);
 
     struct Row {
@@ -344,7 +329,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
                 if constexpr (PAIRS != UNTURNED) {
                     if (k.pair) {
                         Turns<E> turns;
-                        turns.template load<FULL>(s_turns + slot.t * p.pairs + c * E, p.pairs - c * E);
+                        turns.template load<FULL>(s_turns + slot.token * p.pairs + c * E, p.pairs - c * E);
                         turns.template rotate<PAIRS == NEIGHBOURS, false>(z);
                     }
                 }
@@ -382,13 +367,13 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
     typedef typename Pack<W, E>::V VW;
     extern __shared__ float2 s_turns[];
     const int c = threadIdx.x & (p.team - 1);
-    const Slot slot(p);
+    const pk::HeadStart slot = pk::head_start(threadIdx.x >> p.team_shift, p.tokens, p.rows);
     const Chunk<E, FULL> ck(c, p.d, PAIRS ? p.pairs : 0, PAIRS ? p.pair_chunks : 0, p.chunks, PAIRS == HALVES);
     constexpr int SUMS = NORM ? 2 * E : 1;
     float sum_q[SUMS], sum_k[SUMS];  // ONE: sum_q is that side's
 #pragma unroll
     for (int j = 0; j < SUMS; ++j) sum_q[j] = sum_k[j] = 0.f;
-    const W *const weight_one = NORM ? (const W *)(slot.r < p.Hq ? p.q_weight : p.k_weight) : nullptr;
+    const W *const weight_one = NORM ? (const W *)(slot.row < p.Hq ? p.q_weight : p.k_weight) : nullptr;
     VW wa = (VW)(W)0.f, wb = wa;
     if (NORM && ONE && weight_one && ck.on) {
         wa = get<FULL, W, E>(weight_one + ck.oa, ck.na);
@@ -402,7 +387,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
     };
     auto fetch = [&](unsigned first, int row) {
         Row x;
-        const unsigned m = first + slot.t;
+        const unsigned m = first + slot.token;
         x.a = x.b = x.xa = x.xb = (Vec<T>)(T)0.f;
         x.to = nullptr;
         x.side = m >= p.M || row >= p.rows || !ck.on ? NONE : row < p.Hq ? QUERY : KEY;
@@ -427,7 +412,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
     const unsigned step = gridDim.x * p.tokens;
     int half = 0;
     unsigned first = blockIdx.x * p.tokens;
-    Row x = fetch(first, slot.r);
+    Row x = fetch(first, slot.row);
     for (; first < p.M; first += step, half ^= 1) {
         float2 *turns_here = s_turns + half * p.tokens * p.pairs;
         if constexpr (PAIRS != UNTURNED) {
@@ -435,10 +420,10 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
             make_turns(p, turns_here, first);
             __syncthreads();
         }
-        int r = slot.r;
+        int r = slot.row;
         for (int i = 0; i < (ONE ? 1 : p.rounds); ++i) {
             Row now = x;
-            x = !ONE && i + 1 < p.rounds ? fetch(first, r + p.teams) : fetch(first + step, slot.r);
+            x = !ONE && i + 1 < p.rounds ? fetch(first, r + p.teams) : fetch(first + step, slot.row);
             r += p.teams;
             float g[2 * E];
 #pragma unroll
@@ -449,7 +434,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
             if constexpr (PAIRS != UNTURNED) {
                 if (ck.pair) {
                     Turns<E> turns;
-                    turns.template load<FULL>(turns_here + slot.t * p.pairs + c * E, p.pairs - c * E);
+                    turns.template load<FULL>(turns_here + slot.token * p.pairs + c * E, p.pairs - c * E);
                     turns.template rotate<PAIRS == NEIGHBOURS, true>(g);
                 }
             }
@@ -507,7 +492,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_
     }
     if constexpr (NORM) {
         if (ONE) {
-            const bool query = slot.r < p.Hq;
+            const bool query = slot.row < p.Hq;
 #pragma unroll
             for (int j = 0; j < 2 * E; ++j) {
                 sum_k[j] = query ? 0.f : sum_q[j];

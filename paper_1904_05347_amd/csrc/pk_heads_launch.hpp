@@ -51,4 +51,18 @@ constexpr HeadGroup head_group(int64_t rows, int team, int pairs)
     return g;
 }
 
+// Which of its work-group's tokens and of their rows a team begins with.  A team without
+// any has the row `rows`, which is none, of a token whose angles are in LDS like the others'.
+struct HeadStart {
+    int token, row;
+};
+
+constexpr HeadStart head_start(int slot, int tokens, int rows)
+{
+    if (tokens == 1) return {0, slot};
+    const int token = slot / rows;
+    if (token >= tokens) return {0, rows};
+    return {token, slot - token * rows};
+}
+
 }  // namespace pk
