@@ -450,8 +450,8 @@ typedef struct {
  * Rotation of the first 2 * pairs channels of a head by its token's position:
  * pair i, of channels (i, i + pairs), or (2i, 2i + 1) where interleaved, becomes
  *   (a cos t - b sin t, b cos t + a sin t) * amplitude,  t = position * frequencies[i]
- * and the other channels stay.  t is formed in 64 bits and reduced there:
- * positions up to 2^40 lose nothing that 32 bits hold.  Contexts longer than a
+ * and the other channels stay.  t is reduced to less than a turn in 64 bits, before
+ * the product is rounded: positions up to 2^40 lose nothing that 32 bits hold.  Contexts longer than a
  * network was trained for are a matter of the frequencies and the amplitude.
  */
 typedef struct {

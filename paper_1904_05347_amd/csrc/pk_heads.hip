@@ -131,12 +131,17 @@ __device__ __forceinline__ float team_sum(float v, int team)
     return v;
 }
 
-// cos and sin of position * frequency, times the amplitude.  The angle is formed in
-// turns and reduced in 64 bits: 2^-52 of its turns, 2e-10 of one at position 2^20.
+// cos and sin of position * frequency, times the amplitude.  The angle is formed in turns
+// and reduced in 64 bits.  1 / (2 pi) and its product with the frequency are each held in two
+// of these, and the product with the position less whole turns is rounded once, so that no
+// position loses what 32 bits hold (up to 2^53, where a position is no longer exact in 64
+// bits).  With one 64-bit number for each, 2^40 radians would be off by 1.6e-4.
 __device__ __forceinline__ float2 turn_of(int64_t position, double frequency, float amplitude)
 {
-    const double turns = (double)position * (frequency * 0.15915494309189535);
-    const float half_turns = 2.f * (float)(turns - rint(turns));
+    constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;  // of 1 / (2 pi)
+    const double high = frequency * kHigh, low = fma(frequency, kHigh, -high) + frequency * kLow;
+    const double p = (double)position, turns = fma(p, low, fma(p, high, -rint(p * high)));
+    const float half_turns = 2.f * (float)turns;
     float s, c;
     sincospif(half_turns, &s, &c);
     return make_float2(c * amplitude, s * amplitude);
