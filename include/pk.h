@@ -539,7 +539,9 @@ int pk_cache_append(int dtype, int64_t M, int64_t head_size, const pk_heads *q, 
  *                 keep what `out` and `lse` hold.
  *   most          1 <= most <= 64 (else PK_ERR_NOT_SUPPORTED).
  *   mask          M words, or NULL.
- *   cap           >= 0.
+ *   scale         |scale| * log2(e) in fp32's range, as the scores times log2(e) have to be.
+ *   cap           >= 0; cap * log2(e) in fp32's range, and |scale| / cap, if not 0, among
+ *                 its normal numbers.
  *   out           as many heads as q, distinct from every input but q, whose memory
  *                 it may be (same strides).
  *   lse           the logarithm of each row's sum of exponentials, M x q heads, rows

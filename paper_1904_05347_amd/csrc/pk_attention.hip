@@ -25,6 +25,8 @@
 #include "pk_i8.hpp"
 #include "pk_i8_checks.hpp"
 
+#include <cmath>
+
 namespace {
 
 using namespace pk::attention;
@@ -51,7 +53,9 @@ struct Args {
     Shape shape;
     int B, d, page_size, page_shift;  // page_shift: of a power of two, else -1
     // scores are formed in powers of two: scale * log2(e), or scale / cap and cap * log2(e).
-    // scale is positive: q is multiplied by its sign (by 0, and scale is 1, for a scale of 0)
+    // scale is positive: q is multiplied by its sign (by 0, and scale is 1, for a scale of 0).
+    // All are held to what 32 bits hold: an infinite one would make NaN of scores of 0, a
+    // subnormal one has too few bits.
     float scale, cap, sign;
 };
 
@@ -1289,6 +1293,14 @@ int launch(const Args &a, const Form &f, bool copied, bool joined, hipStream_t s
     return copied ? launch<T, true>(a, f, joined, s) : launch<T, false>(a, f, joined, s);
 }
 
+// What products of queries and keys are multiplied by, once q has the scale's sign (and is zero for a
+// scale of 0): see Args.
+float factor_of(float scale, float cap)
+{
+    if (scale == 0.f) return 1.f;
+    return cap != 0.f ? std::fabs(scale) / cap : std::fabs(scale) * kLog2e;
+}
+
 // Whether K and V can be copied in whole chunks: 16-byte rows at 16-byte places, the
 // rows of a copy (up to 8) in one page, pages and places at 32-bit strides.
 bool can_copy(const pk_cache &c, int64_t d, int size)
@@ -1334,7 +1346,10 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     if (P < 0) return api_invalid(8);
     if (ld_table < P) return api_invalid(9);
     if (most < 1) return api_invalid(12);
-    if (!(cap >= 0.f) || cap > 3e38f) return api_invalid(15);
+    const float factor = factor_of(scale, cap), bound = cap * kLog2e;
+    if (cap == 0.f && std::isfinite(scale) && !std::isfinite(factor)) return api_invalid(14);
+    if (!(cap >= 0.f) || !std::isfinite(bound)) return api_invalid(15);
+    if (cap != 0.f && std::isfinite(scale) && !std::isnormal(factor)) return api_invalid(15);
     if (!out || out->heads != q->heads) return api_invalid(16);
     if (lse && ld_lse < q->heads) return api_invalid(18);
     if ((uintptr_t)workspace % 16) return api_invalid(19);
@@ -1407,9 +1422,8 @@ int pk_attention_tree(int dtype, int64_t M, int64_t d, const pk_heads *q, const 
     for (int i = 0; i < 31; ++i)
         if ((int64_t)1 << i == cache->page_size) a.page_shift = i;
     a.sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
-    a.scale = scale < 0.f ? -scale : scale == 0.f ? 1.f : scale;
-    a.scale = cap != 0.f ? a.scale / cap : a.scale * kLog2e;
-    a.cap = cap * kLog2e;
+    a.scale = factor;
+    a.cap = bound;
     hipStream_t s = (hipStream_t)stream;
     st = dtype == PK_F32 ? launch<float>(a, f, copied, joined, s) : dtype == PK_BF16 ? launch<bf16>(a, f, copied, joined, s) : launch<f16>(a, f, copied, joined, s);
     if (st == PK_OK) api_ran(f.wide ? (copied ? "attention_tree_wide" : "attention_tree_wide_read") : copied ? "attention_tree" : "attention_tree_read");
