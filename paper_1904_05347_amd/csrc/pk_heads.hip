@@ -686,7 +686,7 @@ int run_grad(int dtype, int weight_dtype, const HeadsArgs &a, int rows, void *q_
 int check_rotation(const pk_rotation *rot, int64_t d, bool read)
 {
     if (!rot) return PK_OK;
-    if (rot->pairs < 0 || 2 * rot->pairs > d) return PK_ERR_INVALID_VALUE;
+    if (rot->pairs < 0 || rot->pairs > d / 2) return PK_ERR_INVALID_VALUE;
     if (rot->pairs && read &&
         (!rot->positions || !rot->frequencies || (uintptr_t)rot->positions % 8 || (uintptr_t)rot->frequencies % 8))
         return PK_ERR_INVALID_VALUE;
