@@ -1309,7 +1309,7 @@ bool can_copy(const pk_cache &c, int64_t d, int size)
     for (int i = 0; i < 3; ++i)
         if (c.key_stride[i] * size % 16 || c.value_stride[i] * size % 16) return false;
     for (const int64_t *stride : {c.key_stride, c.value_stride})
-        if (stride[0] * size >= (int64_t)1 << 32 || stride[1] * size * c.page_size >= (int64_t)1 << 31) return false;
+        if (stride[0] * size >= (int64_t)1 << 32 || stride[1] * size > (((int64_t)1 << 31) - 1) / c.page_size) return false;
     return true;
 }
 

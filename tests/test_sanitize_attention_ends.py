@@ -5,7 +5,7 @@ import pytest
 from tests.test_sanitize import _run_child, _sanitized_library
 
 
-@pytest.mark.parametrize("file", ["test_rotation_pairs_cpu", "test_attention_factors_cpu"])
+@pytest.mark.parametrize("file", ["test_rotation_pairs_cpu", "test_attention_factors_cpu", "test_attention_strides_cpu"])
 def test_ends_under_asan_ubsan(file):
     lib, rt = _sanitized_library()
     code = "import sys, pytest\nsys.exit(pytest.main(['-x', '-q', '-p', 'no:cacheprovider', 'tests/%s.py']))\n" % file
