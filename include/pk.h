@@ -554,9 +554,9 @@ int pk_cache_append(int dtype, int64_t M, int64_t head_size, const pk_heads *q, 
  *                 not overlap another argument.  Contents on return are unspecified.
  *                 Two calls that overlap in time must not share it.
  * 16-bit operands are multiplied exactly and summed in fp32, as are the softmax's
- * statistics; its weights are multiplied by the values in 16 bits (fp32: in 32), each
- * rounded by half a unit at most (fp16: or by 2^-21 of the largest among up to 64
- * neighbours).
+ * statistics; its weights are multiplied by the values in two parts of 16 bits (fp32: in
+ * 32), together within 2^-16 of each (fp16: 2^-20, or 2^-23 of the largest among up to
+ * 64 neighbours).
  */
 size_t pk_attention_tree_workspace_bytes(int dtype, int64_t head_size, int64_t q_heads, int64_t heads,
                                          int64_t B, int64_t P, int64_t page_size, int64_t most);

@@ -97,6 +97,48 @@ __device__ __forceinline__ f32x4 product(Eight<float>::V a, Eight<float>::V b, f
     return c;
 }
 
+// Softmax's weights for the matrix instruction.  One number of 16 bits would be off by as much as
+// the result's own rounding (2^-8 in bf16, 2^-11 in fp16), so it is two: the weight cut off, and what
+// is left, together within 2^-16 of it in bf16, 2^-20 in fp16 (or 2^-23, two of its least numbers).
+// The products by V double for it.  Of calls over 4096 to 32768 positions the error against 64
+// bits was 1.08 to 1.42 times that of the result's rounding alone, and now is that.  4 trees of 64
+// tokens over up to 32768 positions, 64 heads over 8 of 128 bf16, took 201 us and take 229 (all of
+// 32768 in fp16 360 and 447), small fp16 calls 19.8 for 18.5, what memory bounds up to 1.5 % more.
+template <typename T>
+struct Weights {
+    typename Eight<T>::V first, second;
+    // w[i / 4][i % 4] is weight i
+    __device__ __forceinline__ void set(const f32x4 (&w)[2])
+    {
+        if constexpr (__is_same(T, bf16)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // the upper half of its bits; and 2^-21 more than is left, so that the second is above 0
+                // as well: an infinite value times 0 would be no number
+                const unsigned upper = __float_as_uint(w[i / 4][i % 4]) & 0xffff0000u;
+                first[i] = __builtin_bit_cast(bf16, (unsigned short)(upper >> 16));
+                second[i] = (bf16)fmaf(w[i / 4][i % 4], 1.f + 0x1p-21f, -__uint_as_float(upper));
+            }
+        } else if constexpr (sizeof(T) == 2) {
+            typedef T T2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                // (as many bits as fp16 has; infinite values: stray())
+                float left[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    left[j] = w[i / 4][i % 4 + j] - __uint_as_float(__float_as_uint(w[i / 4][i % 4 + j]) & 0xffffe000u);
+                const T2 f = __builtin_bit_cast(T2, __builtin_amdgcn_cvt_pkrtz(w[i / 4][i % 4], w[i / 4][i % 4 + 1]));
+                const T2 r = __builtin_bit_cast(T2, __builtin_amdgcn_cvt_pkrtz(left[0], left[1]));
+                first[i] = f[0], first[i + 1] = f[1], second[i] = r[0], second[i + 1] = r[1];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) first[i] = w[i / 4][i % 4];
+        }
+    }
+};
+
 // tanh, to 2 units in the last place.  The exponential's form would lose digits
 // below 0.6: there x (1 + x^2 P(x^2)), P a least-squares fit whose error is 2^-30 of
 // the result.
@@ -382,6 +424,10 @@ __device__ __forceinline__ void copy16(char *to, const char *base, unsigned off)
     asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(at), "v"(off), "s"(base) : "memory");
 }
 
+// fp16, whose least numbers are not far below 1.
+template <typename T>
+constexpr bool narrow = sizeof(T) == 2 && !__is_same(T, bf16);
+
 // What one wave brings of an item's K and V into LDS: ROWS rows of a tile, from row
 // `first` of it on (a multiple of 8).
 //   COPIED   straight from memory: rows are whole chunks at multiples of 16 bytes, and a
@@ -580,6 +626,11 @@ __device__ __forceinline__ void own_lds()
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
+// Whether a sum of values is infinite or no number.  An infinite value times a weight that fp16 does not
+// hold makes that of what is infinite: where there are such sums a part is gone through again, carefully,
+// with weights of 32 bits for all values that are no finite numbers.
+__device__ __forceinline__ bool stray(f32x4 sum) { return !(sum[0] * 0.f + sum[1] * 0.f + sum[2] * 0.f + sum[3] * 0.f == 0.f); }
+
 // The larger of v in lanes 16 and 32 apart, in all of them.
 __device__ __forceinline__ float across(float v)
 {
@@ -600,15 +651,14 @@ struct Rows {
     typedef Lds<T, D> L;
     static constexpr int C = D / 32, N = D / 16;
     static constexpr int kGroup = sizeof(T) == 2 ? 8 : 4;  // operands read from LDS at once: 32 registers
-    // Weights are exp2(score - origin + kLift), multiplied in T and summed in 32 bits.  bf16 holds
-    // them however small they are.  fp16 ends at 2^-25, and many positions that each have less than
-    // that beside one far above them may hold a share of the row together (one 17.5 above 2^17
-    // others: 0.3 %).  So in fp16 weights go up to 2^15, and a tile whose largest would have less
-    // than 2^(kLift - kFall) moves the origin down to it: the sums' 32 bits have room for what they then
-    // hold, for kSpan powers of two from the highest origin on.  (4 trees of 64 tokens over 32768
-    // positions, 64 heads over 8, of 128 fp16: 360 us, 355 without; what memory bounds is as it was.)
-    static constexpr bool kNarrow = sizeof(T) == 2 && !__is_same(T, bf16);
-    static constexpr float kLift = kNarrow ? 8.f : 0.f, kRise = kNarrow ? 7.f : 8.f, kFall = 12.f, kSpan = 60.f;
+    // Weights are exp2(score - origin + kLift).  bf16 holds them however small they are.  fp16 ends at
+    // 2^-24, and many positions that each have less than that beside one far above them may hold a
+    // share of the row together (one 17.5 above 2^17 others: 0.3 %).  So in fp16 weights go up to
+    // 2^15, and a tile whose largest would have less than 2^(kLift - kFall) moves the origin down to
+    // it: the sums' 32 bits have room for what they then hold, for kSpan powers of two from the
+    // highest origin on.
+    static constexpr bool kNarrow = narrow<T>;
+    static constexpr float kLift = kNarrow ? 8.f : 0.f, kRise = kNarrow ? 7.f : 8.f, kFall = 8.f, kSpan = 60.f;
     V8 q[NQ][C];
     uint64_t word[NQ];  // the sequence's tokens that a row sees
     f32x4 o[NQ][N];     // sums of values: channels 16 i + 4 (l / 16) + 0..3
@@ -647,11 +697,6 @@ struct Rows {
                         q[n][c] = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
                 }
             }
-            m[n] = -__builtin_inff();
-            if constexpr (kNarrow) highest[n] = m[n];
-            l[n] = 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
         }
         if (p.sign == 1.f) return;
 #pragma unroll
@@ -660,6 +705,18 @@ struct Rows {
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q[n][c][j] = (T)((float)q[n][c][j] * p.sign);
+    }
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            m[n] = -__builtin_inff();
+            if constexpr (kNarrow) highest[n] = m[n];
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[n][i] = (f32x4)0.f;
+        }
     }
 
     // What the sums of row n are relative to, in powers of two.
@@ -715,7 +772,8 @@ struct Rows {
         else
             scores.template operator()<true>();
         // the first columns of V on their way while the weights are made
-        constexpr int G = N < kGroup ? N : kGroup;
+        // (4 at once where a wave has 32 rows: 8 would spill registers)
+        constexpr int G = NQ == 2 || N < kGroup ? 4 : kGroup;
         V8 v[G];
         const typename L::ColumnReader column(s_v, lane);
 #pragma unroll
@@ -723,7 +781,6 @@ struct Rows {
         __builtin_amdgcn_sched_barrier(0);
 
         const bool drafted = at + H * kTile > length;
-        V8 weight[NQ][H];
         float scale = p.scale;
         if (p.cap != 0.f) {
 #pragma unroll
@@ -786,11 +843,14 @@ struct Rows {
             for (int e = 0; e < 8 * H; ++e) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(x[n][e / 4][e % 4], scale, from));
                 l[n] += w;
-                weight[n][e / 8][e % 8] = (T)w;  // to 16 bits, for the matrix instruction; the sum is of all 32
+                x[n][e / 4][e % 4] = w;
             }
         }
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+        for (int h = 0; h < H; ++h) {
+            Weights<T> weight[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) weight[n].set({x[n][2 * h], x[n][2 * h + 1]});
 #pragma unroll
             for (int from = 0; from < N; from += G) {
                 if (h || from) {
@@ -807,8 +867,15 @@ struct Rows {
 #pragma unroll
                 for (int i = 0; i < G; ++i)
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n][h], o[n][from + i]);
+                    for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n].first, o[n][from + i]);
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) o[n][from + i] = product(v[i], weight[n].second, o[n][from + i]);
+                }
             }
+        }
         if (!odd) return;
         // a NaN or an infinity reaches the rows that see it and no other: the products were made
         // with zeros in their places, and here what they add is added position by position
@@ -818,7 +885,7 @@ struct Rows {
             for (int h = 0; h < H; ++h) {
                 own_lds();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) scratch[(e / 4 * 16 + g * 4 + e % 4) * 16 + col] = (float)weight[n][h][e];
+                for (int e = 0; e < 8; ++e) scratch[(e / 4 * 16 + g * 4 + e % 4) * 16 + col] = x[n][2 * h + e / 4][e % 4];
                 own_lds();
                 const unsigned s = (unsigned)(seen(n) >> (h * kTile));
 #pragma unroll 1
@@ -903,20 +970,24 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
     static_assert(kHalf % 1024 == 0 && kOwn % 1024 == 0, "tiles lie at multiples of 1 KiB");
     __shared__ typename Line<THREADS>::Shared s_line;
     __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS], s_scratch[WAVES][kTile * 16];
+    __shared__ int s_strays[WAVES];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     char *const s_own = s_raw + wave * kOwn;
     Mover<T, D, kTile, COPIED> mover(p, 0);
     PK_WALK(THREADS);
     Rows<T, D, NQ> rows;
 
-    for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
+    bool careful = false;
+    for (unsigned u = walk.share_begin; u < walk.share_end;) {
         walk.at(p, u);
         mover.head(walk.b, walk.head);
         const int end = walk.end, length = walk.seq.length;
         // the first turn only brings the first tile: what brings a tile is here once
         int at = walk.begin + (wave - WAVES) * kTile, stage = 0;
         int page = -1, next = mover.entry_at(at + STEP + lane % kTile, end);
-        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, 16, walk.row0 + walk.rows, mover.chunks);
+        // (a second time what it has: `out` may be q's memory)
+        if (!careful) rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0, 16, walk.row0 + walk.rows, mover.chunks);
+        rows.clear();
         for (bool first = true; at < end; at += STEP, first = false) {
             char *const s_k = s_own + stage * 2 * kHalf;
             const unsigned there = (unsigned)__ballot(page >= 0);
@@ -930,7 +1001,8 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             if (!first) {
                 own_lds();
                 bool odd = false;
-                if (at + kTile > length || there != ~0u) odd = mover.odd(s_k + kHalf, there == ~0u ? length - at : 0);
+                if (careful || at + kTile > length || there != ~0u)
+                    odd = mover.odd(s_k + kHalf, there == ~0u && !careful ? length - at : 0);
                 rows.template step<1>(p, s_k, s_k + kHalf, at, length, there, odd, mover.chunks, s_scratch[wave]);
             }
             if (!kAhead && at + STEP < end) {
@@ -954,6 +1026,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
             for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4 *>(s_o + (n * 16 + col) * (D + 4) + i * 16 + g * 4) = rows.o[n][i];
         }
         __syncthreads();
+        bool strays = false;
         float *part = walk.whole ? nullptr : part_of<D>(p, walk.rank, slot_of(walk.part_begin, walk.share_begin));
         for (int i = threadIdx.x; i < walk.rows * (D / 4); i += THREADS) {
             const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -968,6 +1041,7 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
                 sum += *reinterpret_cast<const f32x4 *>(s_raw + w * kOwn + (r * (D + 4) + c) * 4) * f;
                 all += s_l[w][r] * f;
             }
+            if constexpr (narrow<T>) strays |= c < p.d && stray(sum);
             if (walk.whole) {
                 if (c < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, c, sum, all, most);
             } else {
@@ -978,7 +1052,19 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
                 }
             }
         }
+        if constexpr (narrow<T>) {
+            strays = __any(strays);
+            if (lane == 0) s_strays[wave] = strays;
+        }
         __syncthreads();
+        if constexpr (narrow<T>) {
+            // (waves write here again behind the next barrier)
+            strays = false;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) strays |= s_strays[w] != 0;
+            careful = !careful && strays;
+        }
+        if (!careful) u = walk.part_end;
     }
 }
 
@@ -1004,13 +1090,14 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
     __shared__ typename Line<256>::Shared s_line;
     static_assert(ROWS * D * 4 <= 4 * kHalf, "the sums fit the stages");
     __shared__ float s_scratch[4][kTile * 16], s_m[ROWS], s_l[ROWS];
-    __shared__ int s_odd[2][4];
+    __shared__ int s_odd[2][4], s_strays[4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     Mover<T, D, OWN, COPIED> mover(p, wave * OWN);
     PK_WALK(256);
     Rows<T, D, NQ> rows;
 
-    for (unsigned u = walk.share_begin; u < walk.share_end; u = walk.part_end) {
+    bool careful = false;
+    for (unsigned u = walk.share_begin; u < walk.share_end;) {
         walk.at(p, u);
         mover.head(walk.b, walk.head);
         const int end = walk.end, length = walk.seq.length, row0 = wave * 16;
@@ -1018,16 +1105,19 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
         int page = -1, next = mover.entry_at(at + TILE + lane % TILE, end);
         const int sixteens = row0 >= walk.rows ? 0 : NQ == 2 && row0 + 64 < walk.rows ? 2 : 1;
         const bool mine = sixteens > 0;
-        rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + row0, 64, walk.row0 + walk.rows, mover.chunks);
+        // (a second time what it has: `out` may be q's memory)
+        if (!careful) rows.template load<COPIED>(p, walk.seq, walk.head, walk.row0 + row0, 64, walk.row0 + walk.rows, mover.chunks);
+        rows.clear();
         for (bool first = true; at < end; at += TILE, first = false) {
             char *const s_k = s_raw + stage * 2 * kHalf, *const s_v = s_k + kHalf;
             const uint64_t there = __ballot(page >= 0) & (TILE == 64 ? ~0ull : 0xffffffffull);
-            const bool some = at + TILE > length || there != (TILE == 64 ? ~0ull : 0xffffffffull);  // that not all rows see
+            const bool whole = there == (TILE == 64 ? ~0ull : 0xffffffffull) && !careful;
+            const bool some = at + TILE > length || !whole;  // that not all rows see
             if (!first) {
                 mover.end(there >> wave * OWN, s_k, s_v);
                 if (some) {
                     own_lds();
-                    const bool odd = mover.odd(s_v, there == (TILE == 64 ? ~0ull : 0xffffffffull) ? length - at - wave * OWN : 0);
+                    const bool odd = mover.odd(s_v, whole ? length - at - wave * OWN : 0);
                     if (lane == 0) s_odd[stage][wave] = odd;
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1049,6 +1139,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
 
         // each wave's sums through LDS, where the tiles were, so that what stores them is here once
         __syncthreads();  // the last tile has been read
+        bool strays = false;
         if (mine) {
             f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw);
 #pragma unroll
@@ -1069,6 +1160,7 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
                 const int c = i % (D / 4), r = row0 + i / (D / 4) / 16 * 64 + i / (D / 4) % 16;
                 if (r >= walk.rows) break;
                 const f32x4 o = s_o[r * (D / 4) + (c ^ (r & 15))];
+                if constexpr (narrow<T>) strays |= c * 4 < p.d && stray(o);
                 if (walk.whole) {
                     if (c * 4 < p.d) finish<T>(p, walk.seq, walk.head, walk.row0 + r, c * 4, o, s_l[r], s_m[r]);
                 } else {
@@ -1080,7 +1172,13 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
                 }
             }
         }
+        if constexpr (narrow<T>) {
+            strays = __any(strays);
+            if (lane == 0) s_strays[wave] = strays;
+        }
         __syncthreads();  // and the sums
+        if constexpr (narrow<T>) careful = !careful && (s_strays[0] | s_strays[1] | s_strays[2] | s_strays[3]);
+        if (!careful) u = walk.part_end;
     }
 }
 

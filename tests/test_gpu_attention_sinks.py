@@ -42,8 +42,8 @@ def _sequence(torch, kind, scores, values, d, T, G, seed):
 def _check(torch, pk, kind, scores, values, d, T, G, what):
     """A score is one product, exact but for its factor log2(e) and the largest's subtraction (4 U of the
     largest score each), an exponential is off by 2 units; sums of n / 4 + 64 steps; a weight is rounded to 16 bits,
-    half a step, and what is below its type's least number is of tiles of 64 positions whose largest has
-    at least 2^-4, half a step of the least number being 2^-25: 2^-15 of a tile's share."""
+    half a step, at most, and off by two of its type's least numbers where the largest of its tile of 64 positions has
+    at least 1: fewer than 2^-15 of a tile's share."""
     s = _sequence(torch, kind, scores, values, d, T, G, len(scores) + d + T)
     n = len(scores)
     v = _f64(s["held"])
