@@ -852,7 +852,12 @@ def rope_qk(q, k, positions, frequencies, q_weight=None, k_weight=None, eps=1e-6
     ``layout`` tells the pairs: 'half' (i, i + pairs) or 'interleaved' (2i, 2i + 1);
     channels from 2 * pairs on stay as they are.  ``q_weight`` and ``k_weight`` (the
     heads' type or float32) are the norms' weights, None for no norm; ``amplitude``
-    multiplies what is rotated.  ``q_out`` may be ``q`` and ``k_out`` ``k``."""
+    multiplies what is rotated.  ``q_out`` may be ``q`` and ``k_out`` ``k``.
+
+    As all calls of this module it records no graph: its results require no gradient,
+    whatever q, k and the weights do, and autograd is not told that ``q_out`` and ``k_out``
+    are written (none of its graphs may have saved them).  A training step calls
+    ``rope_qk_backward``, by itself or from a torch.autograd.Function of both."""
     r = (_native or _load_native()).rope_qk(q, k, positions, frequencies, q_weight, k_weight, eps, layout, amplitude, q_out, k_out)
     if r is not None:
         return r
