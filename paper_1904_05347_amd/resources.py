@@ -18,6 +18,15 @@ import sys
 
 from .build import RESOURCE_LOG
 
+# what the table's columns are, at its head
+LEGEND = """\
+# Per-kernel registers, spills, LDS and occupancy of every compiled instance (gfx950)
+# command: python -m paper_1904_05347_amd.build && python -m paper_1904_05347_amd.resources
+# source: the compiler's -Rpass-analysis=kernel-resource-usage remarks kept by the build
+# vgpr/agpr: vector / accumulation registers per lane; vspill/sspill: spilled registers; scratch: bytes per lane;
+# lds: static LDS per work-group (dynamic LDS, sized at launch, shows 0); occ: waves per SIMD the registers allow
+"""
+
 _FIELDS = {"VGPRs": "vgpr", "AGPRs": "agpr", "TotalSGPRs": "sgpr", "ScratchSize [bytes/lane]": "scratch",
            "Occupancy [waves/SIMD]": "occupancy", "SGPRs Spill": "sgpr_spill", "VGPRs Spill": "vgpr_spill",
            "LDS Size [bytes/block]": "lds"}
@@ -67,7 +76,7 @@ def table(path: str = RESOURCE_LOG) -> str:
     names = sorted(kernels)
     plain = dict(zip(names, demangle(names)))
     rows = sorted(((kernels[n]["file"], short(plain[n]), kernels[n]) for n in names), key=lambda r: r[:2])
-    out = ["%-22s %-96s %5s %5s %5s %6s %6s %6s %7s %4s" % ("file", "kernel", "vgpr", "agpr", "sgpr", "vspill",
+    out = LEGEND.splitlines() + ["%-22s %-96s %5s %5s %5s %6s %6s %6s %7s %4s" % ("file", "kernel", "vgpr", "agpr", "sgpr", "vspill",
                                                             "sspill", "scratch", "lds", "occ")]
     for f, k, d in rows:
         out.append("%-22s %-96s %5d %5d %5d %6d %6d %6d %7d %4d" % (
