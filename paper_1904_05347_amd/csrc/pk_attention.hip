@@ -16,8 +16,8 @@
 // out of LDS transposed.
 //
 // Few rows: bound by reading the cache (32 sequences of up to 8192 positions, 8 heads of
-// 128 bf16: 675 MB in 129 us, 5.2 TB/s; a large copy 5.1).  Many: by the matrix cores,
-// from about 400 rows a head (reached: 490 to 690 Tflop/s of a large product's 1234).
+// 128 bf16: 675 MB in 133 us, 5.1 TB/s, as a large copy).  Many: by the matrix cores,
+// from about 400 rows a head (reached: 440 to 665 Tflop/s of a large product's 1234).
 // Small calls: by what is waited for one after the other, instructions from a cold cache
 // (about 30 ns for each 64 bytes), lengths, table, K, V, the joining launch.
 #include "pk_attention_plan.hpp"
@@ -102,8 +102,8 @@ __device__ __forceinline__ f32x4 product(Eight<float>::V a, Eight<float>::V b, f
 // is left, together within 2^-16 of it in bf16, 2^-20 in fp16 (or 2^-23, two of its least numbers).
 // The products by V double for it.  Of calls over 4096 to 32768 positions the error against 64
 // bits was 1.08 to 1.42 times that of the result's rounding alone, and now is that.  4 trees of 64
-// tokens over up to 32768 positions, 64 heads over 8 of 128 bf16, took 201 us and take 229 (all of
-// 32768 in fp16 360 and 447), small fp16 calls 19.8 for 18.5, what memory bounds up to 1.5 % more.
+// tokens over up to 32768 positions, 64 heads over 8 of 128 bf16, took 199 us and take 223 (all of
+// 32768 in fp16 348 and 439), small fp16 calls 19.7 for 18.4, what memory bounds up to 1.5 % more.
 template <typename T>
 struct Weights {
     typename Eight<T>::V first, second;
@@ -139,7 +139,7 @@ struct Weights {
     }
 };
 
-// tanh, to 2 units in the last place.  The exponential's form would lose digits
+// tanh, to 1.7 units in the last place (the worst of all numbers from 1e-30 to 20, tried on this card).  The exponential's form would lose digits
 // below 0.6: there x (1 + x^2 P(x^2)), P a least-squares fit whose error is 2^-30 of
 // the result.
 __device__ __forceinline__ float tanh_of(float x)
@@ -533,7 +533,7 @@ struct Mover {
         } else {
             // A head's last chunk is read with the elements before it, which whole() shifts out when
             // they are there: element by element each load would be waited for (one sequence of
-            // 30000 positions, 4 heads of 255 fp16: 61 us, 342 so).
+            // 30000 positions, 4 heads of 255 fp16: 57 us, 342 so).
             const auto each = [&](auto &&part) {
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i) {
@@ -956,7 +956,7 @@ struct Walk {
 // their sums are joined.  One stage leaves room for twice the work-groups on a CU: for
 // calls in which each of them has a tile or two a wave (3 sequences of 5000 positions, 4
 // heads of 64 fp32: 17.0 us in all, 2.5 less than with two; one token over 4096 positions,
-// 8 heads of 128 bf16: 11.0 us and 4.4 to join).
+// 8 heads of 128 bf16: 11.9 us and 5.0 to join under the profiler, 16.2 in all without).
 template <typename T, int D, int NQ, int WAVES, bool COPIED, int STAGES>
 __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
 {
@@ -1059,10 +1059,10 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
         __syncthreads();
         if constexpr (narrow<T>) {
             // (waves write here again behind the next barrier)
-            strays = false;
+            int any = 0;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) strays |= s_strays[w] != 0;
-            careful = !careful && strays;
+            for (int w = 0; w < WAVES; ++w) any |= s_strays[w];
+            careful = !careful && __builtin_amdgcn_readfirstlane(any);  // (a scalar, as the walk is)
         }
         if (!careful) u = walk.part_end;
     }
@@ -1072,12 +1072,11 @@ __global__ void __launch_bounds__(WAVES * 64) stream_kernel(Args p)
 // and V, of which each brings a fourth.  One barrier a tile: the one on its way goes
 // where the one before the last was read.
 // 16 trees of 16 tokens over 16384 positions, 8 heads of 128 bf16 with 4 query heads each:
-// 681 MB in 129 us (5.3 TB/s).  4 trees of 64 over 32768 with 8 query heads: 200 us, 98
-// Gflop, matrix cores busy 22 %: a tile of 64 positions takes a wave about 5600 clocks,
-// more of them the softmax's arithmetic and waits than products; and row groups of one
-// head at different places of their sequence read K and V past L2 each (1.03 GB; lengths
-// that divide evenly reach 688 Tflop/s).  Copies of the next tile begun between the
-// products spilled (440 us).
+// 681 MB in 139 us (4.9 TB/s).  4 trees of 64 over up to 32768 with 8 query heads: 223 us, 98
+// Gflop (V's products, made twice, counted once), matrix cores busy 30 %: the rest is the softmax's
+// arithmetic and waits; and row groups of one head at different places of their sequence read K
+// and V past L2 each (1.03 GB; lengths that divide evenly reach 665 Tflop/s).  Copies of the
+// next tile begun between the products spilled (440 us, when the whole took 200).
 template <typename T, int D>
 constexpr int wide_tile() { return D * (int)sizeof(T) <= 256 ? 64 : 32; }
 
@@ -1177,7 +1176,8 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
             if (lane == 0) s_strays[wave] = strays;
         }
         __syncthreads();  // and the sums
-        if constexpr (narrow<T>) careful = !careful && (s_strays[0] | s_strays[1] | s_strays[2] | s_strays[3]);
+        if constexpr (narrow<T>)
+            careful = !careful && __builtin_amdgcn_readfirstlane(s_strays[0] | s_strays[1] | s_strays[2] | s_strays[3]);
         if (!careful) u = walk.part_end;
     }
 }
@@ -1185,7 +1185,8 @@ __global__ void __launch_bounds__(256, D * sizeof(T) <= 512 ? 2 : 1) wide_kernel
 // Joins the parts of items that more than one work-group had.  A work-group for each
 // border between shares (the first border in an item does it), or for each item where
 // these are fewer and sequences are lanes' (work-groups without anything to join take
-// their time too: 4 trees of 64 tokens, 4 heads of 256: 43 us in all, 50 by borders).  Its
+// their time too: 4 trees of 64 tokens, 4 heads of 256: 43 us in all, 50 by borders, with 3 us
+// less for the first launch than now).  Its
 // lanes take four channels of a row each, and where there are fewer of them than lanes,
 // the parts in turn: many parts (a long sequence alone) would else be read one after the
 // other.  Items of many rows have a work-group for each `some` of them (the same trees by
@@ -1300,6 +1301,11 @@ __global__ void __launch_bounds__(THREADS) join_kernel(Args p, unsigned groups, 
 
 // ------------------------------------------------------------------ launches
 
+// Channels that a head takes in registers and LDS.  Heads of other sizes do the products of the
+// zeros beside them, and their rows are copied by a loop, not by a run of instructions: the 16 trees
+// of wide_kernel's comment, all of 16384 positions, take 119 us with 64 channels, 219 with 80, 218
+// with 128, its 4 trees, all of 32768, 292, 532 and 414.  Each size more would be 30 instances of
+// these kernels.
 int padded(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct Form {
@@ -1307,7 +1313,10 @@ struct Form {
     bool wide, single;           // single: stream_kernel with one stage
     int rows;                    // of an item, at most
     int rows_shift, unit_shift;  // of an item; of a unit: what a work-group's waves have in work
-    int64_t groups;              // work-groups: what the card's LDS holds at once
+    // Work-groups: what the LDS of most forms that copy lets the card hold at once.  Of the others
+    // (16-bit heads of up to 64 channels with one stage, three a CU; through registers, one or two) the
+    // last begin when the first have ended.
+    int64_t groups;
     int64_t items;
     bool spare;    // no more units than work-groups
     size_t bytes;  // of the workspace
@@ -1362,7 +1371,7 @@ int launch(const Args &a, const Form &f, bool joined, hipStream_t s)
     if (!joined || f.groups == 1) return PK_OK;
     const bool by_item = a.B <= 64 && a.shape.heads <= 65535 && f.items < f.groups;
     // Rows of a work-group: of few items fewer, down to what gives a row's parts 16 turns of
-    // lanes (one tree of 16 tokens over 30000 positions, 1 head with 8 query heads: 26 us in
+    // lanes (one tree of 16 tokens over 30000 positions, 1 head with 8 query heads: 27 us in
     // all, 67 with 16 rows; 5 trees of 35 rows 18.4, 20.7).
     int some = f.wide ? 16 : 32;
     const int turn = (f.wide ? 512 : 1024) / 16 / (D / 4), least = turn > 1 ? turn : 1;

@@ -12,9 +12,9 @@
 // and makes them once, into LDS.
 //
 // Memory bounds large calls: 8192 tokens of 40 heads of 128 bf16, normed, move 168 MB in
-// 40.8 us (4.1 TB/s, a large copy 5.1), 4100 tokens into a cache (50 heads of 128 fp16
-// with its v) 101 MB in 20.1 us, gradients of the first 252 MB in 67 us and 4.9.  One
-// token takes 3.6 us, which the launch and instructions from a cold cache fill.
+// 41.3 us (4.1 TB/s, a large copy 5.1), 4100 tokens into a cache (50 heads of 128 fp16
+// with its v) 101 MB in 21.1 us, gradients of the first 252 MB in 67.3 us and 4.7 (medians).
+// One token takes 3.6 us, which the launch and instructions from a cold cache fill.
 #include "pk_heads_checks.hpp"
 #include "pk_heads_launch.hpp"
 #include "pk_i8.hpp"
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(pk::kMostHeadThreads) heads_kernel(HeadsArgs p
 // worked on.
 // ONE: a team has the same head of every token, so that its lanes have one side's
 // weights and sums.
-// (60.7 to 66.8 us for 252 MB, 8192 tokens of 40 heads of 128 bf16; a tenth less than the
+// (67.3 us for 252 MB, 8192 tokens of 40 heads of 128 bf16, 61 at the least; a tenth less than the
 // forward kernel's rate: 21 % of the waves' cycles issue arithmetic, 61 % wait.)
 template <typename T, typename W, bool NORM, int PAIRS, bool FULL, bool ONE>
 __global__ void __launch_bounds__(pk::kMostHeadThreads, ONE ? 4 : 3) heads_grad_kernel(HeadsArgs p)
