@@ -114,7 +114,7 @@ struct Weights {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // the upper half of its bits; and 2^-21 more than is left, so that the second is above 0
-                // as well: an infinite value times 0 would be no number
+                // as well (down to weights of 2^-112): an infinite value times 0 would be no number
                 const unsigned upper = __float_as_uint(w[i / 4][i % 4]) & 0xffff0000u;
                 first[i] = __builtin_bit_cast(bf16, (unsigned short)(upper >> 16));
                 second[i] = (bf16)fmaf(w[i / 4][i % 4], 1.f + 0x1p-21f, -__uint_as_float(upper));
@@ -139,9 +139,9 @@ struct Weights {
     }
 };
 
-// tanh, to 1.7 units in the last place (the worst of all numbers from 1e-30 to 20, tried on this card).  The exponential's form would lose digits
-// below 0.6: there x (1 + x^2 P(x^2)), P a least-squares fit whose error is 2^-30 of
-// the result.
+// tanh, to 1.7 units in the last place (the worst of all numbers from 1e-30 to 20, tried on
+// an MI355X).  The exponential's form would lose digits below 0.6: there x (1 + x^2 P(x^2)), P a
+// least-squares fit whose error is 2^-30 of the result.
 __device__ __forceinline__ float tanh_of(float x)
 {
     const float y = fabsf(x), z = x * x;
