@@ -745,7 +745,10 @@ struct Rows {
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
             for (int h = 0; h < 2 * H; ++h) x[n][h] = (f32x4)0.f;
-        // (reads in groups before their products: one by one each product would wait for its own)
+        // (reads in groups before their products: one by one each product would wait for its own.)
+        // fp32's 32 channels are summed by themselves and added, since 256 in a row round up to
+        // three times as far off as a plain product's sums: 500 positions of 256 channels 3.2e-7
+        // from 64 bits, 1.6e-6 in one sum, for 2 to 6 % of large calls' time.
         const typename L::RowReader row(s_k, lane);
         auto scores = [&]<bool PART>() {
             constexpr int G = C < kGroup / 2 ? C : kGroup / 2;
@@ -760,11 +763,18 @@ struct Rows {
                         for (int i = 0; i < 2; ++i) k[c][i] = row.template get<PART>(h + i, from + c, chunks);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int c = 0; c < G; ++c)
+                    for (int c = 0; c < G; ++c) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int n = 0; n < NQ; ++n) x[n][h + i] = product(k[c][i], q[n][from + c], x[n][h + i]);
+                            for (int n = 0; n < NQ; ++n) {
+                                if constexpr (sizeof(T) == 2)
+                                    x[n][h + i] = product(k[c][i], q[n][from + c], x[n][h + i]);
+                                else
+                                    x[n][h + i] += product(k[c][i], q[n][from + c], (f32x4)0.f);
+                            }
+                        if constexpr (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
         };
         if (p.d == D)
